@@ -1,6 +1,7 @@
 """ctypes binding of libtperm.so: same names as the C ABI in include/tperm.h (the product
-boundary) and include/tperm_tuning.h (overrides, candidate enumeration and the host-side index
-map, for tests and sweeps).
+boundary), include/tperm_experts.h (the operators of a mixture-of-experts layer) and
+include/tperm_tuning.h (overrides, candidate enumeration and the host-side index map, for tests and
+sweeps).
 
 Argument marshalling only.  Every step of the transpose runs in the library's kernels;
 there is no Python or CPU fallback: if the shared library is missing, loading fails.
@@ -38,6 +39,10 @@ EXPORTS = ["tperm_plan_create", "tperm_plan_create_forced", "tperm_plan_create_m
            "tperm_cache_tune", "tperm_cache_stats", "tperm_cache_clear",
            "tperm_product_create", "tperm_product_accumulate", "tperm_product_describe",
            "tperm_product_destroy"]
+# include/tperm_experts.h
+EXPERT_EXPORTS = ["tperm_expert_sort", "tperm_expert_gather", "tperm_expert_combine", "tperm_expert_combine_backward",
+                  "tperm_expert_product", "tperm_expert_weight_gradient", "tperm_checkpoint_store",
+                  "tperm_checkpoint_load", "tperm_gated_forward", "tperm_gated_backward"]
 # include/tperm_tuning.h
 TUNING_EXPORTS = ["tperm_plan_create_ex", "tperm_plan_candidate_count", "tperm_plan_create_candidate",
                   "tperm_plan_index_map", "tperm_plan_model", "tperm_plan_launch_info", "tperm_multiset_compare",
@@ -149,13 +154,14 @@ def lib() -> ctypes.CDLL:
         L.tperm_product_destroy.argtypes = [vp]
         L.tperm_status_string.argtypes = [ctypes.c_int]
         L.tperm_status_string.restype = ctypes.c_char_p
-        for name in EXPORTS + TUNING_EXPORTS:
+        for name in EXPORTS + EXPERT_EXPORTS + TUNING_EXPORTS:
             if name != "tperm_status_string":
                 getattr(L, name).restype = ctypes.c_int
         from . import _fastcall
         _fastcall.bind(*(ctypes.cast(getattr(L, name), vp).value for name in (
             "tperm_execute", "tperm_execute_accumulate", "tperm_execute_verified", "tperm_transpose",
             "tperm_transpose_accumulate", "tperm_product_accumulate")))
+        _fastcall.bind_experts(*(ctypes.cast(getattr(L, name), vp).value for name in EXPERT_EXPORTS))
         _fast = _fastcall
         _lib = L
     return _lib
@@ -468,6 +474,117 @@ def tperm_product_accumulate(product: Product, left_ptr: int, right_ptr: int, ou
     st = _fast.product(product._addr, left_ptr, right_ptr, out_ptr, workspace_ptr, stream, workspace_bytes)
     if st != OK:
         raise TpermError(st, "tperm_product_accumulate")
+
+
+# include/tperm_experts.h.  Pointers are ints or None (NULL); sizes count elements and rows.
+TYPE_F32, TYPE_F16, TYPE_BF16 = range(3)
+TYPES = {"f32": TYPE_F32, "f16": TYPE_F16, "bf16": TYPE_BF16}
+EXPERTS_MAX, SLOTS_MAX, WIDTH_MAX = 1024, 64, 1 << 20
+EXPERT_SORT_ONE_BLOCK = 8192
+
+
+def expert_sort_workspace_bytes(rows: int, experts: int) -> int:
+    """TPERM_EXPERT_SORT_WORKSPACE_BYTES of the header."""
+    return 0 if rows <= EXPERT_SORT_ONE_BLOCK else 256 * (int(experts) + 1) * 4
+
+
+def checkpoint_blocks(width: int) -> int:
+    """TPERM_CHECKPOINT_BLOCKS of the header."""
+    return (int(width) + 31) // 32
+
+
+def _calls():
+    if _fast is None:
+        lib()
+    return _fast
+
+
+def tperm_expert_sort(expert_ptr: int, tokens: int, slots: int, experts: int, offsets_ptr: int, source_ptr: int,
+                      place_ptr: int, workspace_ptr: Optional[int] = None, workspace_bytes: int = 0, stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_sort(expert_ptr, tokens, slots, experts, offsets_ptr, source_ptr, place_ptr,
+                                         workspace_ptr, workspace_bytes, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_sort")
+
+
+def tperm_expert_gather(x_ptr: int, x_stride: int, source_ptr: int, offsets_ptr: int, weights_ptr: Optional[int],
+                        out_ptr: int, out_stride: int, tokens: int, slots: int, experts: int, width: int, dtype: int,
+                        stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_gather(x_ptr, x_stride, source_ptr, offsets_ptr, weights_ptr, out_ptr, out_stride,
+                                           tokens, slots, experts, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_gather")
+
+
+def tperm_expert_combine(rows_ptr: int, rows_stride: int, place_ptr: int, offsets_ptr: int, weights_ptr: Optional[int],
+                         out_ptr: int, out_stride: int, tokens: int, slots: int, experts: int, width: int, dtype: int,
+                         stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_combine(rows_ptr, rows_stride, place_ptr, offsets_ptr, weights_ptr, out_ptr, out_stride,
+                                            tokens, slots, experts, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_combine")
+
+
+def tperm_expert_combine_backward(grad_ptr: int, grad_stride: int, rows_ptr: int, rows_stride: int, place_ptr: int,
+                                  offsets_ptr: int, weights_ptr: int, grad_rows_ptr: int, grad_rows_stride: int,
+                                  grad_weights_ptr: int, tokens: int, slots: int, experts: int, width: int, dtype: int,
+                                  stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_combine_backward(grad_ptr, grad_stride, rows_ptr, rows_stride, place_ptr, offsets_ptr,
+                                                     weights_ptr, grad_rows_ptr, grad_rows_stride, grad_weights_ptr,
+                                                     tokens, slots, experts, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_combine_backward")
+
+
+def tperm_expert_product(x_ptr: int, x_stride: int, x_rows: int, source_ptr: Optional[int], slots: int, offsets_ptr: int,
+                         w_ptr: int, w_k_first: bool, out_ptr: int, out_stride: int, rows: int, experts: int, k: int,
+                         n: int, dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_product(x_ptr, x_stride, x_rows, source_ptr, slots, offsets_ptr, w_ptr, w_k_first,
+                                            out_ptr, out_stride, rows, experts, k, n, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_product")
+
+
+def tperm_expert_weight_gradient(x_ptr: int, x_stride: int, x_scales_ptr: Optional[int], x_rows: int,
+                                 source_ptr: Optional[int], slots: int, grad_ptr: int, grad_stride: int, offsets_ptr: int,
+                                 out_ptr: int, out_dtype: int, w_k_first: bool, accumulate: bool, rows: int, experts: int,
+                                 k: int, n: int, dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_weight_gradient(x_ptr, x_stride, x_scales_ptr, x_rows, source_ptr, slots, grad_ptr,
+                                                    grad_stride, offsets_ptr, out_ptr, out_dtype, w_k_first, accumulate,
+                                                    rows, experts, k, n, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_weight_gradient")
+
+
+def tperm_checkpoint_store(x_ptr: int, x_stride: int, codes_ptr: int, scales_ptr: int, rows: int, width: int, dtype: int,
+                           stream: int = 0) -> None:
+    st = (_fast or _calls()).checkpoint_store(x_ptr, x_stride, codes_ptr, scales_ptr, rows, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_checkpoint_store")
+
+
+def tperm_checkpoint_load(codes_ptr: int, scales_ptr: int, out_ptr: int, out_stride: int, rows: int, width: int, dtype: int,
+                          stream: int = 0) -> None:
+    st = (_fast or _calls()).checkpoint_load(codes_ptr, scales_ptr, out_ptr, out_stride, rows, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_checkpoint_load")
+
+
+def tperm_gated_forward(gates_ptr: int, gates_stride: int, out_ptr: int, out_stride: int, codes_ptr: Optional[int],
+                        scales_ptr: Optional[int], rows: int, width: int, dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).gated_forward(gates_ptr, gates_stride, out_ptr, out_stride, codes_ptr, scales_ptr, rows, width,
+                                           dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_gated_forward")
+
+
+def tperm_gated_backward(grad_ptr: int, grad_stride: int, codes_ptr: int, scales_ptr: int, grad_gates_ptr: int,
+                         grad_gates_stride: int, out_ptr: Optional[int], out_stride: int, rows: int, width: int, dtype: int,
+                         stream: int = 0) -> None:
+    st = (_fast or _calls()).gated_backward(grad_ptr, grad_stride, codes_ptr, scales_ptr, grad_gates_ptr, grad_gates_stride,
+                                            out_ptr, out_stride, rows, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_gated_backward")
 
 
 def tperm_plan_destroy(plan: Plan) -> None:

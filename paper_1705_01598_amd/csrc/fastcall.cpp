@@ -12,7 +12,11 @@
 #include <Python.h>
 #include <stdint.h>
 
-#include "../../include/tperm.h"
+#include <tuple>
+#include <type_traits>
+#include <utility>
+
+#include "../../include/tperm_experts.h"
 
 namespace {
 
@@ -97,6 +101,58 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
+// The calls of tperm_experts.h: pointers, 64-bit sizes and ints, converted by the type of the parameter.
+template <typename A> bool to_argument(PyObject* o, A* a) {
+    if constexpr (std::is_pointer_v<A>) {
+        void* p;
+        if (!to_pointer(o, &p)) return false;
+        *a = (A)p;
+        return true;
+    } else {
+        int64_t v;
+        if (!to_int64(o, &v)) return false;
+        if (sizeof(A) < sizeof(v) && v != (int64_t)(int)v) {
+            PyErr_SetString(PyExc_OverflowError, "flags and types are ints");
+            return false;
+        }
+        *a = (A)v;
+        return true;
+    }
+}
+
+template <typename... A, size_t... I>
+PyObject* call_with(tperm_status_t (*f)(A...), PyObject* const* args, std::index_sequence<I...>) {
+    std::tuple<A...> a;
+    if (!(to_argument(args[I], &std::get<I>(a)) && ...)) return nullptr;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = f(std::get<I>(a)...);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+template <typename... A> PyObject* call(const char* name, tperm_status_t (*f)(A...), PyObject* const* args, Py_ssize_t n) {
+    if (!count_is(name, n, (Py_ssize_t)sizeof...(A))) return nullptr;
+    return call_with(f, args, std::index_sequence_for<A...>());
+}
+
+#define TPERM_EXPERT_CALLS(X)                                                                                     \
+    X(expert_sort) X(expert_gather) X(expert_combine) X(expert_combine_backward) X(expert_product)                \
+    X(expert_weight_gradient) X(checkpoint_store) X(checkpoint_load) X(gated_forward) X(gated_backward)
+#define TPERM_CALL(name)                                                                                          \
+    decltype(&tperm_##name) g_##name;                                                                             \
+    PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t n) { return call(#name, g_##name, args, n); }
+TPERM_EXPERT_CALLS(TPERM_CALL)
+
+// Addresses of the calls above, in their order.
+PyObject* bind_experts(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    void* p[10];
+    if (!count_is("bind_experts", n, 10) || !pointers(args, 10, p)) return nullptr;
+    int i = 0;
+#define TPERM_BIND(name) g_##name = (decltype(g_##name))p[i++];
+    TPERM_EXPERT_CALLS(TPERM_BIND)
+    Py_RETURN_NONE;
+}
+
 // The entries of an iterable as integers; up to TPERM_MAX_RANK of them (the library refuses longer ones
 // by their number alone).  Returns their number, -1 with an exception set.  A conversion may run Python
 // code, and so may change the iterable: a tuple stays as it is, anything else goes through its
@@ -172,6 +228,9 @@ PyMethodDef methods[] = {
     {"verified", (PyCFunction)(void (*)(void))verified, METH_FASTCALL, nullptr},
     {"product", (PyCFunction)(void (*)(void))product, METH_FASTCALL, nullptr},
     {"transpose", (PyCFunction)(void (*)(void))transpose, METH_FASTCALL, nullptr},
+    {"bind_experts", (PyCFunction)(void (*)(void))bind_experts, METH_FASTCALL, nullptr},
+#define TPERM_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr},
+    TPERM_EXPERT_CALLS(TPERM_METHOD)
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
