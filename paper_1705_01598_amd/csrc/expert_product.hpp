@@ -163,20 +163,40 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Stage {
     }
 };
 
-// A workgroup's tile: FAST x SLOW results, four wavefronts, WF of them along the fast side.
-template <int FAST_, int SLOW_, int WF_> struct TileShape {
-    static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = 256;
-    static constexpr int kWavesFast = WF_, kWavesSlow = 4 / WF_;
+// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side.
+template <int FAST_, int SLOW_, int WAVES, int WF_> struct TileShape {
+    static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = WAVES * 64;
+    static constexpr int kWavesFast = WF_, kWavesSlow = WAVES / WF_;
     static constexpr int FI = FAST_ / kWavesFast / 16, SI = SLOW_ / kWavesSlow / 16;   // 16 x 16 blocks of a wavefront
 };
 
-// Sum over depth0 .. depth_end into acc: lane l holds fast indices 4 (l / 16) .. + 3 and slow index l % 16 of a block.
+// Fragments of one step of a stage, and their products: lane l of a 16 x 16 block of the result holds fast indices
+// 4 (l / 16) .. + 3 and slow index l % 16.
+constexpr uint32_t kSteps = 2;      // steps of a stage, whatever the type
+template <typename T, int FL, int SL, typename S> struct Step {
+    static_assert(kStageBytes / sizeof(T) == kSteps * Matrix<T>::kDepth, "two steps");
+    Frag<T> f[S::FI], s[S::SI];
+    __device__ __forceinline__ void read(const char* image, uint32_t kk) {
+        const uint32_t wave = threadIdx.x >> 6;
+        const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
+#pragma unroll
+        for (int i = 0; i < S::SI; ++i) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk);
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i) f[i] = fragment<T, FL, S::kFast>(image, wf + i * 16, kk);
+    }
+    __device__ __forceinline__ void multiply(f32x4 (&acc)[S::SI][S::FI]) const {
+#pragma unroll
+        for (int i = 0; i < S::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < S::SI; ++j) acc[j][i] = Matrix<T>::mul(f[i], s[j], acc[j][i]);
+    }
+};
+
+// Sum over depth0 .. depth_end into acc, by way of registers.
 template <typename T, int FL, int SL, typename S>
 __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0, uint32_t slow_end,
                                          uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
     constexpr uint32_t kDepth = kStageBytes / sizeof(T);
-    const uint32_t wave = threadIdx.x >> 6;
-    const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
     char* const ft = lds;
     char* const st = lds + S::kFast * kStageBytes;
     Stage<T, FL, S::kFast, S::kThreads> fs;
@@ -195,18 +215,160 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
             ss.fetch(slow, slow0, slow_end, d + kDepth, depth_end);
         }
 #pragma unroll
-        for (uint32_t kk = 0; kk < kDepth / Matrix<T>::kDepth; ++kk) {
-            Frag<T> f[S::FI], s[S::SI];
-#pragma unroll
-            for (int i = 0; i < S::FI; ++i) f[i] = fragment<T, FL, S::kFast>(ft, wf + i * 16, kk);
-#pragma unroll
-            for (int i = 0; i < S::SI; ++i) s[i] = fragment<T, SL, S::kSlow>(st, ws + i * 16, kk);
-#pragma unroll
-            for (int j = 0; j < S::SI; ++j)
-#pragma unroll
-                for (int i = 0; i < S::FI; ++i) acc[j][i] = Matrix<T>::mul(f[i], s[j], acc[j][i]);
+        for (uint32_t kk = 0; kk < kSteps; ++kk) {
+            Step<T, FL, SL, S> step;
+            step.read(lds, kk);
+            step.multiply(acc);
         }
     }
+}
+
+// --- from memory straight to LDS: rows of whole 16-byte chunks that start on 16 bytes ---
+
+constexpr uint32_t kBeyond = 0xFFFFFF00u;   // lane offset behind every buffer: the access writes zeros to LDS
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)kBeyond, 0x00020000); }
+
+// The operand of one side.  A lane's 16 bytes arrive at a place in LDS that its number fixes, so the swizzle is
+// applied to where it reads.  MAPPED: depth rows (kFreeFast) are found through source, one stage ahead.
+template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Direct {
+    static constexpr int V = 16 / sizeof(T);
+    static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
+    static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
+    static constexpr uint32_t kAcross = LAYOUT == kDepthFast ? 8 : FREE * sizeof(T) / 16;   // chunks of an LDS row
+    static constexpr uint32_t kRowsPerFetch = THREADS / kAcross;
+    static_assert(kFetches * THREADS * 16 == FREE * kStageBytes && kRowsPerFetch * kAcross == THREADS, "whole passes");
+    const char* base;
+    uint32_t row_bytes;
+    uint32_t off[kFetches];             // from base (kDepthFast: + depth; kFreeFast: + stage, MAPPED: of the column alone)
+    uint32_t row[MAPPED ? kFetches : 1];
+    const int32_t* source;
+    uint32_t slots, rows;
+
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
+    static __device__ __forceinline__ uint32_t chunk(int p) { return swizzle<T, LAYOUT>(lds_row(p), threadIdx.x % kAcross, kAcross); }
+
+    // Depth-fast: rows free0 .. free_end of m, whose row r is m.find(r).
+    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
+        row_bytes = (uint32_t)(m.stride * sizeof(T));
+        source = m.source, slots = m.slots, rows = m.rows;
+        if constexpr (LAYOUT == kDepthFast) {
+            base = (const char*)m.p + (m.source != nullptr ? 0 : (int64_t)free0 * row_bytes);
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                uint32_t r = free0 + lds_row(p), at;
+                off[p] = kBeyond;
+                if (r < free_end && m.find(r, &at)) off[p] = (m.source != nullptr ? at : at - free0) * row_bytes + chunk(p) * 16;
+            }
+        } else {
+            base = (const char*)m.p;
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                const uint32_t f = free0 + chunk(p) * V;
+                off[p] = f < free_end ? f * (uint32_t)sizeof(T) + (MAPPED ? 0u : lds_row(p) * row_bytes) : kBeyond;
+            }
+        }
+    }
+    // MAPPED: memory rows of the stage at `depth0`.
+    __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
+        if constexpr (MAPPED) {
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                const uint32_t d = depth0 + lds_row(p);
+                row[p] = d < depth_end ? (uint32_t)source[d] : 0xFFFFFFFFu;
+            }
+        }
+    }
+    __device__ __forceinline__ void issue(char* tile, uint32_t depth0, uint32_t depth_end) {
+        const uint32_t left = depth0 < depth_end ? depth_end - depth0 : 0;      // beyond the end: zeros
+        char* const to = tile + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x & ~63u)) * 16;
+        const char* from = base;
+        uint32_t scalar = 0;
+        if constexpr (LAYOUT == kDepthFast) scalar = depth0 * (uint32_t)sizeof(T);
+        else if constexpr (!MAPPED) from += (uint64_t)depth0 * row_bytes;
+        const __amdgpu_buffer_rsrc_t r = buffer_at(from);
+#pragma unroll
+        for (int p = 0; p < kFetches; ++p) {
+            uint32_t o = off[p];
+            if constexpr (LAYOUT == kDepthFast) {
+                if (left < kDepth) o = chunk(p) * V < left ? o : kBeyond;
+            } else if constexpr (MAPPED) {
+                const uint32_t at = row[p] / slots;
+                o = row[p] < 1u << 31 && at < rows && o != kBeyond ? at * row_bytes + o : kBeyond;
+            } else {
+                if (left < kDepth) o = lds_row(p) < left ? o : kBeyond;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (TPERM_LDS void*)(TPERM_LDS char*)(to + p * THREADS * 16), 16, (int)o, (int)scalar, 0, 0);
+        }
+    }
+};
+
+// Order for the compiler's scheduler, which would move the reads of the next step behind the products of this one to
+// save registers: READS LDS reads (and LOADS loads to LDS) spread over PRODUCTS matrix instructions.
+template <int READS, int PRODUCTS, int LOADS = 0> __device__ __forceinline__ void interleave() {
+    constexpr int kSlots = READS + LOADS;
+    constexpr int kEach = PRODUCTS / kSlots > 0 ? PRODUCTS / kSlots : 1;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Sum over depth0 .. depth_end into acc with two LDS images.  While the matrix cores work on one step, the fragments of
+// the next one are read; the only barrier of a stage stands between its two steps: all wavefronts have read the
+// stage's last fragments then, so its image can receive the stage after the next.
+template <typename T, int FL, int SL, bool FM, bool SM, typename S>
+__device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
+                                                uint32_t slow_end, uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
+    constexpr uint32_t kDepth = kStageBytes / sizeof(T);
+    constexpr uint32_t kImage = (S::kFast + S::kSlow) * kStageBytes;
+    Direct<T, FL, S::kFast, S::kThreads, FM> fs;
+    Direct<T, SL, S::kSlow, S::kThreads, SM> ss;
+    constexpr bool kOrdered = sizeof(T) == 2;
+    constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
+    constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;
+    if (depth0 >= depth_end) return;
+    fs.start(fast, fast0, fast_end);
+    ss.start(slow, slow0, slow_end);
+    const auto issue = [&](uint32_t image, uint32_t d) {
+        fs.issue(lds + image, d, depth_end);
+        ss.issue(lds + image + S::kFast * kStageBytes, d, depth_end);
+    };
+    const auto look_up = [&](uint32_t d) {
+        fs.look_up(d, depth_end);
+        ss.look_up(d, depth_end);
+    };
+    look_up(depth0);
+    issue(0, depth0);
+    look_up(depth0 + kDepth);
+    __syncthreads();
+    issue(kImage, depth0 + kDepth);
+    look_up(depth0 + 2 * kDepth);
+    uint32_t image = 0;
+    Step<T, FL, SL, S> even, odd;
+    even.read(lds, 0);
+    for (uint32_t d = depth0; d + kDepth < depth_end; d += kDepth) {
+        odd.read(lds + image, 1);
+        even.multiply(acc);
+        if constexpr (kOrdered) interleave<kReads, kProducts>();
+        __syncthreads();
+        issue(image, d + 2 * kDepth);
+        look_up(d + 3 * kDepth);
+        image ^= kImage;
+        even.read(lds + image, 0);
+        odd.multiply(acc);
+        if constexpr (kOrdered) interleave<kReads, kProducts, kLoads>();
+    }
+    odd.read(lds + image, 1);
+    even.multiply(acc);
+    odd.multiply(acc);
 }
 
 // Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been
@@ -243,9 +405,62 @@ __device__ __forceinline__ void rows_of(const int32_t* offsets, uint32_t experts
     *from = o < *end ? o : *end;
 }
 
-// The index-th tile of `height` rows over all bins; false: there are fewer.  Every wavefront looks for itself:
-// a lane takes neighbouring bins, a scan over the lanes and a ballot find the lane, the rest is uniform.
-__device__ __forceinline__ bool find_rows(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t height, uint32_t index, uint32_t* bin, uint32_t* from, uint32_t* end) {
+// The same by way of LDS (LDS_BYTES, free by now), in whole rows of the tile: a wavefront's own results are pieces of 8 or
+// 16 bytes of 16 rows.  Chunks of 16 bytes change places by their row, so that those pieces meet no bank
+// conflicts.
+template <typename O, typename S, int LDS_BYTES>
+__device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
+                                                const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
+    constexpr uint32_t kPitch = S::kFast * sizeof(O), kChunks = kPitch / 16, V = 16 / sizeof(O);
+    constexpr int kPasses = (S::kSlow * (int)kPitch + LDS_BYTES - 1) / LDS_BYTES, kRows = S::kSlow / kPasses;
+    static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow && kChunks >= 16, "whole blocks");
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+    const uint32_t f0 = wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
+    const uint32_t s0 = wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < S::SI; ++j) {
+            const uint32_t row = s0 + j * 16 - pass * kRows;
+            if (row < (uint32_t)kRows) {
+#pragma unroll
+                for (int i = 0; i < S::FI; ++i) {
+                    const uint32_t at = (f0 + i * 16) * (uint32_t)sizeof(O);
+                    *(Vec<O, 4>*)(lds + row * kPitch + ((at / 16) ^ (row & 15u)) * 16 + at % 16) = narrow<O, 4>(acc[j][i]);
+                }
+            }
+        }
+        __syncthreads();
+        for (uint32_t id = threadIdx.x; id < kRows * kChunks; id += S::kThreads) {
+            const uint32_t row = id / kChunks, c = id % kChunks, s = slow0 + pass * kRows + row, f = fast0 + c * V;
+            if (s >= slow_end) break;
+            if (f >= fast_end) continue;
+            Vec<O, V> v = *(const Vec<O, V>*)(lds + row * kPitch + (c ^ (row & 15u)) * 16);
+            O* const p = out + (int64_t)s * stride + f;
+            if constexpr (sizeof(O) == 4)
+                if (accumulate) v += load_some<O, V, false>(p, (int)(fast_end - f));
+            store_some<O, V, false>(p, v, (int)(fast_end - f));
+        }
+    }
+}
+
+// Which tile a workgroup takes.  Workgroups go round the 8 XCDs, so numbers that are 8 apart share an L2: each
+// XCD takes one run of tiles, and inside an expert runs of kGroup row tiles by all columns.
+constexpr uint32_t kXcds = 8, kGroup = 8;
+
+__device__ __forceinline__ void grouped(uint32_t at, uint32_t down, uint32_t across, uint32_t* row, uint32_t* col) {
+    const uint32_t g = at / (kGroup * across), in = at - g * kGroup * across;
+    const uint32_t high = down - g * kGroup < kGroup ? down - g * kGroup : kGroup;
+    *col = in / high;
+    *row = g * kGroup + (in - *col * high);
+}
+
+// Tiles of `height` rows by `across` columns over all bins; false: this workgroup has none.  Every wavefront looks
+// for itself: a lane takes neighbouring bins, a scan over the lanes and a ballot find the lane, the rest is
+// uniform.
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t height, uint32_t across,
+                                          uint32_t* bin, uint32_t* from, uint32_t* end, uint32_t* col) {
     const uint32_t lane = threadIdx.x & 63u, bins = experts + 1, per = (bins + 63) / 64;
     uint32_t n = 0, o, p;
     for (uint32_t i = 0; i < per; ++i)
@@ -258,56 +473,70 @@ __device__ __forceinline__ bool find_rows(const int32_t* offsets, uint32_t exper
         const uint32_t before = (uint32_t)__shfl_up((int)sum, d);
         if (lane >= d) sum += before;
     }
-    const uint64_t at = __ballot(sum > index);
+    const uint32_t tiles = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63) * across, run = (tiles + kXcds - 1) / kXcds;
+    const uint32_t block = (uint32_t)long_block(), index = block % kXcds * run + block / kXcds;
+    if (block / kXcds >= run || index >= tiles) return false;
+    const uint64_t at = __ballot(sum * across > index);
     if (at == 0) return false;
     const int l = __builtin_ctzll(at);
-    uint32_t left = index - (uint32_t)__builtin_amdgcn_readlane((int)(sum - n), l);
+    uint32_t left = index - (uint32_t)__builtin_amdgcn_readlane((int)(sum - n), l) * across;
     for (uint32_t b = (uint32_t)l * per; b < bins; ++b) {
         rows_of(offsets, experts, rows, b, &o, &p);
-        const uint32_t tiles = (p - o + height - 1) / height;
-        if (left < tiles) {
+        const uint32_t down = (p - o + height - 1) / height;
+        if (left < down * across) {
+            uint32_t row;
+            grouped(left, down, across, &row, col);
             *bin = b;
-            *from = o + left * height;
+            *from = o + row * height;
             *end = p - *from < height ? p : *from + height;
             return true;
         }
-        left -= tiles;
+        left -= down * across;
     }
     return false;
 }
 
 // --- kernels ---
 
-template <typename T, int WL, typename S>
+// DIRECT: operands go straight to LDS (two images); else by way of registers.
+template <typename T, int WL, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const ExpertProductArgs a) {
-    __shared__ __attribute__((aligned(16))) char lds[(S::kFast + S::kSlow) * kStageBytes];
+    extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t across = (a.n + S::kFast - 1) / S::kFast;
-    uint32_t bin, row0, row_end;
-    if (!find_rows(a.offsets, a.experts, a.rows, S::kSlow, (uint32_t)long_block() / across, &bin, &row0, &row_end)) return;
-    const uint32_t col0 = (uint32_t)long_block() % across * S::kFast, col_end = a.n;
+    uint32_t bin, row0, row_end, col;
+    if (!find_tile(a.offsets, a.experts, a.rows, S::kSlow, across, &bin, &row0, &row_end, &col)) return;
+    const uint32_t col0 = col * S::kFast, col_end = a.n;
     f32x4 acc[S::SI][S::FI] = {};
     if (bin < a.experts) {
         const T* const w = (const T*)a.w + (int64_t)bin * a.k * a.n;
         const Operand fast = WL == kDepthFast ? Operand(w, a.n, a.k) : Operand(w, a.k, a.n);
-        sum_tile<T, WL, kDepthFast, S>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
+        if constexpr (DIRECT) sum_tile_direct<T, WL, kDepthFast, false, false, S>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
+        else sum_tile<T, WL, kDepthFast, S>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
     }
-    store_tile<T, S>((T*)a.out, a.out_stride, col0, col_end, row0, row_end, false, acc);
+    if constexpr (DIRECT) store_tile_rows<T, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
+    else store_tile<T, S>((T*)a.out, a.out_stride, col0, col_end, row0, row_end, false, acc);
 }
 
-template <typename T, int FL, int SL, typename S>
+// Experts one after the other; every XCD takes a run of an expert's tiles, whichever experts are large.
+template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const WeightGradientArgs a) {
-    __shared__ __attribute__((aligned(16))) char lds[(S::kFast + S::kSlow) * kStageBytes];
-    const uint32_t tf = (a.fast.width + S::kFast - 1) / S::kFast, ts = (a.slow.width + S::kSlow - 1) / S::kSlow;
-    const uint32_t at_tile = (uint32_t)long_block(), expert = at_tile / (tf * ts), tile = at_tile % (tf * ts);
-    if (expert >= a.experts) return;
-    const uint32_t f0 = tile % tf * S::kFast, s0 = tile / tf * S::kSlow;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t tf = (a.fast.width + S::kFast - 1) / S::kFast, ts = (a.slow.width + S::kSlow - 1) / S::kSlow, run = (tf * ts + kXcds - 1) / kXcds;
+    const uint64_t block = long_block();
+    const uint32_t i = (uint32_t)(block / kXcds), expert = i / run, tile = ((uint32_t)(block % kXcds) + expert) % kXcds * run + i % run;
+    if (expert >= a.experts || tile >= tf * ts) return;
+    uint32_t fi, si;
+    grouped(tile, ts, tf, &si, &fi);
+    const uint32_t f0 = fi * S::kFast, s0 = si * S::kSlow;
     uint32_t from, end;
     rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
     f32x4 acc[S::SI][S::FI] = {};
-    sum_tile<T, FL, SL, S>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
+    if constexpr (DIRECT) sum_tile_direct<T, FL, SL, FM, SM, S>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
+    else sum_tile<T, FL, SL, S>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
     const int64_t at = (int64_t)expert * a.fast.width * a.slow.width;
     const bool accumulate = a.accumulate != 0;
-    if (a.out_type == TPERM_TYPE_F32) store_tile<float, S>((float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
+    if (DIRECT && a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
+    else if (a.out_type == TPERM_TYPE_F32) store_tile<float, S>((float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
     else if (a.out_type == TPERM_TYPE_F16) store_tile<_Float16, S>((_Float16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
     else store_tile<__bf16, S>((__bf16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
 }

@@ -4,26 +4,65 @@
 
 namespace tperm {
 
-using WideTile = TileShape<128, 128, 2>;
+using SmallTile = TileShape<128, 128, 4, 2>;
+using WideTile = TileShape<256, 256, 8, 2>;
 
-template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
-    using S = WideTile;
-    const uint64_t tiles = ((uint64_t)a.rows / S::kSlow + a.experts + 1) * ((a.n + S::kFast - 1) / S::kFast);
-    if (w_k_first) hipLaunchKernelGGL((expert_product_kernel<T, kDepthFast, S>), long_grid(tiles), dim3(S::kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((expert_product_kernel<T, kFreeFast, S>), long_grid(tiles), dim3(S::kThreads), 0, stream, a);
+template <typename S> constexpr size_t lds_bytes(bool direct) { return (size_t)(S::kFast + S::kSlow) * kStageBytes * (direct ? 2 : 1); }
+
+// Workgroups with more than 64 KiB of LDS have to ask for it, once a kernel and device.
+template <typename S, typename K, typename A> hipError_t go(K kernel, bool direct, uint64_t blocks, const A& a, hipStream_t stream) {
+    const size_t lds = lds_bytes<S>(direct);
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, long_grid(blocks), dim3(S::kThreads), lds, stream, a);
     return hipGetLastError();
 }
 
+// Rows of whole chunks that start on 16 bytes; offsets inside a tile's rows fit 32 bits.
+inline bool on_chunks(size_t elem, const void* p, int64_t stride, uint32_t width) {
+    return width * elem % 16 == 0 && ((uintptr_t)p | (uintptr_t)stride * elem) % 16 == 0 && stride < (int64_t)1 << 22;
+}
+
+template <typename T, typename S, bool DIRECT> hipError_t product_tiles(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
+    const uint64_t tiles = ((uint64_t)a.rows / S::kSlow + a.experts + 1) * ((a.n + S::kFast - 1) / S::kFast);
+    const uint64_t blocks = (tiles + kXcds - 1) / kXcds * kXcds;
+    return w_k_first ? go<S>(expert_product_kernel<T, kDepthFast, S, DIRECT>, DIRECT, blocks, a, stream)
+                     : go<S>(expert_product_kernel<T, kFreeFast, S, DIRECT>, DIRECT, blocks, a, stream);
+}
+
+template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
+    const bool direct = on_chunks(sizeof(T), a.x.p, a.x.stride, a.k) && on_chunks(sizeof(T), a.w, w_k_first ? a.k : a.n, w_k_first ? a.k : a.n);
+    if (!direct) return product_tiles<T, SmallTile, false>(a, w_k_first, stream);
+    if constexpr (sizeof(T) == 2) {
+        if (a.rows >= 128 * a.experts) return product_tiles<T, WideTile, true>(a, w_k_first, stream);
+    }
+    return product_tiles<T, SmallTile, true>(a, w_k_first, stream);
+}
+
+template <typename T, typename S, bool DIRECT> hipError_t gradient_tiles(const WeightGradientArgs& a, hipStream_t stream) {
+    const uint64_t tiles = (uint64_t)((a.fast.width + S::kFast - 1) / S::kFast) * ((a.slow.width + S::kSlow - 1) / S::kSlow);
+    const uint64_t blocks = (tiles + kXcds - 1) / kXcds * kXcds * a.experts;
+    if constexpr (DIRECT) {
+        if (a.fast.source != nullptr) return go<S>(weight_gradient_kernel<T, kFreeFast, kFreeFast, true, false, S, true>, true, blocks, a, stream);
+        if (a.slow.source != nullptr) return go<S>(weight_gradient_kernel<T, kFreeFast, kFreeFast, false, true, S, true>, true, blocks, a, stream);
+        return go<S>(weight_gradient_kernel<T, kFreeFast, kFreeFast, false, false, S, true>, true, blocks, a, stream);
+    } else {
+        if (a.fast.scales != nullptr) return go<S>(weight_gradient_kernel<T, kCodes, kFreeFast, false, false, S, false>, false, blocks, a, stream);
+        if (a.slow.scales != nullptr) return go<S>(weight_gradient_kernel<T, kFreeFast, kCodes, false, false, S, false>, false, blocks, a, stream);
+        return go<S>(weight_gradient_kernel<T, kFreeFast, kFreeFast, false, false, S, false>, false, blocks, a, stream);
+    }
+}
+
 template <typename T> hipError_t gradient_of(const WeightGradientArgs& a, hipStream_t stream) {
-    using S = WideTile;
-    const uint64_t tiles = (uint64_t)a.experts * ((a.fast.width + S::kFast - 1) / S::kFast) * ((a.slow.width + S::kSlow - 1) / S::kSlow);
-    const auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, long_grid(tiles), dim3(S::kThreads), 0, stream, a);
-        return hipGetLastError();
-    };
-    if (a.fast.scales != nullptr) return go(weight_gradient_kernel<T, kCodes, kFreeFast, S>);
-    if (a.slow.scales != nullptr) return go(weight_gradient_kernel<T, kFreeFast, kCodes, S>);
-    return go(weight_gradient_kernel<T, kFreeFast, kFreeFast, S>);
+    const bool direct = a.fast.scales == nullptr && a.slow.scales == nullptr && on_chunks(sizeof(T), a.fast.p, a.fast.stride, a.fast.width) &&
+                        on_chunks(sizeof(T), a.slow.p, a.slow.stride, a.slow.width);
+    if (!direct) return gradient_tiles<T, SmallTile, false>(a, stream);
+    if constexpr (sizeof(T) == 2) {
+        if ((uint64_t)a.fast.width * a.slow.width * a.experts >= 256ull * 256 * 256) return gradient_tiles<T, WideTile, true>(a, stream);
+    }
+    return gradient_tiles<T, SmallTile, true>(a, stream);
 }
 
 }  // namespace tperm
