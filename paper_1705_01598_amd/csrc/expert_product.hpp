@@ -11,6 +11,8 @@
 #include "expert_vector.hpp"
 #include "experts.hpp"
 
+#include <type_traits>
+
 namespace tperm {
 
 enum Layout { kDepthFast = 0, kFreeFast = 1, kCodes = 2 };  // kCodes: as kFreeFast, 8-bit codes with scales
@@ -301,6 +303,91 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (TPERM_LDS void*)(TPERM_LDS char*)(to + p * THREADS * 16), 16, (int)o, (int)scalar, 0, 0);
         }
     }
+    __device__ __forceinline__ void put(char*) const {}     // it goes there by itself
+};
+
+// 8 codes as elements; `safe`: the scale cannot carry them beyond the type's range.
+template <typename T> __device__ __forceinline__ Vec<T, 8> elements_of(u32x2 codes, float scale, bool safe) {
+    if constexpr (sizeof(T) == 2) {
+        if (safe) {
+            Vec<T, 8> v;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    Vec<T, 2> e;
+                    if constexpr (__is_same(T, __bf16)) e = k ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[h], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[h], scale, false);
+                    else e = k ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[h], scale, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes[h], scale, false);
+                    v[4 * h + 2 * k] = e[0], v[4 * h + 2 * k + 1] = e[1];
+                }
+            return v;
+        }
+    }
+    return narrow<T, 8>(values_of<T>(codes, scale));
+}
+
+// The operand of one side kept in codes (rows of whole 16-byte chunks that start on 16 bytes): through registers, where
+// codes become elements.  A stage is fetched while the one before it is multiplied, its rows looked up one
+// stage before that.
+template <typename T, int FREE, int THREADS> struct Coded {
+    static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
+    static constexpr uint32_t kAcross = FREE / 16, kRowsPerFetch = THREADS / kAcross;
+    static constexpr int kFetches = kDepth / kRowsPerFetch;
+    static_assert(kFetches * kRowsPerFetch == kDepth && kRowsPerFetch * kAcross == THREADS, "whole passes");
+    const uint8_t *codes, *scales;
+    const int32_t* source;
+    uint32_t width, blocks, slots, rows, free;
+    bool there;
+    uint32_t row[kFetches];
+    u32x4 reg[kFetches];
+    uint32_t scale[kFetches];
+
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
+    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
+        free = free0 + threadIdx.x % kAcross * 16;
+        there = free < free_end;
+        codes = (const uint8_t*)m.p, scales = m.scales, source = m.source;
+        width = m.width, blocks = (m.width + 31) / 32, slots = m.slots, rows = m.rows;
+    }
+    __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
+        if (source != nullptr)
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) row[p] = depth0 + lds_row(p) < depth_end ? (uint32_t)source[depth0 + lds_row(p)] : 0xFFFFFFFFu;
+    }
+    __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
+        // rows that are not looked up are reached from the stage's first one: no limit to the tensor
+        const uint64_t from = source != nullptr ? 0 : depth0;
+        const __amdgpu_buffer_rsrc_t c = buffer_at(codes + from * width), s = buffer_at(scales + from * blocks);
+#pragma unroll
+        for (int p = 0; p < kFetches; ++p) {
+            const uint32_t at = source != nullptr ? row[p] / slots : lds_row(p);
+            const bool use = there && (source != nullptr ? row[p] < 1u << 31 && at < rows : depth0 + at < depth_end);
+            reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? at * width + free : kBeyond), 0, 0);
+            scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? at * blocks + free / 32 : kBeyond), 0, 0);
+        }
+    }
+    __device__ __forceinline__ void put(char* tile) const {
+        constexpr uint32_t kChunks = FREE * sizeof(T) / 16;
+        __builtin_amdgcn_sched_barrier(0);      // not before the products: it would wait for the codes there
+#pragma unroll
+        for (int p = 0; p < kFetches; ++p) {
+            const uint32_t d = lds_row(p), c = threadIdx.x % kAcross;
+            char* const at = tile + d * (FREE * sizeof(T));
+            const float by = power_of(scale[p]);
+            const bool safe = __ballot(by > Range<T>::kSafe) == 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const Vec<T, 8> v = elements_of<T>(u32x2{reg[p][2 * h], reg[p][2 * h + 1]}, by, safe);
+                if constexpr (sizeof(T) == 2) {
+                    *(Vec<T, 8>*)(at + swizzle<T, kFreeFast>(d, 2 * c + h, kChunks) * 16) = v;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        *(f32x4*)(at + swizzle<T, kFreeFast>(d, 4 * c + 2 * h + k, kChunks) * 16) = f32x4{(float)v[4 * k], (float)v[4 * k + 1], (float)v[4 * k + 2], (float)v[4 * k + 3]};
+                }
+            }
+        }
+    }
 };
 
 // Order for the compiler's scheduler, which would move the reads of the next step behind the products of this one to
@@ -329,8 +416,8 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
                                                 uint32_t slow_end, uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
     constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     constexpr uint32_t kImage = (S::kFast + S::kSlow) * kStageBytes;
-    Direct<T, FL, S::kFast, S::kThreads, FM> fs;
-    Direct<T, SL, S::kSlow, S::kThreads, SM> ss;
+    std::conditional_t<FL == kCodes, Coded<T, S::kFast, S::kThreads>, Direct<T, FL, S::kFast, S::kThreads, FM>> fs;
+    std::conditional_t<SL == kCodes, Coded<T, S::kSlow, S::kThreads>, Direct<T, SL, S::kSlow, S::kThreads, SM>> ss;
     constexpr bool kOrdered = sizeof(T) == 2;
     constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
     constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;
@@ -345,9 +432,32 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
         fs.look_up(d, depth_end);
         ss.look_up(d, depth_end);
     };
+    const auto put = [&](uint32_t image) {
+        fs.put(lds + image);
+        ss.put(lds + image + S::kFast * kStageBytes);
+    };
     look_up(depth0);
     issue(0, depth0);
     look_up(depth0 + kDepth);
+    put(0);
+    if constexpr (FL == kCodes || SL == kCodes) {
+        // two sets of fragments and codes do not fit the registers: the other wavefront of the SIMD multiplies
+        // while this one reads
+        for (uint32_t d = depth0, image = 0; d < depth_end; d += kDepth, image ^= kImage) {
+            __syncthreads();
+            issue(image ^ kImage, d + kDepth);
+            look_up(d + 2 * kDepth);
+#pragma unroll
+            for (uint32_t kk = 0; kk < kSteps; ++kk) {
+                Step<T, FL, SL, S> step;
+                step.read(lds + image, kk);
+                step.multiply(acc);
+            }
+            put(image ^ kImage);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        return;
+    }
     __syncthreads();
     issue(kImage, depth0 + kDepth);
     look_up(depth0 + 2 * kDepth);
@@ -369,6 +479,7 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
     odd.read(lds + image, 1);
     even.multiply(acc);
     odd.multiply(acc);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // nothing travels to LDS when it is used again
 }
 
 // Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been
@@ -446,10 +557,9 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
 }
 
 // Which tile a workgroup takes.  Workgroups go round the 8 XCDs, so numbers that are 8 apart share an L2: each
-// XCD takes one run of tiles, and inside an expert runs of kGroup row tiles by all columns.
-constexpr uint32_t kXcds = 8, kGroup = 8;
-
-__device__ __forceinline__ void grouped(uint32_t at, uint32_t down, uint32_t across, uint32_t* row, uint32_t* col) {
+// XCD takes one run of tiles, and inside an expert runs of kGroup rows of tiles by all columns.
+constexpr uint32_t kXcds = 8;
+template <uint32_t kGroup> __device__ __forceinline__ void grouped(uint32_t at, uint32_t down, uint32_t across, uint32_t* row, uint32_t* col) {
     const uint32_t g = at / (kGroup * across), in = at - g * kGroup * across;
     const uint32_t high = down - g * kGroup < kGroup ? down - g * kGroup : kGroup;
     *col = in / high;
@@ -485,7 +595,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t exper
         const uint32_t down = (p - o + height - 1) / height;
         if (left < down * across) {
             uint32_t row;
-            grouped(left, down, across, &row, col);
+            grouped<8>(left, down, across, &row, col);
             *bin = b;
             *from = o + row * height;
             *end = p - *from < height ? p : *from + height;
@@ -526,7 +636,7 @@ __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const Weig
     const uint32_t i = (uint32_t)(block / kXcds), expert = i / run, tile = ((uint32_t)(block % kXcds) + expert) % kXcds * run + i % run;
     if (expert >= a.experts || tile >= tf * ts) return;
     uint32_t fi, si;
-    grouped(tile, ts, tf, &si, &fi);
+    grouped<4>(tile, ts, tf, &si, &fi);
     const uint32_t f0 = fi * S::kFast, s0 = si * S::kSlow;
     uint32_t from, end;
     rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
