@@ -92,13 +92,14 @@ struct Operand {
     const uint8_t* scales;
     const int32_t* source;
     int64_t stride;
-    uint32_t slots, rows, width;
+    FastDiv slots;
+    uint32_t rows, width;
     __device__ __forceinline__ explicit Operand(const ProductSide& s) : p(s.p), scales(s.scales), source(s.source), stride(s.stride), slots(s.slots), rows(s.rows), width(s.width) {}
-    __device__ __forceinline__ Operand(const void* at, uint32_t r, uint32_t w) : p(at), scales(nullptr), source(nullptr), stride(w), slots(1), rows(r), width(w) {}
+    __device__ __forceinline__ Operand(const void* at, uint32_t r, uint32_t w) : p(at), scales(nullptr), source(nullptr), stride(w), slots{}, rows(r), width(w) {}
     // Memory row behind row r of the order; false: there is none.
     __device__ __forceinline__ bool find(uint32_t r, uint32_t* row) const {
         const uint32_t s = source != nullptr ? (uint32_t)source[r] : r;
-        *row = source != nullptr ? s / slots : s;
+        *row = source != nullptr ? fdiv(s, slots) : s;      // right for s < 2^31
         return s < 1u << 31 && *row < rows;
     }
 };
@@ -231,6 +232,23 @@ constexpr uint32_t kBeyond = 0xFFFFFF00u;   // lane offset behind every buffer: 
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)kBeyond, 0x00020000); }
 
+// 16 bytes a lane from base + offset + scalar to 1 KiB of LDS from `to` on.  Written out: behind the builtin the
+// compiler lets the next transposing read, of another image, wait for all loads (2.1 us a stage instead of 1.4).  It
+// has no result for the compiler to see; arrive() waits for it.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t to, uint32_t offset, uint32_t scalar) {
+    const uint64_t p = (uint64_t)base;
+    const u32x4 buffer = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFFu, kBeyond, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(buffer), "s"(scalar));
+}
+
+// Waits until at most LOADS of this wavefront's loads are under way and its LDS accesses are done, then for the other
+// wavefronts to do so.
+template <int LOADS> __device__ __forceinline__ void arrive() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LOADS) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // The operand of one side.  A lane's 16 bytes arrive at a place in LDS that its number fixes, so the swizzle is
 // applied to where it reads.  MAPPED: depth rows (kFreeFast) are found through source, one stage ahead.
 template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Direct {
@@ -243,9 +261,13 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     const char* base;
     uint32_t row_bytes;
     uint32_t off[kFetches];             // from base (kDepthFast: + depth; kFreeFast: + stage, MAPPED: of the column alone)
-    uint32_t row[MAPPED ? kFetches : 1];
+    // MAPPED: what a wavefront's lanes add to it in each fetch: kRowsPerWave memory rows, the same for the
+    // lanes of one, kept in scalar registers
+    static constexpr int kRowsPerWave = 64 / kAcross;
+    uint32_t row[MAPPED ? kFetches : 1][MAPPED ? kRowsPerWave : 1];
     const int32_t* source;
-    uint32_t slots, rows;
+    FastDiv slots;
+    uint32_t rows;
 
     static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
     static __device__ __forceinline__ uint32_t chunk(int p) { return swizzle<T, LAYOUT>(lds_row(p), threadIdx.x % kAcross, kAcross); }
@@ -271,36 +293,47 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             }
         }
     }
-    // MAPPED: memory rows of the stage at `depth0`.
+    // MAPPED: entries of source for the stage at `depth0`, by scalar loads.
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
         if constexpr (MAPPED) {
+            typedef const __attribute__((address_space(4))) int32_t* Scalar;
+            const uint32_t first = depth0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kRowsPerWave;
 #pragma unroll
-            for (int p = 0; p < kFetches; ++p) {
-                const uint32_t d = depth0 + lds_row(p);
-                row[p] = d < depth_end ? (uint32_t)source[d] : 0xFFFFFFFFu;
-            }
+            for (int p = 0; p < kFetches; ++p)
+#pragma unroll
+                for (int i = 0; i < kRowsPerWave; ++i) {
+                    const uint32_t d = first + p * kRowsPerFetch + i;
+                    row[p][i] = (uint32_t)((Scalar)(uintptr_t)source)[d < depth_end ? d : depth_end - 1];
+                }
         }
     }
     __device__ __forceinline__ void issue(char* tile, uint32_t depth0, uint32_t depth_end) {
         const uint32_t left = depth0 < depth_end ? depth_end - depth0 : 0;      // beyond the end: zeros
-        char* const to = tile + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x & ~63u)) * 16;
+        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (threadIdx.x & ~63u) * 16));
         const char* from = base;
         uint32_t scalar = 0;
         if constexpr (LAYOUT == kDepthFast) scalar = depth0 * (uint32_t)sizeof(T);
         else if constexpr (!MAPPED) from += (uint64_t)depth0 * row_bytes;
-        const __amdgpu_buffer_rsrc_t r = buffer_at(from);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
             uint32_t o = off[p];
             if constexpr (LAYOUT == kDepthFast) {
                 if (left < kDepth) o = chunk(p) * V < left ? o : kBeyond;
             } else if constexpr (MAPPED) {
-                const uint32_t at = row[p] / slots;
-                o = row[p] < 1u << 31 && at < rows && o != kBeyond ? at * row_bytes + o : kBeyond;
+                const uint32_t in_wave = (threadIdx.x & 63u) / kAcross;
+                uint32_t start = 0;
+#pragma unroll
+                for (int i = 0; i < kRowsPerWave; ++i) {
+                    const uint32_t at = fdiv(row[p][i], slots);
+                    const uint32_t d = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kRowsPerWave + p * kRowsPerFetch + i;
+                    const uint32_t one = d < left && row[p][i] < 1u << 31 && at < rows ? at * row_bytes : kBeyond;
+                    start = in_wave == (uint32_t)i ? one : start;
+                }
+                o = __builtin_elementwise_add_sat(start, o);     // kBeyond and more stays behind the buffer
             } else {
                 if (left < kDepth) o = lds_row(p) < left ? o : kBeyond;
             }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (TPERM_LDS void*)(TPERM_LDS char*)(to + p * THREADS * 16), 16, (int)o, (int)scalar, 0, 0);
+            load_to_lds(from, to + p * THREADS * 16, o, scalar);
         }
     }
     __device__ __forceinline__ void put(char*) const {}     // it goes there by itself
@@ -336,7 +369,8 @@ template <typename T, int FREE, int THREADS> struct Coded {
     static_assert(kFetches * kRowsPerFetch == kDepth && kRowsPerFetch * kAcross == THREADS, "whole passes");
     const uint8_t *codes, *scales;
     const int32_t* source;
-    uint32_t width, blocks, slots, rows, free;
+    uint32_t width, blocks, rows, free;
+    FastDiv slots;
     bool there;
     uint32_t row[kFetches];
     u32x4 reg[kFetches];
@@ -360,7 +394,7 @@ template <typename T, int FREE, int THREADS> struct Coded {
         const __amdgpu_buffer_rsrc_t c = buffer_at(codes + from * width), s = buffer_at(scales + from * blocks);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
-            const uint32_t at = source != nullptr ? row[p] / slots : lds_row(p);
+            const uint32_t at = source != nullptr ? fdiv(row[p], slots) : lds_row(p);
             const bool use = there && (source != nullptr ? row[p] < 1u << 31 && at < rows : depth0 + at < depth_end);
             reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? at * width + free : kBeyond), 0, 0);
             scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? at * blocks + free / 32 : kBeyond), 0, 0);
@@ -391,15 +425,9 @@ template <typename T, int FREE, int THREADS> struct Coded {
 };
 
 // Order for the compiler's scheduler, which would move the reads of the next step behind the products of this one to
-// save registers: READS LDS reads (and LOADS loads to LDS) spread over PRODUCTS matrix instructions.
-template <int READS, int PRODUCTS, int LOADS = 0> __device__ __forceinline__ void interleave() {
-    constexpr int kSlots = READS + LOADS;
-    constexpr int kEach = PRODUCTS / kSlots > 0 ? PRODUCTS / kSlots : 1;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x8, kEach, 0);
-    }
+// save registers: READS LDS reads spread over PRODUCTS matrix instructions.
+template <int READS, int PRODUCTS> __device__ __forceinline__ void interleave() {
+    constexpr int kEach = PRODUCTS / READS > 0 ? PRODUCTS / READS : 1;
 #pragma unroll
     for (int i = 0; i < READS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -420,7 +448,6 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
     std::conditional_t<SL == kCodes, Coded<T, S::kSlow, S::kThreads>, Direct<T, SL, S::kSlow, S::kThreads, SM>> ss;
     constexpr bool kOrdered = sizeof(T) == 2;
     constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
-    constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;
     if (depth0 >= depth_end) return;
     fs.start(fast, fast0, fast_end);
     ss.start(slow, slow0, slow_end);
@@ -444,7 +471,7 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
         // two sets of fragments and codes do not fit the registers: the other wavefront of the SIMD multiplies
         // while this one reads
         for (uint32_t d = depth0, image = 0; d < depth_end; d += kDepth, image ^= kImage) {
-            __syncthreads();
+            arrive<0>();
             issue(image ^ kImage, d + kDepth);
             look_up(d + 2 * kDepth);
 #pragma unroll
@@ -455,10 +482,10 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
             }
             put(image ^ kImage);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        arrive<0>();
         return;
     }
-    __syncthreads();
+    arrive<0>();
     issue(kImage, depth0 + kDepth);
     look_up(depth0 + 2 * kDepth);
     uint32_t image = 0;
@@ -468,18 +495,18 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
         odd.read(lds + image, 1);
         even.multiply(acc);
         if constexpr (kOrdered) interleave<kReads, kProducts>();
-        __syncthreads();
+        arrive<0>();
         issue(image, d + 2 * kDepth);
         look_up(d + 3 * kDepth);
         image ^= kImage;
         even.read(lds + image, 0);
         odd.multiply(acc);
-        if constexpr (kOrdered) interleave<kReads, kProducts, kLoads>();
+        if constexpr (kOrdered) interleave<kReads, kProducts>();
     }
     odd.read(lds + image, 1);
     even.multiply(acc);
     odd.multiply(acc);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // nothing travels to LDS when it is used again
+    arrive<0>();            // nothing travels to LDS when it is used again
 }
 
 // Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been
@@ -627,14 +654,31 @@ __global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const Exper
     else store_tile<T, S>((T*)a.out, a.out_stride, col0, col_end, row0, row_end, false, acc);
 }
 
+// The i-th expert by number of rows, most first (equal ones in their order), for up to 64 experts: every lane counts how many
+// come before its own.  Tiles of large experts that start last would leave the chip idle around them.
+__device__ __forceinline__ uint32_t by_size(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t i) {
+    const uint32_t lane = threadIdx.x & 63u;
+    uint32_t from, end, size = 0, rank = 0;
+    if (lane < experts) {
+        rows_of(offsets, experts, rows, lane, &from, &end);
+        size = end - from;
+    }
+    for (uint32_t e = 0; e < experts; ++e) {
+        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)size, (int)e);
+        rank += other > size || (other == size && e < lane) ? 1u : 0u;
+    }
+    return (uint32_t)__builtin_ctzll(__ballot(lane < experts && rank == i));
+}
+
 // Experts one after the other; every XCD takes a run of an expert's tiles, whichever experts are large.
 template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const WeightGradientArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t tf = (a.fast.width + S::kFast - 1) / S::kFast, ts = (a.slow.width + S::kSlow - 1) / S::kSlow, run = (tf * ts + kXcds - 1) / kXcds;
     const uint64_t block = long_block();
-    const uint32_t i = (uint32_t)(block / kXcds), expert = i / run, tile = ((uint32_t)(block % kXcds) + expert) % kXcds * run + i % run;
-    if (expert >= a.experts || tile >= tf * ts) return;
+    const uint32_t i = (uint32_t)(block / kXcds), turn = i / run, tile = ((uint32_t)(block % kXcds) + turn) % kXcds * run + i % run;
+    if (turn >= a.experts || tile >= tf * ts) return;
+    const uint32_t expert = a.experts <= 64 ? by_size(a.offsets, a.experts, a.rows, turn) : turn;
     uint32_t fi, si;
     grouped<4>(tile, ts, tf, &si, &fi);
     const uint32_t f0 = fi * S::kFast, s0 = si * S::kSlow;

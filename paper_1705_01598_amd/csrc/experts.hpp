@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/tperm_experts.h"
+#include "tperm_desc.h"
 
 namespace tperm {
 
@@ -48,7 +49,8 @@ struct ProductSide {
     const uint8_t* scales;      // of codes
     const int32_t* source;      // row map, or NULL
     int64_t stride;             // elements between rows
-    uint32_t slots, rows;       // row(r) = source[r] / slots; rows there are
+    FastDiv slots;              // row(r) = source[r] / slots
+    uint32_t rows;              // rows there are
     uint32_t width;             // elements of a row
 };
 struct ExpertProductArgs {

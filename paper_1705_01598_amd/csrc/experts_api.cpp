@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include "experts.hpp"
+#include "plan.hpp"
 
 namespace tperm {
 template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream);
@@ -183,7 +184,7 @@ tperm_status_t tperm_expert_product(const void* x, int64_t x_stride, int64_t x_r
     const tperm_status_t bad = check(arrays);
     if (bad != TPERM_OK) return bad;
     ExpertProductArgs a = {};
-    a.x.p = x, a.x.source = source, a.x.stride = x_stride, a.x.slots = source ? (uint32_t)slots : 1u, a.x.rows = (uint32_t)x_rows, a.x.width = (uint32_t)k;
+    a.x.p = x, a.x.source = source, a.x.stride = x_stride, a.x.slots = make_fastdiv(source ? (uint32_t)slots : 1u), a.x.rows = (uint32_t)x_rows, a.x.width = (uint32_t)k;
     a.w = w, a.out = out, a.offsets = offsets, a.out_stride = out_stride;
     a.rows = (uint32_t)rows, a.experts = (uint32_t)experts, a.k = (uint32_t)k, a.n = (uint32_t)n;
     return launched(launch_expert_product(a, type, w_k_first != 0, (hipStream_t)hip_stream));
@@ -213,8 +214,8 @@ tperm_status_t tperm_expert_weight_gradient(const void* x, int64_t x_stride, con
     const tperm_status_t bad = check(arrays);
     if (bad != TPERM_OK) return bad;
     ProductSide xs = {}, gs = {};
-    xs.p = x, xs.scales = x_scales, xs.source = source, xs.stride = x_stride, xs.slots = source ? (uint32_t)slots : 1u, xs.rows = (uint32_t)x_rows, xs.width = (uint32_t)k;
-    gs.p = grad, gs.stride = grad_stride, gs.slots = 1, gs.rows = (uint32_t)rows, gs.width = (uint32_t)n;
+    xs.p = x, xs.scales = x_scales, xs.source = source, xs.stride = x_stride, xs.slots = make_fastdiv(source ? (uint32_t)slots : 1u), xs.rows = (uint32_t)x_rows, xs.width = (uint32_t)k;
+    gs.p = grad, gs.stride = grad_stride, gs.slots = make_fastdiv(1u), gs.rows = (uint32_t)rows, gs.width = (uint32_t)n;
     WeightGradientArgs a = {};
     a.fast = w_k_first ? xs : gs, a.slow = w_k_first ? gs : xs;
     a.out = out, a.offsets = offsets, a.rows = (uint32_t)rows, a.experts = (uint32_t)experts, a.out_type = out_type, a.accumulate = accumulate != 0;
