@@ -41,6 +41,16 @@ template <typename T, int N, bool ALIGNED> __device__ __forceinline__ void store
             if (i < there) p[i] = v[i];
 }
 
+// The same past the caches, for vectors of 16 bytes at their alignment.
+template <typename T, int N, bool ALIGNED> __device__ __forceinline__ Vec<T, N> load_once(const T* p, int there) {
+    if constexpr (ALIGNED && sizeof(Vec<T, N>) == 16) return __builtin_bit_cast(Vec<T, N>, __builtin_nontemporal_load((const u32x4*)p));
+    else return load_some<T, N, ALIGNED>(p, there);
+}
+template <typename T, int N, bool ALIGNED> __device__ __forceinline__ void store_once(T* p, Vec<T, N> v, int there) {
+    if constexpr (ALIGNED && sizeof(Vec<T, N>) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+    else store_some<T, N, ALIGNED>(p, v, there);
+}
+
 // Conversions round to nearest even.
 template <typename T, int N> __device__ __forceinline__ Vec<float, N> widen(Vec<T, N> v) { return __builtin_convertvector(v, Vec<float, N>); }
 template <typename T, int N> __device__ __forceinline__ Vec<T, N> narrow(Vec<float, N> v) { return __builtin_convertvector(v, Vec<T, N>); }
