@@ -84,7 +84,7 @@ template <typename T, int LAYOUT, int FREE> __device__ __forceinline__ Frag<T> f
     }
 }
 
-// --- from memory to LDS, by way of registers: any size, stride and alignment ---
+// --- operands ---
 
 // The operand of one side: a matrix of memory rows.
 struct Operand {
@@ -101,68 +101,6 @@ struct Operand {
         const uint32_t s = source != nullptr ? (uint32_t)source[r] : r;
         *row = source != nullptr ? fdiv(s, slots) : s;      // right for s < 2^31
         return s < 1u << 31 && *row < rows;
-    }
-};
-
-// A stage of FREE free indices x 128 bytes of depth.  `free_end`, `depth_end`: one behind the last index that
-// belongs to the tile; what lies beyond becomes zero.
-template <typename T, int LAYOUT, int FREE, int THREADS> struct Stage {
-    static constexpr int V = 16 / sizeof(T);                                // elements of a chunk in LDS
-    static constexpr int kIn = LAYOUT == kCodes ? 16 : V;                   // elements that a thread fetches at once
-    static constexpr int kDepth = kStageBytes / sizeof(T);
-    static constexpr int kFetches = FREE * kDepth / kIn / THREADS;
-    static constexpr int kAcross = (LAYOUT == kDepthFast ? kDepth : FREE) / kIn;
-    static_assert(kFetches * kIn * THREADS == FREE * kDepth, "whole passes");
-    u32x4 reg[kFetches];
-    float scale[LAYOUT == kCodes ? kFetches : 1];
-
-    __device__ __forceinline__ void fetch(const Operand& m, uint32_t free0, uint32_t free_end, uint32_t depth0, uint32_t depth_end) {
-#pragma unroll
-        for (int p = 0; p < kFetches; ++p) {
-            const uint32_t id = threadIdx.x + p * THREADS, other = id / kAcross, along = id % kAcross * kIn;
-            const uint32_t f = free0 + (LAYOUT == kDepthFast ? other : along), d = depth0 + (LAYOUT == kDepthFast ? along : other);
-            u32x4 v = {};
-            uint32_t row;
-            if constexpr (LAYOUT == kCodes) scale[p] = 0.0f;
-            if (f < free_end && d < depth_end && m.find(LAYOUT == kDepthFast ? f : d, &row)) {
-                const int there = (int)(LAYOUT == kDepthFast ? depth_end - d : free_end - f);
-                if constexpr (LAYOUT == kCodes) {
-                    v = __builtin_bit_cast(u32x4, load_some<uint8_t, 16, false>((const uint8_t*)m.p + (int64_t)row * m.width + f, there));
-                    scale[p] = power_of(m.scales[(int64_t)row * ((m.width + 31) / 32) + f / 32]);
-                } else {
-                    const T* const at = (const T*)m.p + (int64_t)row * m.stride + (LAYOUT == kDepthFast ? d : f);
-                    v = __builtin_bit_cast(u32x4, load_some<T, V, false>(at, there));
-                }
-            }
-            reg[p] = v;
-        }
-    }
-    __device__ __forceinline__ void put(char* tile) const {
-#pragma unroll
-        for (int p = 0; p < kFetches; ++p) {
-            const uint32_t id = threadIdx.x + p * THREADS, row = id / kAcross, c = id % kAcross;
-            if constexpr (LAYOUT == kCodes) {
-                constexpr uint32_t kChunks = FREE * sizeof(T) / 16;
-                char* const at = tile + row * (FREE * sizeof(T));
-                Vec<T, 16> v;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const Vec<T, 8> w = narrow<T, 8>(values_of<T>(u32x2{reg[p][2 * h], reg[p][2 * h + 1]}, scale[p]));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[8 * h + e] = w[e];
-                }
-#pragma unroll
-                for (int k = 0; k < 16 / V; ++k) {
-                    Frag<T> part;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) part[e] = v[k * V + e];
-                    *(Frag<T>*)(at + swizzle<T, LAYOUT>(row, c * (16 / V) + k, kChunks) * 16) = part;
-                }
-            } else {
-                constexpr uint32_t kPitch = LAYOUT == kDepthFast ? kStageBytes : FREE * sizeof(T);
-                *(u32x4*)(tile + row * kPitch + swizzle<T, LAYOUT>(row, c, kPitch / 16) * 16) = reg[p];
-            }
-        }
     }
 };
 
@@ -194,37 +132,6 @@ template <typename T, int FL, int SL, typename S> struct Step {
             for (int j = 0; j < S::SI; ++j) acc[j][i] = Matrix<T>::mul(f[i], s[j], acc[j][i]);
     }
 };
-
-// Sum over depth0 .. depth_end into acc, by way of registers.
-template <typename T, int FL, int SL, typename S>
-__device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0, uint32_t slow_end,
-                                         uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
-    constexpr uint32_t kDepth = kStageBytes / sizeof(T);
-    char* const ft = lds;
-    char* const st = lds + S::kFast * kStageBytes;
-    Stage<T, FL, S::kFast, S::kThreads> fs;
-    Stage<T, SL, S::kSlow, S::kThreads> ss;
-    if (depth0 < depth_end) {
-        fs.fetch(fast, fast0, fast_end, depth0, depth_end);
-        ss.fetch(slow, slow0, slow_end, depth0, depth_end);
-    }
-    for (uint32_t d = depth0; d < depth_end; d += kDepth) {
-        __syncthreads();
-        fs.put(ft);
-        ss.put(st);
-        __syncthreads();
-        if (d + kDepth < depth_end) {
-            fs.fetch(fast, fast0, fast_end, d + kDepth, depth_end);
-            ss.fetch(slow, slow0, slow_end, d + kDepth, depth_end);
-        }
-#pragma unroll
-        for (uint32_t kk = 0; kk < kSteps; ++kk) {
-            Step<T, FL, SL, S> step;
-            step.read(lds, kk);
-            step.multiply(acc);
-        }
-    }
-}
 
 // --- from memory straight to LDS: rows of whole 16-byte chunks that start on 16 bytes ---
 
@@ -339,6 +246,94 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     __device__ __forceinline__ void put(char*) const {}     // it goes there by itself
 };
 
+// Up to 16 bytes from q on of a tensor that ends at `end`: `there` elements exist, the others become zero.
+template <typename E> __device__ __forceinline__ u32x4 fetch_some(const E* q, int there, const char* end) {
+    constexpr int V = 16 / sizeof(E);
+    u32x4 v = {};
+    if (there > 0) {
+        if ((const char*)q + 16 <= end) {
+            __builtin_memcpy(&v, q, 16);
+            if (there < V) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int bits = (there * (int)sizeof(E) - 4 * w) * 8;
+                    v[w] = bits >= 32 ? v[w] : bits <= 0 ? 0u : v[w] & ((1u << bits) - 1u);
+                }
+            }
+        } else {
+            E e[V] = {};
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < there) e[i] = q[i];
+            __builtin_memcpy(&v, e, 16);
+        }
+    }
+    return v;
+}
+
+// The operand of one side, of any size, stride and alignment, by way of registers: requested while the stage before is
+// multiplied, put to LDS behind that.
+template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
+    static constexpr int V = 16 / sizeof(T);
+    static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
+    static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
+    static constexpr uint32_t kAcross = LAYOUT == kDepthFast ? 8 : FREE * sizeof(T) / 16;
+    static constexpr uint32_t kRowsPerFetch = THREADS / kAcross;
+    static_assert(kFetches * THREADS * 16 == FREE * kStageBytes && kRowsPerFetch * kAcross == THREADS, "whole passes");
+    const char *base, *end;
+    int64_t row_bytes;
+    const char* at[LAYOUT == kDepthFast ? kFetches : 1];    // a row's chunk, without the depth; NULL: no such row
+    uint32_t row[LAYOUT == kDepthFast ? 1 : kFetches];
+    const int32_t* source;
+    FastDiv slots;
+    uint32_t rows, free, free_end;
+    u32x4 reg[kFetches];
+
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
+    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end_) {
+        base = (const char*)m.p, row_bytes = m.stride * (int64_t)sizeof(T);
+        end = base + ((int64_t)m.rows - 1) * row_bytes + (int64_t)m.width * (int64_t)sizeof(T);
+        source = m.source, slots = m.slots, rows = m.rows;
+        if constexpr (LAYOUT == kDepthFast) {
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                uint32_t r = free0 + lds_row(p), to;
+                at[p] = r < free_end_ && m.find(r, &to) ? base + to * row_bytes + threadIdx.x % kAcross * 16 : nullptr;
+            }
+        } else {
+            free = free0 + threadIdx.x % kAcross * V, free_end = free_end_;
+        }
+    }
+    __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
+        if constexpr (LAYOUT != kDepthFast)
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                const uint32_t d = depth0 + lds_row(p);
+                row[p] = d >= depth_end ? 0xFFFFFFFFu : source != nullptr ? (uint32_t)source[d] : d;
+            }
+    }
+    __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
+#pragma unroll
+        for (int p = 0; p < kFetches; ++p) {
+            if constexpr (LAYOUT == kDepthFast) {
+                const uint32_t d = depth0 + threadIdx.x % kAcross * V;
+                reg[p] = fetch_some((const T*)(at[p] + (uint64_t)depth0 * sizeof(T)), at[p] != nullptr && d < depth_end ? (int)(depth_end - d) : 0, end);
+            } else {
+                const uint32_t to = source != nullptr ? fdiv(row[p], slots) : row[p];
+                const bool there = row[p] < 1u << 31 && to < rows && free < free_end;
+                reg[p] = fetch_some((const T*)(base + to * row_bytes) + free, there ? (int)(free_end - free) : 0, end);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char* tile) const {
+        __builtin_amdgcn_sched_barrier(0);      // not before the products: it would wait for the loads there
+        constexpr uint32_t kPitch = LAYOUT == kDepthFast ? kStageBytes : FREE * sizeof(T);
+#pragma unroll
+        for (int p = 0; p < kFetches; ++p)
+            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), threadIdx.x % kAcross, kAcross) * 16) = reg[p];
+    }
+};
+
 // 8 codes as elements; `safe`: the scale cannot carry them beyond the type's range.
 template <typename T> __device__ __forceinline__ Vec<T, 8> elements_of(u32x2 codes, float scale, bool safe) {
     if constexpr (sizeof(T) == 2) {
@@ -359,17 +354,19 @@ template <typename T> __device__ __forceinline__ Vec<T, 8> elements_of(u32x2 cod
     return narrow<T, 8>(values_of<T>(codes, scale));
 }
 
-// The operand of one side kept in codes (rows of whole 16-byte chunks that start on 16 bytes): through registers, where
-// codes become elements.  A stage is fetched while the one before it is multiplied, its rows looked up one
-// stage before that.
-template <typename T, int FREE, int THREADS> struct Coded {
+// The operand of one side kept in codes: through registers, where codes become elements.  A stage is fetched while the one
+// before it is multiplied, its rows looked up one stage before that.  LOOSE: rows of any length and alignment;
+// else of whole 16-byte chunks that start on 16 bytes.
+template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr uint32_t kAcross = FREE / 16, kRowsPerFetch = THREADS / kAcross;
-    static constexpr int kFetches = kDepth / kRowsPerFetch;
-    static_assert(kFetches * kRowsPerFetch == kDepth && kRowsPerFetch * kAcross == THREADS, "whole passes");
+    // a stage of few 32-bit columns is less than one fetch: the last threads have nothing to do
+    static constexpr int kFetches = kRowsPerFetch > kDepth ? 1 : kDepth / kRowsPerFetch;
+    static_assert(kFetches * kRowsPerFetch >= kDepth && kRowsPerFetch * kAcross == THREADS, "whole passes");
     const uint8_t *codes, *scales;
     const int32_t* source;
     uint32_t width, blocks, rows, free;
+    int free_there;
     FastDiv slots;
     bool there;
     uint32_t row[kFetches];
@@ -379,14 +376,14 @@ template <typename T, int FREE, int THREADS> struct Coded {
     static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
     __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
         free = free0 + threadIdx.x % kAcross * 16;
-        there = free < free_end;
+        there = free < free_end && lds_row(0) < kDepth, free_there = (int)(free_end - free);
         codes = (const uint8_t*)m.p, scales = m.scales, source = m.source;
         width = m.width, blocks = (m.width + 31) / 32, slots = m.slots, rows = m.rows;
     }
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
         if (source != nullptr)
 #pragma unroll
-            for (int p = 0; p < kFetches; ++p) row[p] = depth0 + lds_row(p) < depth_end ? (uint32_t)source[depth0 + lds_row(p)] : 0xFFFFFFFFu;
+            for (int p = 0; p < kFetches; ++p) row[p] = there && depth0 + lds_row(p) < depth_end ? (uint32_t)source[depth0 + lds_row(p)] : 0xFFFFFFFFu;
     }
     __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
         // rows that are not looked up are reached from the stage's first one: no limit to the tensor
@@ -396,7 +393,8 @@ template <typename T, int FREE, int THREADS> struct Coded {
         for (int p = 0; p < kFetches; ++p) {
             const uint32_t at = source != nullptr ? fdiv(row[p], slots) : lds_row(p);
             const bool use = there && (source != nullptr ? row[p] < 1u << 31 && at < rows : depth0 + at < depth_end);
-            reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? at * width + free : kBeyond), 0, 0);
+            if constexpr (LOOSE) reg[p] = fetch_some(codes + (from + at) * width + free, use ? free_there : 0, (const char*)codes + (uint64_t)rows * width);
+            else reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? at * width + free : kBeyond), 0, 0);
             scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? at * blocks + free / 32 : kBeyond), 0, 0);
         }
     }
@@ -406,6 +404,7 @@ template <typename T, int FREE, int THREADS> struct Coded {
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
             const uint32_t d = lds_row(p), c = threadIdx.x % kAcross;
+            if (kRowsPerFetch > kDepth && d >= kDepth) return;
             char* const at = tile + d * (FREE * sizeof(T));
             const float by = power_of(scale[p]);
             const bool safe = __ballot(by > Range<T>::kSafe) == 0;
@@ -439,13 +438,18 @@ template <int READS, int PRODUCTS> __device__ __forceinline__ void interleave() 
 // Sum over depth0 .. depth_end into acc with two LDS images.  While the matrix cores work on one step, the fragments of
 // the next one are read; the only barrier of a stage stands between its two steps: all wavefronts have read the
 // stage's last fragments then, so its image can receive the stage after the next.
-template <typename T, int FL, int SL, bool FM, bool SM, typename S>
-__device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
+//
+// LOOSE: operands of any size and alignment.  Two sets of fragments beside operands in registers (those, and codes) do
+// not fit: there the other wavefront of the SIMD multiplies while this one reads.
+template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED, bool LOOSE>
+using Side = std::conditional_t<LAYOUT == kCodes, Coded<T, FREE, THREADS, LOOSE>, std::conditional_t<LOOSE, Loose<T, LAYOUT, FREE, THREADS>, Direct<T, LAYOUT, FREE, THREADS, MAPPED>>>;
+template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE>
+__device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
                                                 uint32_t slow_end, uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
     constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     constexpr uint32_t kImage = (S::kFast + S::kSlow) * kStageBytes;
-    std::conditional_t<FL == kCodes, Coded<T, S::kFast, S::kThreads>, Direct<T, FL, S::kFast, S::kThreads, FM>> fs;
-    std::conditional_t<SL == kCodes, Coded<T, S::kSlow, S::kThreads>, Direct<T, SL, S::kSlow, S::kThreads, SM>> ss;
+    Side<T, FL, S::kFast, S::kThreads, FM, LOOSE> fs;
+    Side<T, SL, S::kSlow, S::kThreads, SM, LOOSE> ss;
     constexpr bool kOrdered = sizeof(T) == 2;
     constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
     if (depth0 >= depth_end) return;
@@ -467,9 +471,7 @@ __device__ __forceinline__ void sum_tile_direct(char* lds, const Operand& fast, 
     issue(0, depth0);
     look_up(depth0 + kDepth);
     put(0);
-    if constexpr (FL == kCodes || SL == kCodes) {
-        // two sets of fragments and codes do not fit the registers: the other wavefront of the SIMD multiplies
-        // while this one reads
+    if constexpr (LOOSE || FL == kCodes || SL == kCodes) {
         for (uint32_t d = depth0, image = 0; d < depth_end; d += kDepth, image ^= kImage) {
             arrive<0>();
             issue(image ^ kImage, d + kDepth);
@@ -551,7 +553,7 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
                                                 const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
     constexpr uint32_t kPitch = S::kFast * sizeof(O), kChunks = kPitch / 16, V = 16 / sizeof(O);
     constexpr int kPasses = (S::kSlow * (int)kPitch + LDS_BYTES - 1) / LDS_BYTES, kRows = S::kSlow / kPasses;
-    static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow && kChunks >= 16, "whole blocks");
+    static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow, "whole blocks");
     const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
     const uint32_t f0 = wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
     const uint32_t s0 = wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
@@ -565,7 +567,7 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
 #pragma unroll
                 for (int i = 0; i < S::FI; ++i) {
                     const uint32_t at = (f0 + i * 16) * (uint32_t)sizeof(O);
-                    *(Vec<O, 4>*)(lds + row * kPitch + ((at / 16) ^ (row & 15u)) * 16 + at % 16) = narrow<O, 4>(acc[j][i]);
+                    *(Vec<O, 4>*)(lds + row * kPitch + ((at / 16) ^ (row & (kChunks < 16 ? kChunks - 1 : 15u))) * 16 + at % 16) = narrow<O, 4>(acc[j][i]);
                 }
             }
         }
@@ -574,7 +576,7 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
             const uint32_t row = id / kChunks, c = id % kChunks, s = slow0 + pass * kRows + row, f = fast0 + c * V;
             if (s >= slow_end) break;
             if (f >= fast_end) continue;
-            Vec<O, V> v = *(const Vec<O, V>*)(lds + row * kPitch + (c ^ (row & 15u)) * 16);
+            Vec<O, V> v = *(const Vec<O, V>*)(lds + row * kPitch + (c ^ (row & (kChunks < 16 ? kChunks - 1 : 15u))) * 16);
             O* const p = out + (int64_t)s * stride + f;
             if constexpr (sizeof(O) == 4)
                 if (accumulate) v += load_some<O, V, false>(p, (int)(fast_end - f));
@@ -635,8 +637,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t exper
 
 // --- kernels ---
 
-// DIRECT: operands go straight to LDS (two images); else by way of registers.
-template <typename T, int WL, typename S, bool DIRECT>
+template <typename T, int WL, typename S, bool LOOSE>
 __global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const ExpertProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t across = (a.n + S::kFast - 1) / S::kFast;
@@ -647,11 +648,9 @@ __global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const Exper
     if (bin < a.experts) {
         const T* const w = (const T*)a.w + (int64_t)bin * a.k * a.n;
         const Operand fast = WL == kDepthFast ? Operand(w, a.n, a.k) : Operand(w, a.k, a.n);
-        if constexpr (DIRECT) sum_tile_direct<T, WL, kDepthFast, false, false, S>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
-        else sum_tile<T, WL, kDepthFast, S>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
+        sum_tile<T, WL, kDepthFast, false, false, S, LOOSE>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
     }
-    if constexpr (DIRECT) store_tile_rows<T, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
-    else store_tile<T, S>((T*)a.out, a.out_stride, col0, col_end, row0, row_end, false, acc);
+    store_tile_rows<T, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
 }
 
 // The i-th expert by number of rows, most first (equal ones in their order), for up to 64 experts: every lane counts how many
@@ -671,7 +670,7 @@ __device__ __forceinline__ uint32_t by_size(const int32_t* offsets, uint32_t exp
 }
 
 // Experts one after the other; every XCD takes a run of an expert's tiles, whichever experts are large.
-template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool DIRECT>
+template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE>
 __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const WeightGradientArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t tf = (a.fast.width + S::kFast - 1) / S::kFast, ts = (a.slow.width + S::kSlow - 1) / S::kSlow, run = (tf * ts + kXcds - 1) / kXcds;
@@ -685,12 +684,10 @@ __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const Weig
     uint32_t from, end;
     rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
     f32x4 acc[S::SI][S::FI] = {};
-    if constexpr (DIRECT) sum_tile_direct<T, FL, SL, FM, SM, S>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
-    else sum_tile<T, FL, SL, S>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
+    sum_tile<T, FL, SL, FM, SM, S, LOOSE>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
     const int64_t at = (int64_t)expert * a.fast.width * a.slow.width;
     const bool accumulate = a.accumulate != 0;
-    if (DIRECT && a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
-    else if (a.out_type == TPERM_TYPE_F32) store_tile<float, S>((float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
+    if (a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
     else if (a.out_type == TPERM_TYPE_F16) store_tile<_Float16, S>((_Float16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
     else store_tile<__bf16, S>((__bf16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
 }
