@@ -104,8 +104,9 @@ struct Operand {
     }
 };
 
-// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side.
-template <int FAST_, int SLOW_, int WAVES, int WF_> struct TileShape {
+// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side, IMAGES stages in LDS.
+template <int FAST_, int SLOW_, int WAVES, int WF_, int IMAGES> struct TileShape {
+    static constexpr int kImages = IMAGES, kImage = (FAST_ + SLOW_) * kStageBytes;
     static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = WAVES * 64;
     static constexpr int kWavesFast = WF_, kWavesSlow = WAVES / WF_;
     static constexpr int FI = FAST_ / kWavesFast / 16, SI = SLOW_ / kWavesSlow / 16;   // 16 x 16 blocks of a wavefront
@@ -168,10 +169,11 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     const char* base;
     uint32_t row_bytes;
     uint32_t off[kFetches];             // from base (kDepthFast: + depth; kFreeFast: + stage, MAPPED: of the column alone)
-    // MAPPED: what a wavefront's lanes add to it in each fetch: kRowsPerWave memory rows, the same for the
-    // lanes of one, kept in scalar registers
+    // MAPPED: memory rows that a wavefront's lanes read in each fetch; two are kept in scalar registers (16 a stage of
+    // narrower tiles take longer than a look-up by every lane: 81 us against 61 with 128 columns)
     static constexpr int kRowsPerWave = 64 / kAcross;
-    uint32_t row[MAPPED ? kFetches : 1][MAPPED ? kRowsPerWave : 1];
+    static constexpr bool kScalar = kRowsPerWave <= 2;
+    uint32_t row[MAPPED ? kFetches : 1][MAPPED && kScalar ? kRowsPerWave : 1];
     const int32_t* source;
     FastDiv slots;
     uint32_t rows;
@@ -200,9 +202,15 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             }
         }
     }
-    // MAPPED: entries of source for the stage at `depth0`, by scalar loads.
+    // MAPPED: entries of source for the stage at `depth0`.
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
-        if constexpr (MAPPED) {
+        if constexpr (MAPPED && !kScalar) {
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) {
+                const uint32_t d = depth0 + lds_row(p);
+                row[p][0] = (uint32_t)source[d < depth_end ? d : depth_end - 1];
+            }
+        } else if constexpr (MAPPED) {
             typedef const __attribute__((address_space(4))) int32_t* Scalar;
             const uint32_t first = depth0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kRowsPerWave;
 #pragma unroll
@@ -226,6 +234,9 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             uint32_t o = off[p];
             if constexpr (LAYOUT == kDepthFast) {
                 if (left < kDepth) o = chunk(p) * V < left ? o : kBeyond;
+            } else if constexpr (MAPPED && !kScalar) {
+                const uint32_t at = fdiv(row[p][0], slots);
+                o = lds_row(p) < left && row[p][0] < 1u << 31 && at < rows && o != kBeyond ? at * row_bytes + o : kBeyond;
             } else if constexpr (MAPPED) {
                 const uint32_t in_wave = (threadIdx.x & 63u) / kAcross;
                 uint32_t start = 0;
@@ -435,9 +446,9 @@ template <int READS, int PRODUCTS> __device__ __forceinline__ void interleave() 
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Sum over depth0 .. depth_end into acc with two LDS images.  While the matrix cores work on one step, the fragments of
-// the next one are read; the only barrier of a stage stands between its two steps: all wavefronts have read the
-// stage's last fragments then, so its image can receive the stage after the next.
+// Sum over depth0 .. depth_end into acc with a ring of LDS images.  While the matrix cores work on one step, the fragments
+// of the next one are read; the only barrier of a stage stands between its two steps: all wavefronts have read the
+// stage's last fragments then, so its image can receive another stage.
 //
 // LOOSE: operands of any size and alignment.  Two sets of fragments beside operands in registers (those, and codes) do
 // not fit: there the other wavefront of the SIMD multiplies while this one reads.
@@ -447,7 +458,7 @@ template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE>
 __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
                                                 uint32_t slow_end, uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
     constexpr uint32_t kDepth = kStageBytes / sizeof(T);
-    constexpr uint32_t kImage = (S::kFast + S::kSlow) * kStageBytes;
+    constexpr uint32_t kImage = S::kImage;
     Side<T, FL, S::kFast, S::kThreads, FM, LOOSE> fs;
     Side<T, SL, S::kSlow, S::kThreads, SM, LOOSE> ss;
     constexpr bool kOrdered = sizeof(T) == 2;
@@ -467,11 +478,11 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
         fs.put(lds + image);
         ss.put(lds + image + S::kFast * kStageBytes);
     };
-    look_up(depth0);
-    issue(0, depth0);
-    look_up(depth0 + kDepth);
-    put(0);
     if constexpr (LOOSE || FL == kCodes || SL == kCodes) {
+        look_up(depth0);
+        issue(0, depth0);
+        look_up(depth0 + kDepth);
+        put(0);
         for (uint32_t d = depth0, image = 0; d < depth_end; d += kDepth, image ^= kImage) {
             arrive<0>();
             issue(image ^ kImage, d + kDepth);
@@ -484,30 +495,34 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
             }
             put(image ^ kImage);
         }
-        arrive<0>();
-        return;
-    }
-    arrive<0>();
-    issue(kImage, depth0 + kDepth);
-    look_up(depth0 + 2 * kDepth);
-    uint32_t image = 0;
-    Step<T, FL, SL, S> even, odd;
-    even.read(lds, 0);
-    for (uint32_t d = depth0; d + kDepth < depth_end; d += kDepth) {
+    } else {
+        constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;     // of a stage
+        look_up(depth0);
+#pragma unroll
+        for (int i = 0; i < S::kImages; ++i) {
+            issue(i * kImage, depth0 + i * kDepth);
+            look_up(depth0 + (i + 1) * kDepth);
+        }
+        arrive<(S::kImages - 1) * kLoads>();
+        uint32_t image = 0;
+        Step<T, FL, SL, S> even, odd;
+        even.read(lds, 0);
+        for (uint32_t d = depth0; d + kDepth < depth_end; d += kDepth) {
+            odd.read(lds + image, 1);
+            even.multiply(acc);
+            if constexpr (kOrdered) interleave<kReads, kProducts>();
+            arrive<(S::kImages - 2) * kLoads>();        // the next stage has arrived
+            issue(image, d + S::kImages * kDepth);
+            look_up(d + (S::kImages + 1) * kDepth);
+            image = image == (S::kImages - 1) * kImage ? 0 : image + kImage;
+            even.read(lds + image, 0);
+            odd.multiply(acc);
+            if constexpr (kOrdered) interleave<kReads, kProducts>();
+        }
         odd.read(lds + image, 1);
         even.multiply(acc);
-        if constexpr (kOrdered) interleave<kReads, kProducts>();
-        arrive<0>();
-        issue(image, d + 2 * kDepth);
-        look_up(d + 3 * kDepth);
-        image ^= kImage;
-        even.read(lds + image, 0);
         odd.multiply(acc);
-        if constexpr (kOrdered) interleave<kReads, kProducts>();
     }
-    odd.read(lds + image, 1);
-    even.multiply(acc);
-    odd.multiply(acc);
     arrive<0>();            // nothing travels to LDS when it is used again
 }
 
@@ -545,12 +560,13 @@ __device__ __forceinline__ void rows_of(const int32_t* offsets, uint32_t experts
     *from = o < *end ? o : *end;
 }
 
-// The same by way of LDS (LDS_BYTES, free by now), in whole rows of the tile: a wavefront's own results are pieces of 8 or
+// The same by way of LDS (all of it, free by now), in whole rows of the tile: a wavefront's own results are pieces of 8 or
 // 16 bytes of 16 rows.  Chunks of 16 bytes change places by their row, so that those pieces meet no bank
 // conflicts.
-template <typename O, typename S, int LDS_BYTES>
+template <typename O, typename S>
 __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
                                                 const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
+    constexpr int LDS_BYTES = S::kImages * S::kImage;
     constexpr uint32_t kPitch = S::kFast * sizeof(O), kChunks = kPitch / 16, V = 16 / sizeof(O);
     constexpr int kPasses = (S::kSlow * (int)kPitch + LDS_BYTES - 1) / LDS_BYTES, kRows = S::kSlow / kPasses;
     static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow, "whole blocks");
@@ -650,7 +666,7 @@ __global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const Exper
         const Operand fast = WL == kDepthFast ? Operand(w, a.n, a.k) : Operand(w, a.k, a.n);
         sum_tile<T, WL, kDepthFast, false, false, S, LOOSE>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
     }
-    store_tile_rows<T, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
+    store_tile_rows<T, S>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
 }
 
 // The i-th expert by number of rows, most first (equal ones in their order), for up to 64 experts: every lane counts how many
@@ -687,7 +703,7 @@ __global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const Weig
     sum_tile<T, FL, SL, FM, SM, S, LOOSE>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
     const int64_t at = (int64_t)expert * a.fast.width * a.slow.width;
     const bool accumulate = a.accumulate != 0;
-    if (a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S, 2 * (S::kFast + S::kSlow) * kStageBytes>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
+    if (a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
     else if (a.out_type == TPERM_TYPE_F16) store_tile<_Float16, S>((_Float16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
     else store_tile<__bf16, S>((__bf16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
 }

@@ -6,9 +6,9 @@
 
 namespace tperm {
 
-using TinyTile = TileShape<64, 64, 4, 2>;
-using SmallTile = TileShape<128, 128, 4, 2>;
-using WideTile = TileShape<256, 256, 8, 4>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
+using TinyTile = TileShape<64, 64, 4, 2, 4>;
+using SmallTile = TileShape<128, 128, 4, 2, 2>;
+using WideTile = TileShape<256, 256, 8, 4, 2>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
 
 // Workgroups with more than 64 KiB of LDS have to be allowed it, once on each device.
 template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
@@ -24,7 +24,7 @@ template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
 }
 
 template <auto KERNEL, typename S, typename A> hipError_t go(uint64_t blocks, const A& a, hipStream_t stream) {
-    constexpr size_t kLds = 2 * (size_t)(S::kFast + S::kSlow) * kStageBytes;    // two images
+    constexpr size_t kLds = (size_t)S::kImages * S::kImage;
     if constexpr (kLds > 64 * 1024) {
         const hipError_t e = allow_lds<KERNEL>(kLds);
         if (e != hipSuccess) return e;
@@ -38,15 +38,6 @@ inline bool on_chunks(size_t elem, const void* p, int64_t stride, uint32_t width
     return width * elem % 16 == 0 && ((uintptr_t)p | (uintptr_t)stride * elem) % 16 == 0 && stride < (int64_t)1 << 22;
 }
 
-enum Tile { kTiny, kSmall, kWide };
-
-// The tile for `results` results in rectangles of which every expert has one or some: large tiles need fewer bytes from
-// LDS and L2 an operation, small ones fill the 256 compute units.
-inline Tile tile_for(uint64_t wide_tiles, uint64_t small_tiles, size_t elem) {
-    if (elem == 2 && wide_tiles >= 128) return kWide;
-    return small_tiles >= 128 ? kSmall : kTiny;
-}
-
 inline uint64_t over(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 template <typename T, typename S, bool LOOSE> hipError_t product_tiles(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
@@ -55,15 +46,17 @@ template <typename T, typename S, bool LOOSE> hipError_t product_tiles(const Exp
 }
 
 template <typename T, bool LOOSE> hipError_t product_with(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
-    // rows of an expert on the average, tiles of it
+    // Large tiles need fewer bytes an operation, small ones fill the 256 compute units and waste less on experts of
+    // few rows (bf16, us with tiles of 256, 128, 64; rows of all experts on the average):
+    //   8 experts 1024 x 1024: 128 rows 28 19 13, 256 rows 29 19 19, 512 rows 30 24 27, 1024 rows 32 39 46
+    //   8 experts 2048 x 2048: 256 rows 48 38 44, 512 rows 51 60 72;  64 experts: 128 rows 183 177 197, 256 rows 238 244 326
+    //   64 experts 2048 x 1024, one row: 24 with 128, 19 with 64; 16 rows 60, 56
     const uint64_t rows = over(a.rows, a.experts);
     const auto tiles = [&](uint64_t side) { return over(rows, side) * a.experts * over(a.n, side); };
-    switch (tile_for(rows >= 128 ? tiles(256) : 0, tiles(128), sizeof(T))) {
-        case kWide:
-            if constexpr (sizeof(T) == 2) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
-        case kSmall: return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
-        default: return product_tiles<T, TinyTile, LOOSE>(a, w_k_first, stream);
-    }
+    if constexpr (sizeof(T) == 2)
+        if (rows >= 192 && tiles(256) >= 128) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
+    if (rows >= 64 && tiles(128) >= 128) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
+    return product_tiles<T, TinyTile, LOOSE>(a, w_k_first, stream);
 }
 
 template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
@@ -84,12 +77,11 @@ template <typename T, typename S, bool LOOSE> hipError_t gradient_tiles(const We
 
 template <typename T, bool LOOSE> hipError_t gradient_with(const WeightGradientArgs& a, hipStream_t stream) {
     const auto tiles = [&](uint64_t side) { return over(a.fast.width, side) * over(a.slow.width, side) * a.experts; };
-    switch (tile_for(tiles(256), tiles(128), sizeof(T))) {
-        case kWide:
-            if constexpr (sizeof(T) == 2) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
-        case kSmall: return gradient_tiles<T, SmallTile, LOOSE>(a, stream);
-        default: return gradient_tiles<T, TinyTile, LOOSE>(a, stream);
-    }
+    // As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 79 49 71,
+    // 2048 x 2048 (512) 104 117 270
+    if constexpr (sizeof(T) == 2)
+        if (tiles(256) >= 192) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
+    return tiles(128) >= 256 ? gradient_tiles<T, SmallTile, LOOSE>(a, stream) : gradient_tiles<T, TinyTile, LOOSE>(a, stream);
 }
 
 template <typename T> hipError_t gradient_of(const WeightGradientArgs& a, hipStream_t stream) {
