@@ -5,6 +5,7 @@
 // bit patterns.  Scales are powers of two, so the division is exact and the only rounding is that of the code.
 #include "experts.hpp"
 #include "expert_vector.hpp"
+#include "plan.hpp"
 
 namespace tperm {
 
@@ -36,16 +37,17 @@ struct Place {
     uint32_t row, col;
     int there;
 };
-__device__ __forceinline__ Place place_of(uint64_t at, uint32_t rows, uint32_t width) {
-    const uint32_t per_row = (width + 31) / 32 * 4;
+__device__ __forceinline__ Place place_of(const CheckpointArgs& a) {
+    const uint32_t rows = a.rows, width = a.width, per_row = (width + 31) / 32 * 4;
+    const uint64_t at = long_block() * kCheckpointThreads + threadIdx.x;
     Place p;
-    const uint64_t row = at / per_row;
+    // a 64-bit division takes longer than the rest of a thread's arithmetic
+    const uint64_t row = a.per_row.magic != 0 ? fdiv((uint32_t)at, a.per_row) : at / per_row;
     p.row = (uint32_t)row;
     p.col = (uint32_t)(at - row * per_row) * 8;
     p.there = row < rows && p.col < width ? (int)(width - p.col) : 0;
     return p;
 }
-__device__ __forceinline__ uint64_t thread_at() { return long_block() * kCheckpointThreads + threadIdx.x; }
 
 // Codes and scale of one part of a row; part_scales: where the part's scales start.
 template <bool ALIGNED> __device__ __forceinline__ void keep(Vec<float, 8> x, const Place& p, uint8_t* codes, uint8_t* scales) {
@@ -54,7 +56,7 @@ template <bool ALIGNED> __device__ __forceinline__ void keep(Vec<float, 8> x, co
     Vec<uint8_t, 8> b;
     __builtin_memcpy(&b, &c, 8);
     if (p.there > 0) {
-        store_some<uint8_t, 8, ALIGNED>(codes + p.col, b, p.there);
+        store_once<uint8_t, 8, ALIGNED>(codes + p.col, b, p.there);
         if (p.col % 32 == 0) scales[p.col / 32] = (uint8_t)s;
     }
 }
@@ -68,24 +70,24 @@ template <typename T, bool ALIGNED> __device__ __forceinline__ Vec<float, 8> kep
 }
 
 template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThreads) void store_kernel(const CheckpointArgs a) {
-    const Place p = place_of(thread_at(), a.rows, a.width);
+    const Place p = place_of(a);
     Vec<float, 8> x = {};
     if (p.there > 0) x = widen<T, 8>(load_some<T, 8, ALIGNED>((const T*)a.in + (int64_t)p.row * a.in_stride + p.col, p.there));
     keep<ALIGNED>(x, p, a.codes + (int64_t)p.row * a.width, a.scales + (int64_t)p.row * ((a.width + 31) / 32));
 }
 
 template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThreads) void load_kernel(const CheckpointArgs a) {
-    const Place p = place_of(thread_at(), a.rows, a.width);
+    const Place p = place_of(a);
     if (p.there <= 0) return;
     const Vec<float, 8> x = kept<T, ALIGNED>(p, a.codes + (int64_t)p.row * a.width, a.scales + (int64_t)p.row * ((a.width + 31) / 32));
-    store_some<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(x), p.there);
+    store_once<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(x), p.there);
 }
 
 // 1 / (1 + exp(-g)) in binary32: exp2 and reciprocal of the hardware, 1 ulp each.
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * g)); }
 
 template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThreads) void gated_forward_kernel(const CheckpointArgs a) {
-    const Place p = place_of(thread_at(), a.rows, a.width);
+    const Place p = place_of(a);
     Vec<float, 8> g = {}, u = {};
     if (p.there > 0) {
         const T* const row = (const T*)a.in + (int64_t)p.row * a.in_stride;
@@ -94,7 +96,7 @@ template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThre
         Vec<float, 8> h;
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] = g[i] * sigmoid(g[i]) * u[i];
-        store_some<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(h), p.there);
+        store_once<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(h), p.there);
     }
     if (a.codes != nullptr) {
         const uint32_t blocks = (a.width + 31) / 32;
@@ -106,7 +108,7 @@ template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThre
 }
 
 template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThreads) void gated_backward_kernel(const CheckpointArgs a) {
-    const Place p = place_of(thread_at(), a.rows, a.width);
+    const Place p = place_of(a);
     if (p.there <= 0) return;
     const uint32_t blocks = (a.width + 31) / 32;
     const uint8_t* const codes = a.codes + (int64_t)p.row * 2 * a.width;
@@ -122,15 +124,17 @@ template <typename T, bool ALIGNED> __global__ __launch_bounds__(kCheckpointThre
         h[i] = silu * u[i];
     }
     T* const grad = (T*)a.grad_gates + (int64_t)p.row * a.grad_stride + p.col;
-    store_some<T, 8, ALIGNED>(grad, narrow<T, 8>(dg), p.there);
-    store_some<T, 8, ALIGNED>(grad + a.width, narrow<T, 8>(du), p.there);
-    if (a.out != nullptr) store_some<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(h), p.there);
+    store_once<T, 8, ALIGNED>(grad, narrow<T, 8>(dg), p.there);
+    store_once<T, 8, ALIGNED>(grad + a.width, narrow<T, 8>(du), p.there);
+    if (a.out != nullptr) store_once<T, 8, ALIGNED>((T*)a.out + (int64_t)p.row * a.out_stride + p.col, narrow<T, 8>(h), p.there);
 }
 
 bool on_eight(size_t elem, const void* p, int64_t stride) { return ((uintptr_t)p | (uintptr_t)stride * elem) % (elem * 8 < 16 ? elem * 8 : 16) == 0; }
 
-template <typename K> hipError_t go(K kernel, const CheckpointArgs& a, hipStream_t stream) {
-    const uint64_t threads = (uint64_t)a.rows * ((a.width + 31) / 32 * 4);
+template <typename K> hipError_t go(K kernel, CheckpointArgs a, hipStream_t stream) {
+    const uint32_t per_row = (a.width + 31) / 32 * 4;
+    const uint64_t threads = (uint64_t)a.rows * per_row;
+    a.per_row = threads < (1ull << 31) - kCheckpointThreads ? make_fastdiv(per_row) : FastDiv{0, 0};
     hipLaunchKernelGGL(kernel, long_grid((threads + kCheckpointThreads - 1) / kCheckpointThreads), dim3(kCheckpointThreads), 0, stream, a);
     return hipGetLastError();
 }
@@ -138,7 +142,7 @@ template <typename K> hipError_t go(K kernel, const CheckpointArgs& a, hipStream
 }  // namespace
 
 // Rows of whole eights that start on 16 bytes, codes on 8.
-hipError_t launch_checkpoint_store(const CheckpointArgs& a, int type, hipStream_t stream) {
+hipError_t launch_checkpoint_store(CheckpointArgs a, int type, hipStream_t stream) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool aligned = a.width % 8 == 0 && on_eight(sizeof(T), a.in, a.in_stride) && (uintptr_t)a.codes % 8 == 0;
@@ -146,7 +150,7 @@ hipError_t launch_checkpoint_store(const CheckpointArgs& a, int type, hipStream_
     });
 }
 
-hipError_t launch_checkpoint_load(const CheckpointArgs& a, int type, hipStream_t stream) {
+hipError_t launch_checkpoint_load(CheckpointArgs a, int type, hipStream_t stream) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool aligned = a.width % 8 == 0 && on_eight(sizeof(T), a.out, a.out_stride) && (uintptr_t)a.codes % 8 == 0;
@@ -154,7 +158,7 @@ hipError_t launch_checkpoint_load(const CheckpointArgs& a, int type, hipStream_t
     });
 }
 
-hipError_t launch_gated_forward(const CheckpointArgs& a, int type, hipStream_t stream) {
+hipError_t launch_gated_forward(CheckpointArgs a, int type, hipStream_t stream) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool aligned = a.width % 8 == 0 && on_eight(sizeof(T), a.in, a.in_stride) && on_eight(sizeof(T), a.out, a.out_stride) && (uintptr_t)a.codes % 8 == 0;
@@ -162,7 +166,7 @@ hipError_t launch_gated_forward(const CheckpointArgs& a, int type, hipStream_t s
     });
 }
 
-hipError_t launch_gated_backward(const CheckpointArgs& a, int type, hipStream_t stream) {
+hipError_t launch_gated_backward(CheckpointArgs a, int type, hipStream_t stream) {
     return with_type(type, [&](auto t) {
         using T = decltype(t);
         const bool aligned = a.width % 8 == 0 && on_eight(sizeof(T), a.in, a.in_stride) && on_eight(sizeof(T), a.out, a.out_stride) &&

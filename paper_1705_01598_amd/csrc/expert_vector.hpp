@@ -41,14 +41,21 @@ template <typename T, int N, bool ALIGNED> __device__ __forceinline__ void store
             if (i < there) p[i] = v[i];
 }
 
-// The same past the caches, for vectors of 16 bytes at their alignment.
+// The same past the caches, for vectors at their alignment (16 bytes at most).
 template <typename T, int N, bool ALIGNED> __device__ __forceinline__ Vec<T, N> load_once(const T* p, int there) {
     if constexpr (ALIGNED && sizeof(Vec<T, N>) == 16) return __builtin_bit_cast(Vec<T, N>, __builtin_nontemporal_load((const u32x4*)p));
     else return load_some<T, N, ALIGNED>(p, there);
 }
 template <typename T, int N, bool ALIGNED> __device__ __forceinline__ void store_once(T* p, Vec<T, N> v, int there) {
-    if constexpr (ALIGNED && sizeof(Vec<T, N>) == 16) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-    else store_some<T, N, ALIGNED>(p, v, there);
+    if constexpr (ALIGNED && sizeof(v) == 8) {
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x2, v), (u32x2*)p);
+    } else if constexpr (ALIGNED && sizeof(v) % 16 == 0) {
+        u32x4 w[sizeof(v) / 16];
+        __builtin_memcpy(w, &v, sizeof(v));
+        for (size_t i = 0; i < sizeof(v) / 16; ++i) __builtin_nontemporal_store(w[i], (u32x4*)p + i);
+    } else {
+        store_some<T, N, ALIGNED>(p, v, there);
+    }
 }
 
 // Conversions round to nearest even.

@@ -37,11 +37,12 @@ struct CheckpointArgs {
     uint8_t *codes, *scales;
     int64_t in_stride, out_stride, grad_stride;
     uint32_t rows, width;
+    FastDiv per_row;            // by the threads of a row, for thread numbers below 2^31 (set by the launcher)
 };
-hipError_t launch_checkpoint_store(const CheckpointArgs& a, int type, hipStream_t stream);
-hipError_t launch_checkpoint_load(const CheckpointArgs& a, int type, hipStream_t stream);
-hipError_t launch_gated_forward(const CheckpointArgs& a, int type, hipStream_t stream);
-hipError_t launch_gated_backward(const CheckpointArgs& a, int type, hipStream_t stream);
+hipError_t launch_checkpoint_store(CheckpointArgs a, int type, hipStream_t stream);
+hipError_t launch_checkpoint_load(CheckpointArgs a, int type, hipStream_t stream);
+hipError_t launch_gated_forward(CheckpointArgs a, int type, hipStream_t stream);
+hipError_t launch_gated_backward(CheckpointArgs a, int type, hipStream_t stream);
 
 // One side of an experts' product.
 struct ProductSide {
