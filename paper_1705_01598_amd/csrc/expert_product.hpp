@@ -104,10 +104,13 @@ struct Operand {
     }
 };
 
-// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side, IMAGES stages in LDS.
-template <int FAST_, int SLOW_, int WAVES, int WF_, int IMAGES> struct TileShape {
-    static constexpr int kImages = IMAGES, kImage = (FAST_ + SLOW_) * kStageBytes;
-    static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = WAVES * 64;
+// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side, IMAGES stages in LDS.  GROUPS
+// such sets of wavefronts and images each take a piece of the depth; their sums are joined in order.
+template <int FAST_, int SLOW_, int WAVES, int WF_, int IMAGES, int GROUPS = 1> struct TileShape {
+    static constexpr int kImages = IMAGES, kImage = (FAST_ + SLOW_) * kStageBytes, kGroups = GROUPS, kLds = GROUPS * IMAGES * kImage;
+    static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = WAVES * 64, kAllThreads = GROUPS * kThreads;     // kThreads: of a group
+    static __device__ __forceinline__ uint32_t wave() { return threadIdx.x % kThreads >> 6; }
+    static __device__ __forceinline__ uint32_t group() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kThreads)); }
     static constexpr int kWavesFast = WF_, kWavesSlow = WAVES / WF_;
     static constexpr int FI = FAST_ / kWavesFast / 16, SI = SLOW_ / kWavesSlow / 16;   // 16 x 16 blocks of a wavefront
 };
@@ -119,7 +122,7 @@ template <typename T, int FL, int SL, typename S> struct Step {
     static_assert(kStageBytes / sizeof(T) == kSteps * Matrix<T>::kDepth, "two steps");
     Frag<T> f[S::FI], s[S::SI];
     __device__ __forceinline__ void read(const char* image, uint32_t kk) {
-        const uint32_t wave = threadIdx.x >> 6;
+        const uint32_t wave = S::wave();
         const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
 #pragma unroll
         for (int i = 0; i < S::SI; ++i) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk);
@@ -132,7 +135,7 @@ template <typename T, int FL, int SL, typename S> struct Step {
     }
     // The i-th of FI parts of either.
     __device__ __forceinline__ void read(const char* image, uint32_t kk, int part) {
-        const uint32_t wave = threadIdx.x >> 6;
+        const uint32_t wave = S::wave();
         const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
 #pragma unroll
         for (int i = 0; i < S::SI; ++i)
@@ -171,6 +174,7 @@ template <int LOADS> __device__ __forceinline__ void arrive() {
 // The operand of one side.  A lane's 16 bytes arrive at a place in LDS that its number fixes, so the swizzle is
 // applied to where it reads.  MAPPED: depth rows (kFreeFast) are found through source, one stage ahead.
 template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Direct {
+    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
     static constexpr int V = 16 / sizeof(T);
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
@@ -189,8 +193,8 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     FastDiv slots;
     uint32_t rows;
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
-    static __device__ __forceinline__ uint32_t chunk(int p) { return swizzle<T, LAYOUT>(lds_row(p), threadIdx.x % kAcross, kAcross); }
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
+    static __device__ __forceinline__ uint32_t chunk(int p) { return swizzle<T, LAYOUT>(lds_row(p), thread() % kAcross, kAcross); }
 
     // Depth-fast: rows free0 .. free_end of m, whose row r is m.find(r).
     __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
@@ -223,7 +227,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             }
         } else if constexpr (MAPPED) {
             typedef const __attribute__((address_space(4))) int32_t* Scalar;
-            const uint32_t first = depth0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kRowsPerWave;
+            const uint32_t first = depth0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread() >> 6)) * kRowsPerWave;
 #pragma unroll
             for (int p = 0; p < kFetches; ++p)
 #pragma unroll
@@ -235,7 +239,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     }
     __device__ __forceinline__ void issue(char* tile, uint32_t depth0, uint32_t depth_end, int part = 0, int parts = 1) {
         const uint32_t left = depth0 < depth_end ? depth_end - depth0 : 0;      // beyond the end: zeros
-        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (threadIdx.x & ~63u) * 16));
+        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (thread() & ~63u) * 16));
         const char* from = base;
         uint32_t scalar = 0;
         if constexpr (LAYOUT == kDepthFast) scalar = depth0 * (uint32_t)sizeof(T);
@@ -250,12 +254,12 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
                 const uint32_t at = fdiv(row[p][0], slots);
                 o = lds_row(p) < left && row[p][0] < 1u << 31 && at < rows && o != kBeyond ? at * row_bytes + o : kBeyond;
             } else if constexpr (MAPPED) {
-                const uint32_t in_wave = (threadIdx.x & 63u) / kAcross;
+                const uint32_t in_wave = (thread() & 63u) / kAcross;
                 uint32_t start = 0;
 #pragma unroll
                 for (int i = 0; i < kRowsPerWave; ++i) {
                     const uint32_t at = fdiv(row[p][i], slots);
-                    const uint32_t d = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * kRowsPerWave + p * kRowsPerFetch + i;
+                    const uint32_t d = (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread() >> 6)) * kRowsPerWave + p * kRowsPerFetch + i;
                     const uint32_t one = d < left && row[p][i] < 1u << 31 && at < rows ? at * row_bytes : kBeyond;
                     start = in_wave == (uint32_t)i ? one : start;
                 }
@@ -297,6 +301,7 @@ template <typename E> __device__ __forceinline__ u32x4 fetch_some(const E* q, in
 // The operand of one side, of any size, stride and alignment, by way of registers: requested while the stage before is
 // multiplied, put to LDS behind that.
 template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
+    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
     static constexpr int V = 16 / sizeof(T);
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
@@ -312,7 +317,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
     uint32_t rows, free, free_end;
     u32x4 reg[kFetches];
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
     __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end_) {
         base = (const char*)m.p, row_bytes = m.stride * (int64_t)sizeof(T);
         end = base + ((int64_t)m.rows - 1) * row_bytes + (int64_t)m.width * (int64_t)sizeof(T);
@@ -321,10 +326,10 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) {
                 uint32_t r = free0 + lds_row(p), to;
-                at[p] = r < free_end_ && m.find(r, &to) ? base + to * row_bytes + threadIdx.x % kAcross * 16 : nullptr;
+                at[p] = r < free_end_ && m.find(r, &to) ? base + to * row_bytes + thread() % kAcross * 16 : nullptr;
             }
         } else {
-            free = free0 + threadIdx.x % kAcross * V, free_end = free_end_;
+            free = free0 + thread() % kAcross * V, free_end = free_end_;
         }
     }
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
@@ -339,7 +344,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
             if constexpr (LAYOUT == kDepthFast) {
-                const uint32_t d = depth0 + threadIdx.x % kAcross * V;
+                const uint32_t d = depth0 + thread() % kAcross * V;
                 reg[p] = fetch_some((const T*)(at[p] + (uint64_t)depth0 * sizeof(T)), at[p] != nullptr && d < depth_end ? (int)(depth_end - d) : 0, end);
             } else {
                 const uint32_t to = source != nullptr ? fdiv(row[p], slots) : row[p];
@@ -353,7 +358,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
         constexpr uint32_t kPitch = LAYOUT == kDepthFast ? kStageBytes : FREE * sizeof(T);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p)
-            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), threadIdx.x % kAcross, kAcross) * 16) = reg[p];
+            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), thread() % kAcross, kAcross) * 16) = reg[p];
     }
 };
 
@@ -381,6 +386,7 @@ template <typename T> __device__ __forceinline__ Vec<T, 8> elements_of(u32x2 cod
 // before it is multiplied, its rows looked up one stage before that.  LOOSE: rows of any length and alignment;
 // else of whole 16-byte chunks that start on 16 bytes.
 template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
+    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr uint32_t kAcross = FREE / 16, kRowsPerFetch = THREADS / kAcross;
     // a stage of few 32-bit columns is less than one fetch: the last threads have nothing to do
@@ -396,9 +402,9 @@ template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
     u32x4 reg[kFetches];
     uint32_t scale[kFetches];
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return threadIdx.x / kAcross + (uint32_t)p * kRowsPerFetch; }
+    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
     __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
-        free = free0 + threadIdx.x % kAcross * 16;
+        free = free0 + thread() % kAcross * 16;
         there = free < free_end && lds_row(0) < kDepth, free_there = (int)(free_end - free);
         codes = (const uint8_t*)m.p, scales = m.scales, source = m.source;
         width = m.width, blocks = (m.width + 31) / 32, slots = m.slots, rows = m.rows;
@@ -426,7 +432,7 @@ template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
         __builtin_amdgcn_sched_barrier(0);      // not before the products: it would wait for the codes there
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
-            const uint32_t d = lds_row(p), c = threadIdx.x % kAcross;
+            const uint32_t d = lds_row(p), c = thread() % kAcross;
             if (kRowsPerFetch > kDepth && d >= kDepth) return;
             char* const at = tile + d * (FREE * sizeof(T));
             const float by = power_of(scale[p]);
@@ -476,6 +482,14 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
     constexpr bool kOrdered = sizeof(T) == 2;
     constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
     if (depth0 >= depth_end) return;
+    uint32_t stages = (depth_end - depth0 + kDepth - 1) / kDepth;
+    if constexpr (S::kGroups > 1) {
+        // every group the same number of stages, since all meet at the barriers: those beyond the end are zeros
+        stages = (stages + S::kGroups - 1) / S::kGroups;
+        depth0 += S::group() * stages * kDepth;
+        depth_end = depth_end - (depth0 < depth_end ? depth0 : depth_end) < stages * kDepth ? depth_end : depth0 + stages * kDepth;
+        lds += S::group() * S::kImages * kImage;
+    }
     fs.start(fast, fast0, fast_end);
     ss.start(slow, slow0, slow_end);
     const auto issue = [&](uint32_t image, uint32_t d) {
@@ -495,7 +509,7 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
         issue(0, depth0);
         look_up(depth0 + kDepth);
         put(0);
-        for (uint32_t d = depth0, image = 0; d < depth_end; d += kDepth, image ^= kImage) {
+        for (uint32_t d = depth0, image = 0; stages > 0; --stages, d += kDepth, image ^= kImage) {
             arrive<0>();
             issue(image ^ kImage, d + kDepth);
             look_up(d + 2 * kDepth);
@@ -519,7 +533,7 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
         uint32_t image = 0;
         Step<T, FL, SL, S> even, odd;
         even.read(lds, 0);
-        for (uint32_t d = depth0; d + kDepth < depth_end; d += kDepth) {
+        for (uint32_t d = depth0; stages > 1; --stages, d += kDepth) {
             odd.read(lds + image, 1);
             even.multiply(acc);
             if constexpr (kOrdered) interleave<kReads, kProducts>();
@@ -542,6 +556,21 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
         odd.multiply(acc);
     }
     arrive<0>();            // nothing travels to LDS when it is used again
+    if constexpr (S::kGroups > 1) {
+        // the sums of the others to the first group, in the groups' order
+        f32x4* const sums = (f32x4*)(lds - S::group() * S::kImages * kImage);
+#pragma unroll
+        for (int g = 1; g < S::kGroups; ++g) {
+            if (S::group() == (uint32_t)g)
+#pragma unroll
+                for (int i = 0; i < S::SI * S::FI; ++i) sums[i * S::kThreads + threadIdx.x % S::kThreads] = acc[i / S::FI][i % S::FI];
+            __syncthreads();
+            if (S::group() == 0)
+#pragma unroll
+                for (int i = 0; i < S::SI * S::FI; ++i) acc[i / S::FI][i % S::FI] += sums[i * S::kThreads + threadIdx.x % S::kThreads];
+            __syncthreads();
+        }
+    }
 }
 
 // Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been
@@ -549,7 +578,8 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
 template <typename O, typename S>
 __device__ __forceinline__ void store_tile(O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end, bool accumulate,
                                            const f32x4 (&acc)[S::SI][S::FI]) {
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+    if (S::group() != 0) return;
+    const uint32_t wave = S::wave(), lane = threadIdx.x & 63u;
     const uint32_t f0 = fast0 + wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
     const uint32_t s0 = slow0 + wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
 #pragma unroll
@@ -584,11 +614,11 @@ __device__ __forceinline__ void rows_of(const int32_t* offsets, uint32_t experts
 template <typename O, typename S>
 __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
                                                 const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
-    constexpr int LDS_BYTES = S::kImages * S::kImage;
+    constexpr int LDS_BYTES = S::kLds;
     constexpr uint32_t kPitch = S::kFast * sizeof(O), kChunks = kPitch / 16, V = 16 / sizeof(O);
     constexpr int kPasses = (S::kSlow * (int)kPitch + LDS_BYTES - 1) / LDS_BYTES, kRows = S::kSlow / kPasses;
     static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow, "whole blocks");
-    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63u;
+    const uint32_t wave = S::wave(), lane = threadIdx.x & 63u;
     const uint32_t f0 = wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
     const uint32_t s0 = wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
 #pragma unroll
@@ -597,7 +627,7 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
 #pragma unroll
         for (int j = 0; j < S::SI; ++j) {
             const uint32_t row = s0 + j * 16 - pass * kRows;
-            if (row < (uint32_t)kRows) {
+            if (row < (uint32_t)kRows && S::group() == 0) {
 #pragma unroll
                 for (int i = 0; i < S::FI; ++i) {
                     const uint32_t at = (f0 + i * 16) * (uint32_t)sizeof(O);
@@ -606,7 +636,7 @@ __device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t strid
             }
         }
         __syncthreads();
-        for (uint32_t id = threadIdx.x; id < kRows * kChunks; id += S::kThreads) {
+        for (uint32_t id = threadIdx.x; id < kRows * kChunks; id += S::kAllThreads) {
             const uint32_t row = id / kChunks, c = id % kChunks, s = slow0 + pass * kRows + row, f = fast0 + c * V;
             if (s >= slow_end) break;
             if (f >= fast_end) continue;
@@ -674,7 +704,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t exper
 // --- kernels ---
 
 template <typename T, int WL, typename S, bool LOOSE>
-__global__ __launch_bounds__(S::kThreads) void expert_product_kernel(const ExpertProductArgs a) {
+__global__ __launch_bounds__(S::kAllThreads) void expert_product_kernel(const ExpertProductArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t across = (a.n + S::kFast - 1) / S::kFast;
     uint32_t bin, row0, row_end, col;
@@ -707,7 +737,7 @@ __device__ __forceinline__ uint32_t by_size(const int32_t* offsets, uint32_t exp
 
 // Experts one after the other; every XCD takes a run of an expert's tiles, whichever experts are large.
 template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE>
-__global__ __launch_bounds__(S::kThreads) void weight_gradient_kernel(const WeightGradientArgs a) {
+__global__ __launch_bounds__(S::kAllThreads) void weight_gradient_kernel(const WeightGradientArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const uint32_t tf = (a.fast.width + S::kFast - 1) / S::kFast, ts = (a.slow.width + S::kSlow - 1) / S::kSlow, run = (tf * ts + kXcds - 1) / kXcds;
     const uint64_t block = long_block();

@@ -6,7 +6,7 @@
 
 namespace tperm {
 
-using TinyTile = TileShape<64, 64, 4, 2, 4>;
+using TinyTile = TileShape<64, 64, 4, 2, 2, 2>;
 using SmallTile = TileShape<128, 128, 4, 2, 2>;
 using WideTile = TileShape<256, 256, 8, 4, 2>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
 
@@ -24,12 +24,12 @@ template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
 }
 
 template <auto KERNEL, typename S, typename A> hipError_t go(uint64_t blocks, const A& a, hipStream_t stream) {
-    constexpr size_t kLds = (size_t)S::kImages * S::kImage;
+    constexpr size_t kLds = S::kLds;
     if constexpr (kLds > 64 * 1024) {
         const hipError_t e = allow_lds<KERNEL>(kLds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(KERNEL, long_grid(blocks), dim3(S::kThreads), kLds, stream, a);
+    hipLaunchKernelGGL(KERNEL, long_grid(blocks), dim3(S::kAllThreads), kLds, stream, a);
     return hipGetLastError();
 }
 
