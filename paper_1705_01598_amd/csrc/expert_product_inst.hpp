@@ -8,6 +8,7 @@ namespace tperm {
 
 using TinyTile = TileShape<64, 64, 4, 2, 2, 2>;
 using SmallTile = TileShape<128, 128, 4, 2, 2>;
+using NarrowTile = TileShape<128, 64, 4, 2, 2>;    // 32-bit elements, which the matrix cores bound: finer rounds of tiles
 using WideTile = TileShape<256, 256, 8, 4, 2>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
 
 // Workgroups with more than 64 KiB of LDS have to be allowed it, once on each device.
@@ -53,9 +54,14 @@ template <typename T, bool LOOSE> hipError_t product_with(const ExpertProductArg
     //   64 experts 2048 x 1024, one row: 24 with 128, 19 with 64; 16 rows 60, 56
     const uint64_t rows = over(a.rows, a.experts);
     const auto tiles = [&](uint64_t side) { return over(rows, side) * a.experts * over(a.n, side); };
-    if constexpr (sizeof(T) == 2)
+    //   f32, 8 experts 1024 x 1024, tiles of 128, 128 x 64, 64: 1024 rows 203 178 172, 4096 rows 559 555 572;
+    //   701 x 903: 750 rows 125 142 108
+    if constexpr (sizeof(T) == 2) {
         if (rows >= 192 && tiles(256) >= 128) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
-    if (rows >= 64 && tiles(128) >= 128) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
+        if (rows >= 64 && tiles(128) >= 128) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
+    } else {
+        if (rows >= 64 && tiles(128) >= 512) return product_tiles<T, NarrowTile, LOOSE>(a, w_k_first, stream);
+    }
     return product_tiles<T, TinyTile, LOOSE>(a, w_k_first, stream);
 }
 
@@ -78,10 +84,14 @@ template <typename T, typename S, bool LOOSE> hipError_t gradient_tiles(const We
 template <typename T, bool LOOSE> hipError_t gradient_with(const WeightGradientArgs& a, hipStream_t stream) {
     const auto tiles = [&](uint64_t side) { return over(a.fast.width, side) * over(a.slow.width, side) * a.experts; };
     // As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 79 49 71,
-    // 2048 x 2048 (512) 104 117 270
-    if constexpr (sizeof(T) == 2)
+    // 2048 x 2048 (512) 104 117 270; f32, 8 experts 1024 x 1024 (512 of 128), 128, 128 x 64, 64: 232 149 155
+    if constexpr (sizeof(T) == 2) {
         if (tiles(256) >= 192) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
-    return tiles(128) >= 256 ? gradient_tiles<T, SmallTile, LOOSE>(a, stream) : gradient_tiles<T, TinyTile, LOOSE>(a, stream);
+        if (tiles(128) >= 256) return gradient_tiles<T, SmallTile, LOOSE>(a, stream);
+    } else {
+        if (tiles(128) >= 512) return gradient_tiles<T, NarrowTile, LOOSE>(a, stream);
+    }
+    return gradient_tiles<T, TinyTile, LOOSE>(a, stream);
 }
 
 template <typename T> hipError_t gradient_of(const WeightGradientArgs& a, hipStream_t stream) {
