@@ -62,7 +62,7 @@ typedef enum {
  * looked at for up to TPERM_EXPERT_SORT_ONE_BLOCK assignments. */
 #define TPERM_EXPERT_SORT_ONE_BLOCK 8192
 #define TPERM_EXPERT_SORT_WORKSPACE_BYTES(rows, experts) \
-    ((rows) <= TPERM_EXPERT_SORT_ONE_BLOCK ? (size_t)0 : (size_t)256 * ((size_t)(experts) + 1) * 4)
+    ((rows) <= TPERM_EXPERT_SORT_ONE_BLOCK ? (size_t)0 : (size_t)128 * ((size_t)(experts) + 1) * 4)
 tperm_status_t tperm_expert_sort(const int32_t *expert, int64_t tokens, int64_t slots, int64_t experts,
                                  int32_t *offsets, int32_t *source, int32_t *place, void *workspace,
                                  size_t workspace_bytes, void *hip_stream);

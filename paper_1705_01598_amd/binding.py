@@ -485,7 +485,7 @@ EXPERT_SORT_ONE_BLOCK = 8192
 
 def expert_sort_workspace_bytes(rows: int, experts: int) -> int:
     """TPERM_EXPERT_SORT_WORKSPACE_BYTES of the header."""
-    return 0 if rows <= EXPERT_SORT_ONE_BLOCK else 256 * (int(experts) + 1) * 4
+    return 0 if rows <= EXPERT_SORT_ONE_BLOCK else 128 * (int(experts) + 1) * 4
 
 
 def checkpoint_blocks(width: int) -> int:

@@ -15,6 +15,7 @@ namespace {
 constexpr uint32_t kPieces = 128;       // workgroups of a large sort at most: with 256 each reads twice the counts, with 64 it
                                         // places twice the rows (524288 assignments: 16.8 us, 20.0, 18.4)
 constexpr uint32_t kLeast = 2048;       // assignments of a piece at least
+static_assert(TPERM_EXPERT_SORT_WORKSPACE_BYTES(1 << 20, 7) == kPieces * 8 * 4, "a count for every piece and bin");
 
 // Assignments that name no expert count as one more expert.
 __device__ __forceinline__ uint32_t bin_of(int32_t expert, uint32_t experts) { return (uint32_t)expert < experts ? (uint32_t)expert : experts; }

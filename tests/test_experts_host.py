@@ -112,7 +112,7 @@ def test_types_alignment_and_overlap(name):
 def test_sort_asks_for_its_workspace():
     many = dict(CALLS["tperm_expert_sort"], tokens=B.EXPERT_SORT_ONE_BLOCK, slots=2)
     need = B.expert_sort_workspace_bytes(2 * B.EXPERT_SORT_ONE_BLOCK, 3)
-    assert need == 256 * 4 * 4 and B.expert_sort_workspace_bytes(B.EXPERT_SORT_ONE_BLOCK, 3) == 0
+    assert need == 128 * 4 * 4 and B.expert_sort_workspace_bytes(B.EXPERT_SORT_ONE_BLOCK, 3) == 0
     for ws, status in ((dict(), B.ERR_NULL), (dict(workspace_ptr=_at(5), workspace_bytes=need - 1), B.ERR_TOO_LARGE),
                        (dict(workspace_ptr=_at(5) + 2, workspace_bytes=need), B.ERR_ALIGN), (dict(workspace_ptr=_at(0), workspace_bytes=need), B.ERR_ALIAS)):
         with pytest.raises(B.TpermError) as e:
