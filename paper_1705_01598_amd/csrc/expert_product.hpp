@@ -491,7 +491,7 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
         lds += S::group() * S::kImages * kImage;
     }
     fs.start(fast, fast0, fast_end);
-    ss.start(slow, slow0, slow_end);
+    if constexpr (LOOSE || FL == kCodes || SL == kCodes || SM) ss.start(slow, slow0, slow_end);
     const auto issue = [&](uint32_t image, uint32_t d) {
         fs.issue(lds + image, d, depth_end);
         ss.issue(lds + image + S::kFast * kStageBytes, d, depth_end);
@@ -524,8 +524,13 @@ __device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_
     } else {
         constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;     // of a stage
         look_up(depth0);
+        // the fast side's first stage travels while the slow side's rows are looked up
+        fs.issue(lds, depth0, depth_end);
+        if constexpr (!SM) ss.start(slow, slow0, slow_end);
+        ss.issue(lds + S::kFast * kStageBytes, depth0, depth_end);
+        look_up(depth0 + kDepth);
 #pragma unroll
-        for (int i = 0; i < S::kImages; ++i) {
+        for (int i = 1; i < S::kImages; ++i) {
             issue(i * kImage, depth0 + i * kDepth);
             look_up(depth0 + (i + 1) * kDepth);
         }
@@ -667,7 +672,7 @@ template <uint32_t kGroup> __device__ __forceinline__ void grouped(uint32_t at, 
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t height, uint32_t across,
                                           uint32_t* bin, uint32_t* from, uint32_t* end, uint32_t* col) {
     const uint32_t lane = threadIdx.x & 63u, bins = experts + 1, per = (bins + 63) / 64;
-    uint32_t n = 0, o, p;
+    uint32_t n = 0, o = 0, p = 0;
     for (uint32_t i = 0; i < per; ++i)
         if (lane * per + i < bins) {
             rows_of(offsets, experts, rows, lane * per + i, &o, &p);
@@ -685,20 +690,25 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t exper
     if (at == 0) return false;
     const int l = __builtin_ctzll(at);
     uint32_t left = index - (uint32_t)__builtin_amdgcn_readlane((int)(sum - n), l) * across;
-    for (uint32_t b = (uint32_t)l * per; b < bins; ++b) {
-        rows_of(offsets, experts, rows, b, &o, &p);
-        const uint32_t down = (p - o + height - 1) / height;
-        if (left < down * across) {
-            uint32_t row;
-            grouped<8>(left, down, across, &row, col);
-            *bin = b;
-            *from = o + row * height;
-            *end = p - *from < height ? p : *from + height;
-            return true;
+    uint32_t b = (uint32_t)l * per, down;
+    if (per == 1) {         // the lane has the bin's rows
+        o = (uint32_t)__builtin_amdgcn_readlane((int)o, l), p = (uint32_t)__builtin_amdgcn_readlane((int)p, l);
+        down = (p - o + height - 1) / height;
+    } else {
+        for (;; ++b) {
+            if (b >= bins) return false;
+            rows_of(offsets, experts, rows, b, &o, &p);
+            down = (p - o + height - 1) / height;
+            if (left < down * across) break;
+            left -= down * across;
         }
-        left -= down * across;
     }
-    return false;
+    uint32_t row;
+    grouped<8>(left, down, across, &row, col);
+    *bin = b;
+    *from = o + row * height;
+    *end = p - *from < height ? p : *from + height;
+    return true;
 }
 
 // --- kernels ---
@@ -721,18 +731,18 @@ __global__ __launch_bounds__(S::kAllThreads) void expert_product_kernel(const Ex
 
 // The i-th expert by number of rows, most first (equal ones in their order), for up to 64 experts: every lane counts how many
 // come before its own.  Tiles of large experts that start last would leave the chip idle around them.
-__device__ __forceinline__ uint32_t by_size(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t i) {
+__device__ __forceinline__ uint32_t by_size(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t i, uint32_t* first, uint32_t* behind) {
     const uint32_t lane = threadIdx.x & 63u;
-    uint32_t from, end, size = 0, rank = 0;
-    if (lane < experts) {
-        rows_of(offsets, experts, rows, lane, &from, &end);
-        size = end - from;
-    }
+    uint32_t from = 0, end = 0, rank = 0;
+    if (lane < experts) rows_of(offsets, experts, rows, lane, &from, &end);
+    const uint32_t size = end - from;
     for (uint32_t e = 0; e < experts; ++e) {
         const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)size, (int)e);
         rank += other > size || (other == size && e < lane) ? 1u : 0u;
     }
-    return (uint32_t)__builtin_ctzll(__ballot(lane < experts && rank == i));
+    const int expert = __builtin_ctzll(__ballot(lane < experts && rank == i));
+    *first = (uint32_t)__builtin_amdgcn_readlane((int)from, expert), *behind = (uint32_t)__builtin_amdgcn_readlane((int)end, expert);
+    return (uint32_t)expert;
 }
 
 // Experts one after the other; every XCD takes a run of an expert's tiles, whichever experts are large.
@@ -743,12 +753,12 @@ __global__ __launch_bounds__(S::kAllThreads) void weight_gradient_kernel(const W
     const uint64_t block = long_block();
     const uint32_t i = (uint32_t)(block / kXcds), turn = i / run, tile = ((uint32_t)(block % kXcds) + turn) % kXcds * run + i % run;
     if (turn >= a.experts || tile >= tf * ts) return;
-    const uint32_t expert = a.experts <= 64 ? by_size(a.offsets, a.experts, a.rows, turn) : turn;
+    uint32_t expert = turn, from, end;
+    if (a.experts <= 64) expert = by_size(a.offsets, a.experts, a.rows, turn, &from, &end);
+    else rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
     uint32_t fi, si;
     grouped<4>(tile, ts, tf, &si, &fi);
     const uint32_t f0 = fi * S::kFast, s0 = si * S::kSlow;
-    uint32_t from, end;
-    rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
     f32x4 acc[S::SI][S::FI] = {};
     sum_tile<T, FL, SL, FM, SM, S, LOOSE>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
     const int64_t at = (int64_t)expert * a.fast.width * a.slow.width;

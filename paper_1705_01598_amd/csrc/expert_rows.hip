@@ -7,10 +7,13 @@
 // Results are stored past the caches (rows of 4 KiB: gather of 16384 x 2 50 -> 39 us, backward of 2048 x 4 of 8 KiB
 // 36 -> 25 us); rows are read past them (ONCE) where they fill half of the memory-side cache (combine of 16384 x 2
 // 53 -> 43 us), while smaller ones may still be there from the product that wrote them (2048 x 4 of 8 KiB 15 -> 19 us).
+// Rows of 4 KiB now: combine of 8192 x 8 50 us, 5.9 TB/s, its backward 105 us, 5.4 TB/s, both near what a copy
+// reaches (6.1); gather 74 us, 4.1 TB/s, where a token's row is read eight times, from the memory-side cache.
 #include <type_traits>
 
 #include "experts.hpp"
 #include "expert_vector.hpp"
+#include "plan.hpp"
 
 namespace tperm {
 
@@ -18,14 +21,24 @@ namespace {
 
 constexpr int kRowThreads = 256;
 
-// LANES lanes to a row, STEPS vectors a lane: a workgroup takes kRowThreads / LANES rows and one piece of
-// LANES * STEPS vectors of them.
+// Which row (or token) a group of LANES lanes works on, and which piece of it: the pieces of a row side by side,
+// so that a row is read and written at once (combine, rows of 4 KiB, against all first pieces before all second ones:
+// 8192 x 8 67 -> 51 us, 16384 x 2 46 -> 37 us).
+template <int LANES> __device__ __forceinline__ uint64_t row_of_group(const RowsArgs& a, uint32_t* piece) {
+    const uint64_t at = long_block() * (kRowThreads / LANES) + threadIdx.x / LANES;
+    const uint64_t row = a.by_pieces.magic != 0 ? fdiv((uint32_t)at, a.by_pieces) : at / a.pieces;
+    *piece = (uint32_t)(at - row * a.pieces);
+    return row;
+}
+
+// LANES lanes to a piece of a row, STEPS vectors a lane.
 template <typename T, int LANES, int STEPS, bool ALIGNED>
 __global__ __launch_bounds__(kRowThreads) void gather_kernel(const RowsArgs a) {
     constexpr int V = 16 / sizeof(T);
-    const uint64_t row = long_block() * (kRowThreads / LANES) + threadIdx.x / LANES;
+    uint32_t piece;
+    const uint64_t row = row_of_group<LANES>(a, &piece);
     if (row >= a.count) return;
-    const uint32_t col = (blockIdx.y * (LANES * STEPS) + threadIdx.x % LANES) * V;
+    const uint32_t col = (piece * (LANES * STEPS) + threadIdx.x % LANES) * V;
     const uint32_t from = (uint32_t)a.map[row];
     const bool used = row < (uint32_t)*a.used && from < a.count;
     const T* const x = (const T*)a.in + (int64_t)(used ? from / a.slots : 0u) * a.in_stride;
@@ -64,10 +77,11 @@ template <int LANES> __device__ __forceinline__ uint32_t uniform(uint32_t v) {
 template <typename T, int LANES, int SLOTS, bool ALIGNED, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void combine_kernel(const RowsArgs a) {
     constexpr int V = 16 / sizeof(T);
-    const uint64_t at = long_block() * (kRowThreads / LANES) + threadIdx.x / LANES;
+    uint32_t piece;
+    const uint64_t at = row_of_group<LANES>(a, &piece);
     if (at >= a.tokens) return;
     const uint32_t token = uniform<LANES>((uint32_t)at);
-    const uint32_t col = (blockIdx.y * LANES + threadIdx.x % LANES) * V;
+    const uint32_t col = (piece * LANES + threadIdx.x % LANES) * V;
     if (col >= a.width) return;
     const int there = (int)(a.width - col);
     const uint32_t end = (uint32_t)*a.used < a.count ? (uint32_t)*a.used : a.count;
@@ -180,9 +194,13 @@ bool on_vectors(size_t elem, uint32_t width, const void* p, int64_t stride) {
     return (width * elem) % 16 == 0 && ((uintptr_t)p | (uintptr_t)stride * elem) % 16 == 0;
 }
 
-template <int LANES> dim3 grid_of(uint32_t rows, uint32_t vectors, uint32_t steps) {
-    const uint32_t per = kRowThreads / LANES;
-    return long_grid(((uint64_t)rows + per - 1) / per, (vectors + LANES * steps - 1) / (LANES * steps));
+// Grid for rows in pieces of LANES * steps vectors.
+template <int LANES> dim3 grid_of(RowsArgs* a, uint32_t rows, uint32_t vectors, uint32_t steps) {
+    constexpr uint32_t kPer = kRowThreads / LANES;
+    a->pieces = (vectors + LANES * steps - 1) / (LANES * steps);
+    const uint64_t blocks = ((uint64_t)rows * a->pieces + kPer - 1) / kPer;
+    a->by_pieces = blocks * kPer < 1ull << 31 ? make_fastdiv(a->pieces) : FastDiv{0, 0};
+    return long_grid(blocks);
 }
 
 }  // namespace
@@ -196,9 +214,9 @@ hipError_t launch_expert_gather(RowsArgs a, int type, hipStream_t stream) {
             hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, a);
             return hipGetLastError();
         };
-        if (vectors <= 8) return aligned ? go(gather_kernel<T, 4, 2, true>, grid_of<4>(a.count, vectors, 2)) : go(gather_kernel<T, 4, 2, false>, grid_of<4>(a.count, vectors, 2));
-        if (vectors <= 64) return aligned ? go(gather_kernel<T, 16, 4, true>, grid_of<16>(a.count, vectors, 4)) : go(gather_kernel<T, 16, 4, false>, grid_of<16>(a.count, vectors, 4));
-        return aligned ? go(gather_kernel<T, 64, 4, true>, grid_of<64>(a.count, vectors, 4)) : go(gather_kernel<T, 64, 4, false>, grid_of<64>(a.count, vectors, 4));
+        if (vectors <= 8) return aligned ? go(gather_kernel<T, 4, 2, true>, grid_of<4>(&a, a.count, vectors, 2)) : go(gather_kernel<T, 4, 2, false>, grid_of<4>(&a, a.count, vectors, 2));
+        if (vectors <= 64) return aligned ? go(gather_kernel<T, 16, 4, true>, grid_of<16>(&a, a.count, vectors, 4)) : go(gather_kernel<T, 16, 4, false>, grid_of<16>(&a, a.count, vectors, 4));
+        return aligned ? go(gather_kernel<T, 64, 4, true>, grid_of<64>(&a, a.count, vectors, 4)) : go(gather_kernel<T, 64, 4, false>, grid_of<64>(&a, a.count, vectors, 4));
     });
 }
 
@@ -227,9 +245,9 @@ hipError_t launch_expert_combine(RowsArgs a, int type, hipStream_t stream) {
                 hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, a);
                 return hipGetLastError();
             };
-            if (vectors <= 4) return aligned ? go(combine_kernel<T, 4, N, true, false>, grid_of<4>(a.tokens, vectors, 1)) : go(combine_kernel<T, 4, N, false, false>, grid_of<4>(a.tokens, vectors, 1));
-            if (vectors <= 32) return aligned ? go(combine_kernel<T, 16, N, true, false>, grid_of<16>(a.tokens, vectors, 1)) : go(combine_kernel<T, 16, N, false, false>, grid_of<16>(a.tokens, vectors, 1));
-            const dim3 grid = grid_of<64>(a.tokens, vectors, 1);
+            if (vectors <= 4) return aligned ? go(combine_kernel<T, 4, N, true, false>, grid_of<4>(&a, a.tokens, vectors, 1)) : go(combine_kernel<T, 4, N, false, false>, grid_of<4>(&a, a.tokens, vectors, 1));
+            if (vectors <= 32) return aligned ? go(combine_kernel<T, 16, N, true, false>, grid_of<16>(&a, a.tokens, vectors, 1)) : go(combine_kernel<T, 16, N, false, false>, grid_of<16>(&a, a.tokens, vectors, 1));
+            const dim3 grid = grid_of<64>(&a, a.tokens, vectors, 1);
             return !aligned ? go(combine_kernel<T, 64, N, false, false>, grid) : read_once(a, sizeof(T)) ? go(combine_kernel<T, 64, N, true, true>, grid) : go(combine_kernel<T, 64, N, true, false>, grid);
         });
     });

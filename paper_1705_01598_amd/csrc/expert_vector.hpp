@@ -111,12 +111,12 @@ __device__ __forceinline__ uint32_t finite_magnitude(float v) {
 }
 
 // A launch has fewer than 2^32 threads along each dimension of its grid: more workgroups than kRow go on along
-// the third.
+// the second.
 constexpr uint32_t kRow = 1u << 22;
-inline dim3 long_grid(uint64_t blocks, uint32_t y = 1) {
-    return blocks <= kRow ? dim3((uint32_t)blocks, y, 1) : dim3(kRow, y, (uint32_t)((blocks + kRow - 1) / kRow));
+inline dim3 long_grid(uint64_t blocks) {
+    return blocks <= kRow ? dim3((uint32_t)blocks) : dim3(kRow, (uint32_t)((blocks + kRow - 1) / kRow));
 }
-__device__ __forceinline__ uint64_t long_block() { return blockIdx.x + (uint64_t)kRow * blockIdx.z; }
+__device__ __forceinline__ uint64_t long_block() { return blockIdx.x + (uint64_t)kRow * blockIdx.y; }
 
 // Calls f with the element type behind a tperm_type_t.
 template <typename F> inline auto with_type(int type, F f) {

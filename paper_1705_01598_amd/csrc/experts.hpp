@@ -25,6 +25,8 @@ struct RowsArgs {
     const float* weights;
     int64_t in_stride, rows_stride, out_stride;
     uint32_t tokens, slots, count, width;   // count = tokens * slots
+    uint32_t pieces;            // of a row, one to a group of lanes (this and the next set by the launcher)
+    FastDiv by_pieces;          // for group numbers below 2^31, else magic 0
 };
 hipError_t launch_expert_gather(RowsArgs a, int type, hipStream_t stream);
 hipError_t launch_expert_combine(RowsArgs a, int type, hipStream_t stream);
