@@ -20,6 +20,10 @@ constexpr int kStageBytes = 128;                            // depth of a stage 
 
 #define TPERM_LDS __attribute__((address_space(3)))
 
+// A value that all lanes have, in a scalar register.  Left in a vector register, where a load may leave it, it makes
+// branches of lanes of what follows from it, and buffers that are read in a loop over the lanes.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 // --- fragments ---
 
 template <typename T> struct Matrix;   // the matrix instruction of a type: kDepth summed indices of 16 x 16 results
@@ -50,10 +54,10 @@ template <typename T, int LAYOUT> __device__ __forceinline__ uint32_t swizzle(ui
     else return c ^ ((row & 12u) & (chunks - 1));
 }
 
-// Fragment of 16 free indices from `free` on, step `kk` of the stage: lane l holds free index l % 16 and the
+// Fragment of 16 free indices from `free` on, step `kk` of the stage: lane l (`lane`) holds free index l % 16 and the
 // depth of its quarter l / 16.
-template <typename T, int LAYOUT, int FREE> __device__ __forceinline__ Frag<T> fragment(const char* tile, uint32_t free, uint32_t kk) {
-    const uint32_t lane = threadIdx.x & 63u, q = lane >> 4, i = lane & 15u;
+template <typename T, int LAYOUT, int FREE> __device__ __forceinline__ Frag<T> fragment(const char* tile, uint32_t free, uint32_t kk, uint32_t lane) {
+    const uint32_t q = lane >> 4, i = lane & 15u;
     if constexpr (LAYOUT == kDepthFast) {
         const uint32_t f = free + i;
         return *(const Frag<T>*)(tile + f * kStageBytes + swizzle<T, LAYOUT>(f, kk * 4 + q, 8) * 16);
@@ -104,13 +108,13 @@ struct Operand {
     }
 };
 
-// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side, IMAGES stages in LDS.  GROUPS
-// such sets of wavefronts and images each take a piece of the depth; their sums are joined in order.
-template <int FAST_, int SLOW_, int WAVES, int WF_, int IMAGES, int GROUPS = 1> struct TileShape {
-    static constexpr int kImages = IMAGES, kImage = (FAST_ + SLOW_) * kStageBytes, kGroups = GROUPS, kLds = GROUPS * IMAGES * kImage;
+// A workgroup's tile: FAST x SLOW results, WAVES wavefronts, WF of them along the fast side, two images of a stage in LDS.
+// GROUPS such sets of wavefronts and images each take a piece of the depth; their sums are joined in order.
+template <int FAST_, int SLOW_, int WAVES, int WF_, int GROUPS = 1> struct TileShape {
+    static constexpr int kImage = (FAST_ + SLOW_) * kStageBytes, kGroups = GROUPS, kLds = 2 * GROUPS * kImage;
     static constexpr int kFast = FAST_, kSlow = SLOW_, kThreads = WAVES * 64, kAllThreads = GROUPS * kThreads;     // kThreads: of a group
-    static __device__ __forceinline__ uint32_t wave() { return threadIdx.x % kThreads >> 6; }
-    static __device__ __forceinline__ uint32_t group() { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kThreads)); }
+    static __device__ __forceinline__ uint32_t wave(uint32_t thread) { return thread % kThreads >> 6; }
+    static __device__ __forceinline__ uint32_t group() { return uniform(threadIdx.x / kThreads); }
     static constexpr int kWavesFast = WF_, kWavesSlow = WAVES / WF_;
     static constexpr int FI = FAST_ / kWavesFast / 16, SI = SLOW_ / kWavesSlow / 16;   // 16 x 16 blocks of a wavefront
 };
@@ -121,26 +125,26 @@ constexpr uint32_t kSteps = 2;      // steps of a stage, whatever the type
 template <typename T, int FL, int SL, typename S> struct Step {
     static_assert(kStageBytes / sizeof(T) == kSteps * Matrix<T>::kDepth, "two steps");
     Frag<T> f[S::FI], s[S::SI];
-    __device__ __forceinline__ void read(const char* image, uint32_t kk) {
-        const uint32_t wave = S::wave();
+    __device__ __forceinline__ void read(uint32_t thread, const char* image, uint32_t kk) {
+        const uint32_t wave = S::wave(thread), lane = thread & 63u;
         const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
 #pragma unroll
-        for (int i = 0; i < S::SI; ++i) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk);
+        for (int i = 0; i < S::SI; ++i) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk, lane);
 #pragma unroll
-        for (int i = 0; i < S::FI; ++i) f[i] = fragment<T, FL, S::kFast>(image, wf + i * 16, kk);
+        for (int i = 0; i < S::FI; ++i) f[i] = fragment<T, FL, S::kFast>(image, wf + i * 16, kk, lane);
     }
     __device__ __forceinline__ void multiply(f32x4 (&acc)[S::SI][S::FI]) const {
 #pragma unroll
         for (int i = 0; i < S::FI; ++i) multiply(acc, i);
     }
     // The i-th of FI parts of either.
-    __device__ __forceinline__ void read(const char* image, uint32_t kk, int part) {
-        const uint32_t wave = S::wave();
+    __device__ __forceinline__ void read(uint32_t thread, const char* image, uint32_t kk, int part) {
+        const uint32_t wave = S::wave(thread), lane = thread & 63u;
         const uint32_t wf = wave % S::kWavesFast * (S::FI * 16), ws = wave / S::kWavesFast * (S::SI * 16);
 #pragma unroll
         for (int i = 0; i < S::SI; ++i)
-            if (i * S::FI / S::SI == part) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk);
-        f[part] = fragment<T, FL, S::kFast>(image, wf + part * 16, kk);
+            if (i * S::FI / S::SI == part) s[i] = fragment<T, SL, S::kSlow>(image + S::kFast * kStageBytes, ws + i * 16, kk, lane);
+        f[part] = fragment<T, FL, S::kFast>(image, wf + part * 16, kk, lane);
     }
     __device__ __forceinline__ void multiply(f32x4 (&acc)[S::SI][S::FI], int i) const {
 #pragma unroll
@@ -152,14 +156,17 @@ template <typename T, int FL, int SL, typename S> struct Step {
 
 constexpr uint32_t kBeyond = 0xFFFFFF00u;   // lane offset behind every buffer: the access writes zeros to LDS
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)kBeyond, 0x00020000); }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
+    const uint64_t at = (uint64_t)p, same = (uint64_t)uniform((uint32_t)(at >> 32)) << 32 | uniform((uint32_t)at);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)same, 0, (int)kBeyond, 0x00020000);
+}
 
 // 16 bytes a lane from base + offset + scalar to 1 KiB of LDS from `to` on.  Written out: behind the builtin the
 // compiler lets the next transposing read, of another image, wait for all loads (2.1 us a stage instead of 1.4).  It
 // has no result for the compiler to see; arrive() waits for it.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t to, uint32_t offset, uint32_t scalar) {
     const uint64_t p = (uint64_t)base;
-    const u32x4 buffer = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xFFFFu, kBeyond, 0x00020000u};
+    const u32x4 buffer = {uniform((uint32_t)p), uniform((uint32_t)(p >> 32)) & 0xFFFFu, kBeyond, 0x00020000u};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(buffer), "s"(scalar));
 }
 
@@ -174,7 +181,7 @@ template <int LOADS> __device__ __forceinline__ void arrive() {
 // The operand of one side.  A lane's 16 bytes arrive at a place in LDS that its number fixes, so the swizzle is
 // applied to where it reads.  MAPPED: depth rows (kFreeFast) are found through source, one stage ahead.
 template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Direct {
-    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
+    uint32_t me;        // of THREADS
     static constexpr int V = 16 / sizeof(T);
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
@@ -193,11 +200,12 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     FastDiv slots;
     uint32_t rows;
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
-    static __device__ __forceinline__ uint32_t chunk(int p) { return swizzle<T, LAYOUT>(lds_row(p), thread() % kAcross, kAcross); }
+    __device__ __forceinline__ uint32_t lds_row(int p) const { return me / kAcross + (uint32_t)p * kRowsPerFetch; }
+    __device__ __forceinline__ uint32_t chunk(int p) const { return swizzle<T, LAYOUT>(lds_row(p), me % kAcross, kAcross); }
 
     // Depth-fast: rows free0 .. free_end of m, whose row r is m.find(r).
-    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
+    __device__ __forceinline__ void start(uint32_t thread, const Operand& m, uint32_t free0, uint32_t free_end) {
+        me = thread % THREADS;
         row_bytes = (uint32_t)(m.stride * sizeof(T));
         source = m.source, slots = m.slots, rows = m.rows;
         if constexpr (LAYOUT == kDepthFast) {
@@ -227,7 +235,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             }
         } else if constexpr (MAPPED) {
             typedef const __attribute__((address_space(4))) int32_t* Scalar;
-            const uint32_t first = depth0 + (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread() >> 6)) * kRowsPerWave;
+            const uint32_t first = depth0 + uniform(me >> 6) * kRowsPerWave;
 #pragma unroll
             for (int p = 0; p < kFetches; ++p)
 #pragma unroll
@@ -237,9 +245,16 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
                 }
         }
     }
+    // Looked-up entries are here from now on.  The compiler does not see load_to_lds(): left to it, the waits for the
+    // entries come between a stage's loads and wait for those too (2048 rows of 8 experts 34 us instead of 25).
+    __device__ __forceinline__ void looked_up() const {
+        if constexpr (MAPPED && !kScalar)
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) asm volatile("" ::"v"(row[p][0]));
+    }
     __device__ __forceinline__ void issue(char* tile, uint32_t depth0, uint32_t depth_end, int part = 0, int parts = 1) {
         const uint32_t left = depth0 < depth_end ? depth_end - depth0 : 0;      // beyond the end: zeros
-        const uint32_t to = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (thread() & ~63u) * 16));
+        const uint32_t to = uniform((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (me & ~63u) * 16);
         const char* from = base;
         uint32_t scalar = 0;
         if constexpr (LAYOUT == kDepthFast) scalar = depth0 * (uint32_t)sizeof(T);
@@ -252,15 +267,17 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
                 if (left < kDepth) o = chunk(p) * V < left ? o : kBeyond;
             } else if constexpr (MAPPED && !kScalar) {
                 const uint32_t at = fdiv(row[p][0], slots);
-                o = lds_row(p) < left && row[p][0] < 1u << 31 && at < rows && o != kBeyond ? at * row_bytes + o : kBeyond;
+                const bool use = (lds_row(p) < left) & (row[p][0] < 1u << 31) & (at < rows) & (o != kBeyond);     // without branches
+                o = use ? at * row_bytes + o : kBeyond;
             } else if constexpr (MAPPED) {
-                const uint32_t in_wave = (thread() & 63u) / kAcross;
+                const uint32_t in_wave = (me & 63u) / kAcross;
                 uint32_t start = 0;
 #pragma unroll
                 for (int i = 0; i < kRowsPerWave; ++i) {
                     const uint32_t at = fdiv(row[p][i], slots);
-                    const uint32_t d = (uint32_t)__builtin_amdgcn_readfirstlane((int)(thread() >> 6)) * kRowsPerWave + p * kRowsPerFetch + i;
-                    const uint32_t one = d < left && row[p][i] < 1u << 31 && at < rows ? at * row_bytes : kBeyond;
+                    const uint32_t d = uniform(me >> 6) * kRowsPerWave + p * kRowsPerFetch + i;
+                    const bool use = (d < left) & (row[p][i] < 1u << 31) & (at < rows);
+                    const uint32_t one = use ? at * row_bytes : kBeyond;
                     start = in_wave == (uint32_t)i ? one : start;
                 }
                 o = __builtin_elementwise_add_sat(start, o);     // kBeyond and more stays behind the buffer
@@ -301,7 +318,7 @@ template <typename E> __device__ __forceinline__ u32x4 fetch_some(const E* q, in
 // The operand of one side, of any size, stride and alignment, by way of registers: requested while the stage before is
 // multiplied, put to LDS behind that.
 template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
-    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
+    uint32_t me;        // of THREADS
     static constexpr int V = 16 / sizeof(T);
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr int kFetches = FREE * kStageBytes / 16 / THREADS;
@@ -317,8 +334,9 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
     uint32_t rows, free, free_end;
     u32x4 reg[kFetches];
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
-    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end_) {
+    __device__ __forceinline__ uint32_t lds_row(int p) const { return me / kAcross + (uint32_t)p * kRowsPerFetch; }
+    __device__ __forceinline__ void start(uint32_t thread, const Operand& m, uint32_t free0, uint32_t free_end_) {
+        me = thread % THREADS;
         base = (const char*)m.p, row_bytes = m.stride * (int64_t)sizeof(T);
         end = base + ((int64_t)m.rows - 1) * row_bytes + (int64_t)m.width * (int64_t)sizeof(T);
         source = m.source, slots = m.slots, rows = m.rows;
@@ -326,10 +344,10 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) {
                 uint32_t r = free0 + lds_row(p), to;
-                at[p] = r < free_end_ && m.find(r, &to) ? base + to * row_bytes + thread() % kAcross * 16 : nullptr;
+                at[p] = r < free_end_ && m.find(r, &to) ? base + to * row_bytes + me % kAcross * 16 : nullptr;
             }
         } else {
-            free = free0 + thread() % kAcross * V, free_end = free_end_;
+            free = free0 + me % kAcross * V, free_end = free_end_;
         }
     }
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
@@ -340,11 +358,12 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
                 row[p] = d >= depth_end ? 0xFFFFFFFFu : source != nullptr ? (uint32_t)source[d] : d;
             }
     }
+    __device__ __forceinline__ void looked_up() const {}
     __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
             if constexpr (LAYOUT == kDepthFast) {
-                const uint32_t d = depth0 + thread() % kAcross * V;
+                const uint32_t d = depth0 + me % kAcross * V;
                 reg[p] = fetch_some((const T*)(at[p] + (uint64_t)depth0 * sizeof(T)), at[p] != nullptr && d < depth_end ? (int)(depth_end - d) : 0, end);
             } else {
                 const uint32_t to = source != nullptr ? fdiv(row[p], slots) : row[p];
@@ -358,7 +377,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
         constexpr uint32_t kPitch = LAYOUT == kDepthFast ? kStageBytes : FREE * sizeof(T);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p)
-            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), thread() % kAcross, kAcross) * 16) = reg[p];
+            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), me % kAcross, kAcross) * 16) = reg[p];
     }
 };
 
@@ -385,8 +404,8 @@ template <typename T> __device__ __forceinline__ Vec<T, 8> elements_of(u32x2 cod
 // The operand of one side kept in codes: through registers, where codes become elements.  A stage is fetched while the one
 // before it is multiplied, its rows looked up one stage before that.  LOOSE: rows of any length and alignment;
 // else of whole 16-byte chunks that start on 16 bytes.
-template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
-    static __device__ __forceinline__ uint32_t thread() { return threadIdx.x % THREADS; }
+template <typename T, int FREE, int THREADS, bool MAPPED, bool LOOSE> struct Coded {
+    uint32_t me;        // of THREADS
     static constexpr uint32_t kDepth = kStageBytes / sizeof(T);
     static constexpr uint32_t kAcross = FREE / 16, kRowsPerFetch = THREADS / kAcross;
     // a stage of few 32-bit columns is less than one fetch: the last threads have nothing to do
@@ -398,33 +417,40 @@ template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
     int free_there;
     FastDiv slots;
     bool there;
-    uint32_t row[kFetches];
+    uint32_t row[MAPPED ? kFetches : 1];
     u32x4 reg[kFetches];
     uint32_t scale[kFetches];
 
-    static __device__ __forceinline__ uint32_t lds_row(int p) { return thread() / kAcross + (uint32_t)p * kRowsPerFetch; }
-    __device__ __forceinline__ void start(const Operand& m, uint32_t free0, uint32_t free_end) {
-        free = free0 + thread() % kAcross * 16;
+    __device__ __forceinline__ uint32_t lds_row(int p) const { return me / kAcross + (uint32_t)p * kRowsPerFetch; }
+    __device__ __forceinline__ void start(uint32_t thread, const Operand& m, uint32_t free0, uint32_t free_end) {
+        me = thread % THREADS;
+        free = free0 + me % kAcross * 16;
         there = free < free_end && lds_row(0) < kDepth, free_there = (int)(free_end - free);
         codes = (const uint8_t*)m.p, scales = m.scales, source = m.source;
         width = m.width, blocks = (m.width + 31) / 32, slots = m.slots, rows = m.rows;
     }
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
-        if (source != nullptr)
+        if constexpr (MAPPED)
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) row[p] = there && depth0 + lds_row(p) < depth_end ? (uint32_t)source[depth0 + lds_row(p)] : 0xFFFFFFFFu;
     }
+    __device__ __forceinline__ void looked_up() const {     // before the other side's loads, as above
+        if constexpr (MAPPED)
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) asm volatile("" ::"v"(row[p]));
+    }
     __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
         // rows that are not looked up are reached from the stage's first one: no limit to the tensor
-        const uint64_t from = source != nullptr ? 0 : depth0;
+        const uint64_t from = MAPPED ? 0 : depth0;
         const __amdgpu_buffer_rsrc_t c = buffer_at(codes + from * width), s = buffer_at(scales + from * blocks);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
-            const uint32_t at = source != nullptr ? fdiv(row[p], slots) : lds_row(p);
-            const bool use = there && (source != nullptr ? row[p] < 1u << 31 && at < rows : depth0 + at < depth_end);
+            const uint32_t at = MAPPED ? fdiv(row[p], slots) : lds_row(p);
+            const bool use = there & (MAPPED ? (row[p] < 1u << 31) & (at < rows) : depth0 + at < depth_end);
+            const uint32_t code = at * width + free, scale_at = at * blocks + free / 32;
             if constexpr (LOOSE) reg[p] = fetch_some(codes + (from + at) * width + free, use ? free_there : 0, (const char*)codes + (uint64_t)rows * width);
-            else reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? at * width + free : kBeyond), 0, 0);
-            scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? at * blocks + free / 32 : kBeyond), 0, 0);
+            else reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? code : kBeyond), 0, 0);
+            scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? scale_at : kBeyond), 0, 0);
         }
     }
     __device__ __forceinline__ void put(char* tile) const {
@@ -432,7 +458,7 @@ template <typename T, int FREE, int THREADS, bool LOOSE> struct Coded {
         __builtin_amdgcn_sched_barrier(0);      // not before the products: it would wait for the codes there
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
-            const uint32_t d = lds_row(p), c = thread() % kAcross;
+            const uint32_t d = lds_row(p), c = me % kAcross;
             if (kRowsPerFetch > kDepth && d >= kDepth) return;
             char* const at = tile + d * (FREE * sizeof(T));
             const float by = power_of(scale[p]);
@@ -464,196 +490,212 @@ template <int READS, int PRODUCTS> __device__ __forceinline__ void interleave() 
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Sum over depth0 .. depth_end into acc with a ring of LDS images.  While the matrix cores work on one step, the fragments
-// of the next one are read; the only barrier of a stage stands between its two steps: all wavefronts have read the
-// stage's last fragments then, so its image can receive another stage.
+// The sum of a tile, over depth0 .. depth_end.  begin() requests the first stages, multiply() adds up.  While the matrix
+// cores work on one step, the fragments of the next one are read; the only barrier of a stage stands between its two
+// steps: all wavefronts have read the stage's last fragments then, so its image can receive another stage.
 //
 // LOOSE: operands of any size and alignment.  Two sets of fragments beside operands in registers (those, and codes) do
 // not fit: there the other wavefront of the SIMD multiplies while this one reads.
 template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED, bool LOOSE>
-using Side = std::conditional_t<LAYOUT == kCodes, Coded<T, FREE, THREADS, LOOSE>, std::conditional_t<LOOSE, Loose<T, LAYOUT, FREE, THREADS>, Direct<T, LAYOUT, FREE, THREADS, MAPPED>>>;
-template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE>
-__device__ __forceinline__ void sum_tile(char* lds, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
-                                                uint32_t slow_end, uint32_t depth0, uint32_t depth_end, f32x4 (&acc)[S::SI][S::FI]) {
-    constexpr uint32_t kDepth = kStageBytes / sizeof(T);
-    constexpr uint32_t kImage = S::kImage;
+using Side = std::conditional_t<LAYOUT == kCodes, Coded<T, FREE, THREADS, MAPPED, LOOSE>, std::conditional_t<LOOSE, Loose<T, LAYOUT, FREE, THREADS>, Direct<T, LAYOUT, FREE, THREADS, MAPPED>>>;
+template <typename T, int FL, int SL, bool FM, bool SM, typename S, bool LOOSE> struct Sum {
+    static constexpr uint32_t kDepth = kStageBytes / sizeof(T), kImage = S::kImage;
+    static constexpr bool kRegisters = LOOSE || FL == kCodes || SL == kCodes;      // operands pass through them
+    static constexpr bool kOrdered = sizeof(T) == 2;
+    static constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
+    char* lds;
+    uint32_t depth0, depth_end, stages, thread;
     Side<T, FL, S::kFast, S::kThreads, FM, LOOSE> fs;
     Side<T, SL, S::kSlow, S::kThreads, SM, LOOSE> ss;
-    constexpr bool kOrdered = sizeof(T) == 2;
-    constexpr int kReads = S::FI * (FL == kDepthFast ? 1 : 2) + S::SI * (SL == kDepthFast ? 1 : 2), kProducts = S::FI * S::SI;
-    if (depth0 >= depth_end) return;
-    uint32_t stages = (depth_end - depth0 + kDepth - 1) / kDepth;
-    if constexpr (S::kGroups > 1) {
-        // every group the same number of stages, since all meet at the barriers: those beyond the end are zeros
-        stages = (stages + S::kGroups - 1) / S::kGroups;
-        depth0 += S::group() * stages * kDepth;
-        depth_end = depth_end - (depth0 < depth_end ? depth0 : depth_end) < stages * kDepth ? depth_end : depth0 + stages * kDepth;
-        lds += S::group() * S::kImages * kImage;
+
+    __device__ __forceinline__ void looked_up() {
+        fs.looked_up();
+        ss.looked_up();
     }
-    fs.start(fast, fast0, fast_end);
-    if constexpr (LOOSE || FL == kCodes || SL == kCodes || SM) ss.start(slow, slow0, slow_end);
-    const auto issue = [&](uint32_t image, uint32_t d) {
+    __device__ __forceinline__ void issue(uint32_t image, uint32_t d) {
+        looked_up();
         fs.issue(lds + image, d, depth_end);
         ss.issue(lds + image + S::kFast * kStageBytes, d, depth_end);
-    };
-    const auto look_up = [&](uint32_t d) {
+    }
+    __device__ __forceinline__ void look_up(uint32_t d) {
         fs.look_up(d, depth_end);
         ss.look_up(d, depth_end);
-    };
-    const auto put = [&](uint32_t image) {
+    }
+    __device__ __forceinline__ void put(uint32_t image) {
         fs.put(lds + image);
         ss.put(lds + image + S::kFast * kStageBytes);
-    };
-    if constexpr (LOOSE || FL == kCodes || SL == kCodes) {
-        look_up(depth0);
-        issue(0, depth0);
-        look_up(depth0 + kDepth);
-        put(0);
-        for (uint32_t d = depth0, image = 0; stages > 0; --stages, d += kDepth, image ^= kImage) {
-            arrive<0>();
-            issue(image ^ kImage, d + kDepth);
-            look_up(d + 2 * kDepth);
-#pragma unroll
-            for (uint32_t kk = 0; kk < kSteps; ++kk) {
-                Step<T, FL, SL, S> step;
-                step.read(lds + image, kk);
-                step.multiply(acc);
-            }
-            put(image ^ kImage);
+    }
+    // The images are free: no wavefront reads them any more.
+    __device__ __forceinline__ void begin(char* images, const Operand& fast, uint32_t fast0, uint32_t fast_end, const Operand& slow, uint32_t slow0,
+                                          uint32_t slow_end, uint32_t from, uint32_t end) {
+        lds = images, depth0 = from, depth_end = end, stages = 0, thread = threadIdx.x;
+        if (depth0 >= depth_end) return;
+        stages = (depth_end - depth0 + kDepth - 1) / kDepth;
+        if constexpr (S::kGroups > 1) {
+            // every group the same number of stages, since all meet at the barriers: those beyond the end are zeros
+            stages = (stages + S::kGroups - 1) / S::kGroups;
+            depth0 += S::group() * stages * kDepth;
+            depth_end = depth_end - (depth0 < depth_end ? depth0 : depth_end) < stages * kDepth ? depth_end : depth0 + stages * kDepth;
+            lds += S::group() * 2 * kImage;
         }
-    } else {
-        constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;     // of a stage
+        fs.start(thread, fast, fast0, fast_end);
+        if constexpr (kRegisters || SM) ss.start(thread, slow, slow0, slow_end);
         look_up(depth0);
         // the fast side's first stage travels while the slow side's rows are looked up
         fs.issue(lds, depth0, depth_end);
-        if constexpr (!SM) ss.start(slow, slow0, slow_end);
+        if constexpr (!kRegisters && !SM) ss.start(thread, slow, slow0, slow_end);
         ss.issue(lds + S::kFast * kStageBytes, depth0, depth_end);
         look_up(depth0 + kDepth);
-#pragma unroll
-        for (int i = 1; i < S::kImages; ++i) {
-            issue(i * kImage, depth0 + i * kDepth);
-            look_up(depth0 + (i + 1) * kDepth);
+        if constexpr (!kRegisters) {
+            issue(kImage, depth0 + kDepth);
+            look_up(depth0 + 2 * kDepth);
         }
-        arrive<(S::kImages - 1) * kLoads>();
-        uint32_t image = 0;
-        Step<T, FL, SL, S> even, odd;
-        even.read(lds, 0);
-        for (uint32_t d = depth0; stages > 1; --stages, d += kDepth) {
-            odd.read(lds + image, 1);
-            even.multiply(acc);
-            if constexpr (kOrdered) interleave<kReads, kProducts>();
-            arrive<(S::kImages - 2) * kLoads>();        // the next stage has arrived
-            // requests, reads and products in turn: behind each other the requests would hold up the products
-            const uint32_t free_image = image;
-            image = image == (S::kImages - 1) * kImage ? 0 : image + kImage;
+    }
+    __device__ __forceinline__ void multiply(f32x4 (&acc)[S::SI][S::FI]) {
+        if (stages == 0) return;
+        if constexpr (kRegisters) {
+            put(0);
+            for (uint32_t d = depth0, image = 0; stages > 0; --stages, d += kDepth, image ^= kImage) {
+                arrive<0>();
+                issue(image ^ kImage, d + kDepth);
+                look_up(d + 2 * kDepth);
 #pragma unroll
-            for (int i = 0; i < S::FI; ++i) {
-                fs.issue(lds + free_image, d + S::kImages * kDepth, depth_end, i, S::FI);
-                ss.issue(lds + free_image + S::kFast * kStageBytes, d + S::kImages * kDepth, depth_end, i, S::FI);
-                even.read(lds + image, 0, i);
-                odd.multiply(acc, i);
-                __builtin_amdgcn_sched_barrier(0);
+                for (uint32_t kk = 0; kk < kSteps; ++kk) {
+                    Step<T, FL, SL, S> step;
+                    step.read(thread, lds + image, kk);
+                    step.multiply(acc);
+                }
+                put(image ^ kImage);
             }
-            look_up(d + (S::kImages + 1) * kDepth);
+        } else {
+            constexpr int kLoads = decltype(fs)::kFetches + decltype(ss)::kFetches;     // of a stage
+            arrive<kLoads>();
+            uint32_t image = 0;
+            Step<T, FL, SL, S> even, odd;
+            even.read(thread, lds, 0);
+            for (uint32_t d = depth0; stages > 1; --stages, d += kDepth) {
+                odd.read(thread, lds + image, 1);
+                even.multiply(acc);
+                if constexpr (kOrdered) interleave<kReads, kProducts>();
+                arrive<0>();        // the next stage has arrived
+                // requests, reads and products in turn: behind each other the requests would hold up the products
+                const uint32_t free_image = image;
+                looked_up();
+                image ^= kImage;
+#pragma unroll
+                for (int i = 0; i < S::FI; ++i) {
+                    fs.issue(lds + free_image, d + 2 * kDepth, depth_end, i, S::FI);
+                    ss.issue(lds + free_image + S::kFast * kStageBytes, d + 2 * kDepth, depth_end, i, S::FI);
+                    even.read(thread, lds + image, 0, i);
+                    odd.multiply(acc, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                look_up(d + 3 * kDepth);
+            }
+            odd.read(thread, lds + image, 1);
+            even.multiply(acc);
+            odd.multiply(acc);
         }
-        odd.read(lds + image, 1);
-        even.multiply(acc);
-        odd.multiply(acc);
-    }
-    arrive<0>();            // nothing travels to LDS when it is used again
-    if constexpr (S::kGroups > 1) {
-        // the sums of the others to the first group, in the groups' order
-        f32x4* const sums = (f32x4*)(lds - S::group() * S::kImages * kImage);
+        arrive<0>();            // nothing travels to LDS when it is used again
+        if constexpr (S::kGroups > 1) {
+            // the sums of the others to the first group, in the groups' order
+            f32x4* const sums = (f32x4*)(lds - S::group() * 2 * kImage);
 #pragma unroll
-        for (int g = 1; g < S::kGroups; ++g) {
-            if (S::group() == (uint32_t)g)
+            for (int g = 1; g < S::kGroups; ++g) {
+                if (S::group() == (uint32_t)g)
 #pragma unroll
-                for (int i = 0; i < S::SI * S::FI; ++i) sums[i * S::kThreads + threadIdx.x % S::kThreads] = acc[i / S::FI][i % S::FI];
-            __syncthreads();
-            if (S::group() == 0)
+                    for (int i = 0; i < S::SI * S::FI; ++i) sums[i * S::kThreads + threadIdx.x % S::kThreads] = acc[i / S::FI][i % S::FI];
+                __syncthreads();
+                if (S::group() == 0)
 #pragma unroll
-                for (int i = 0; i < S::SI * S::FI; ++i) acc[i / S::FI][i % S::FI] += sums[i * S::kThreads + threadIdx.x % S::kThreads];
-            __syncthreads();
+                    for (int i = 0; i < S::SI * S::FI; ++i) acc[i / S::FI][i % S::FI] += sums[i * S::kThreads + threadIdx.x % S::kThreads];
+                __syncthreads();
+            }
         }
     }
-}
+};
 
-// Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been
-// added with `accumulate`.
-template <typename O, typename S>
-__device__ __forceinline__ void store_tile(O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end, bool accumulate,
+// Results of a tile to out (stride: between slow indices): rounded once, after what out holds has been added with
+// ACCUMULATE.  A lane's own results are pieces of 4 of 16 rows; every wavefront brings them into rows by way of a
+// piece of LDS that it alone uses (L: the type there, O or binary32), whose chunks of 16 bytes change places by their
+// row, so that the pieces meet no bank conflicts.  A block of 16 rows is written while the one before is stored.
+// WHOLE: rows of out are whole chunks that start on 16 bytes.
+template <typename O, typename L, typename S, bool WHOLE, bool ACCUMULATE>
+__device__ __forceinline__ void store_rows(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
                                            const f32x4 (&acc)[S::SI][S::FI]) {
-    if (S::group() != 0) return;
-    const uint32_t wave = S::wave(), lane = threadIdx.x & 63u;
-    const uint32_t f0 = fast0 + wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
-    const uint32_t s0 = slow0 + wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
+    constexpr uint32_t V = 16 / sizeof(O), kPitch = S::FI * 16 * sizeof(L), kRowChunks = kPitch / 16, kLane = V * sizeof(L) / 16;
+    constexpr uint32_t kAcross = S::FI * 16 / V, kDown = 64 / kAcross;      // lanes to a row, rows at once
+    static_assert(S::kThreads / 64 * 16 * kPitch <= (uint32_t)S::kLds && kRowChunks <= 16 && 16 % kDown == 0, "a wavefront's LDS");
+    constexpr uint32_t kPiece = 16 * kPitch;
+    const uint32_t wave = S::wave(threadIdx.x), lane = threadIdx.x & 63u;
+    lds += wave * kPiece;
+    fast0 += wave % S::kWavesFast * (S::FI * 16), slow0 += wave / S::kWavesFast * (S::SI * 16);
+    const auto chunk = [](uint32_t row, uint32_t c) { return row * kPitch + (c ^ ((row * kRowChunks / 16) & (kRowChunks - 1))) * 16; };
+    const uint32_t f = fast0 + lane % kAcross * V, down = lane / kAcross;
+    O* p = out + (int64_t)(slow0 + down) * stride + f;
+    Vec<L, V> l[16 / kDown];
+    const auto store = [&](uint32_t j) {
+#pragma unroll
+        for (uint32_t t = 0; t < 16 / kDown; ++t, p += kDown * stride) {
+            const int there = (int)(fast_end - f);
+            if (slow0 + j * 16 + t * kDown + down >= slow_end || f >= fast_end) continue;
+            Vec<O, V> v;
+            if constexpr (sizeof(L) == 4) {
+                if constexpr (ACCUMULATE) l[t] += widen<O, V>(load_some<O, V, WHOLE>(p, there));
+                v = narrow<O, V>(l[t]);
+            } else {
+                v = l[t];
+            }
+            // past the caches, which hold operands: 2 to 11 % of a call
+            if constexpr (WHOLE) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+            else store_some<O, V, false>(p, v, there);
+        }
+    };
 #pragma unroll
     for (int j = 0; j < S::SI; ++j) {
-        const uint32_t s = s0 + j * 16;
-        if (s >= slow_end) continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // a wavefront's LDS accesses are done in their order
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < S::FI; ++i) {
-            const uint32_t f = f0 + i * 16;
-            if (f >= fast_end) continue;
-            O* const p = out + (int64_t)s * stride + f;
-            const int there = (int)(fast_end - f);
-            f32x4 v = acc[j][i];
-            if (accumulate) v += widen<O, 4>(load_some<O, 4, false>(p, there));
-            store_some<O, 4, false>(p, narrow<O, 4>(v), there);
+            const uint32_t at = (i * 16 + (lane >> 4) * 4) * (uint32_t)sizeof(L);
+            *(Vec<L, 4>*)(lds + chunk(lane & 15u, at / 16) + at % 16) = narrow<L, 4>(acc[j][i]);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (j > 0) store(j - 1);
+#pragma unroll
+        for (uint32_t t = 0; t < 16 / kDown; ++t)
+#pragma unroll
+            for (uint32_t h = 0; h < kLane; ++h) {
+                constexpr int kPart = 16 / sizeof(L);
+                const Vec<L, kPart> part = *(const Vec<L, kPart>*)(lds + chunk(t * kDown + down, lane % kAcross * kLane + h));
+#pragma unroll
+                for (int e = 0; e < kPart; ++e) l[t][h * kPart + e] = part[e];
+            }
     }
+    store(S::SI - 1);
+}
+
+template <typename O, typename L, typename S>
+__device__ __forceinline__ void store_tile(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
+                                           const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
+    if (S::group() != 0) return;
+    const bool whole = (fast_end * sizeof(O)) % 16 == 0 && ((uintptr_t)out | (uintptr_t)stride * sizeof(O)) % 16 == 0;
+    if constexpr (sizeof(L) == 4) {
+        if (accumulate) return whole ? store_rows<O, L, S, true, true>(lds, out, stride, fast0, fast_end, slow0, slow_end, acc)
+                                     : store_rows<O, L, S, false, true>(lds, out, stride, fast0, fast_end, slow0, slow_end, acc);
+    }
+    whole ? store_rows<O, L, S, true, false>(lds, out, stride, fast0, fast_end, slow0, slow_end, acc)
+          : store_rows<O, L, S, false, false>(lds, out, stride, fast0, fast_end, slow0, slow_end, acc);
 }
 
 // --- which tile ---
 
 // Rows from, end of bin b: expert b, or the unused rows for b == experts.  Held to 0 .. rows whatever offsets says.
 __device__ __forceinline__ void rows_of(const int32_t* offsets, uint32_t experts, uint32_t rows, uint32_t b, uint32_t* from, uint32_t* end) {
-    const uint32_t o = (uint32_t)offsets[b], p = b < experts ? (uint32_t)offsets[b + 1] : rows;
+    const uint32_t o = (uint32_t)offsets[b], next = (uint32_t)offsets[b < experts ? b + 1 : b], p = b < experts ? next : rows;   // both at once
     *end = p < rows ? p : rows;
     *from = o < *end ? o : *end;
-}
-
-// The same by way of LDS (all of it, free by now), in whole rows of the tile: a wavefront's own results are pieces of 8 or
-// 16 bytes of 16 rows.  Chunks of 16 bytes change places by their row, so that those pieces meet no bank
-// conflicts.
-template <typename O, typename S>
-__device__ __forceinline__ void store_tile_rows(char* lds, O* out, int64_t stride, uint32_t fast0, uint32_t fast_end, uint32_t slow0, uint32_t slow_end,
-                                                const f32x4 (&acc)[S::SI][S::FI], bool accumulate) {
-    constexpr int LDS_BYTES = S::kLds;
-    constexpr uint32_t kPitch = S::kFast * sizeof(O), kChunks = kPitch / 16, V = 16 / sizeof(O);
-    constexpr int kPasses = (S::kSlow * (int)kPitch + LDS_BYTES - 1) / LDS_BYTES, kRows = S::kSlow / kPasses;
-    static_assert(kRows % 16 == 0 && kRows * kPasses == S::kSlow, "whole blocks");
-    const uint32_t wave = S::wave(), lane = threadIdx.x & 63u;
-    const uint32_t f0 = wave % S::kWavesFast * (S::FI * 16) + (lane >> 4) * 4;
-    const uint32_t s0 = wave / S::kWavesFast * (S::SI * 16) + (lane & 15u);
-#pragma unroll
-    for (int pass = 0; pass < kPasses; ++pass) {
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < S::SI; ++j) {
-            const uint32_t row = s0 + j * 16 - pass * kRows;
-            if (row < (uint32_t)kRows && S::group() == 0) {
-#pragma unroll
-                for (int i = 0; i < S::FI; ++i) {
-                    const uint32_t at = (f0 + i * 16) * (uint32_t)sizeof(O);
-                    *(Vec<O, 4>*)(lds + row * kPitch + ((at / 16) ^ (row & (kChunks < 16 ? kChunks - 1 : 15u))) * 16 + at % 16) = narrow<O, 4>(acc[j][i]);
-                }
-            }
-        }
-        __syncthreads();
-        for (uint32_t id = threadIdx.x; id < kRows * kChunks; id += S::kAllThreads) {
-            const uint32_t row = id / kChunks, c = id % kChunks, s = slow0 + pass * kRows + row, f = fast0 + c * V;
-            if (s >= slow_end) break;
-            if (f >= fast_end) continue;
-            Vec<O, V> v = *(const Vec<O, V>*)(lds + row * kPitch + (c ^ (row & (kChunks < 16 ? kChunks - 1 : 15u))) * 16);
-            O* const p = out + (int64_t)s * stride + f;
-            if constexpr (sizeof(O) == 4)
-                if (accumulate) v += load_some<O, V, false>(p, (int)(fast_end - f));
-            // past the caches, which hold operands: 2 to 11 % of a call
-            if (f + V <= fast_end && (uintptr_t)p % 16 == 0) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-            else store_some<O, V, false>(p, v, (int)(fast_end - f));
-        }
-    }
 }
 
 // Which tile a workgroup takes.  Workgroups go round the 8 XCDs, so numbers that are 8 apart share an L2: each
@@ -705,9 +747,10 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, uint32_t exper
     }
     uint32_t row;
     grouped<8>(left, down, across, &row, col);
-    *bin = b;
-    *from = o + row * height;
-    *end = p - *from < height ? p : *from + height;
+    *bin = uniform(b);
+    *from = uniform(o + row * height);
+    *end = uniform(p - *from < height ? p : *from + height);
+    *col = uniform(*col);
     return true;
 }
 
@@ -719,14 +762,14 @@ __global__ __launch_bounds__(S::kAllThreads) void expert_product_kernel(const Ex
     const uint32_t across = (a.n + S::kFast - 1) / S::kFast;
     uint32_t bin, row0, row_end, col;
     if (!find_tile(a.offsets, a.experts, a.rows, S::kSlow, across, &bin, &row0, &row_end, &col)) return;
-    const uint32_t col0 = col * S::kFast, col_end = a.n;
+    const uint32_t col0 = col * S::kFast;
+    const T* const w = (const T*)a.w + (int64_t)bin * a.k * a.n;
+    const Operand fast = WL == kDepthFast ? Operand(w, a.n, a.k) : Operand(w, a.k, a.n);
     f32x4 acc[S::SI][S::FI] = {};
-    if (bin < a.experts) {
-        const T* const w = (const T*)a.w + (int64_t)bin * a.k * a.n;
-        const Operand fast = WL == kDepthFast ? Operand(w, a.n, a.k) : Operand(w, a.k, a.n);
-        sum_tile<T, WL, kDepthFast, false, false, S, LOOSE>(lds, fast, col0, col_end, Operand(a.x), row0, row_end, 0, a.k, acc);
-    }
-    store_tile_rows<T, S>(lds, (T*)a.out, a.out_stride, col0, col_end, row0, row_end, acc, false);
+    Sum<T, WL, kDepthFast, false, false, S, LOOSE> sum;
+    sum.begin(lds, fast, col0, a.n, Operand(a.x), row0, row_end, 0, bin < a.experts ? a.k : 0);
+    sum.multiply(acc);
+    store_tile<T, T, S>(lds, (T*)a.out, a.out_stride, col0, a.n, row0, row_end, acc, false);
 }
 
 // The i-th expert by number of rows, most first (equal ones in their order), for up to 64 experts: every lane counts how many
@@ -756,16 +799,22 @@ __global__ __launch_bounds__(S::kAllThreads) void weight_gradient_kernel(const W
     uint32_t expert = turn, from, end;
     if (a.experts <= 64) expert = by_size(a.offsets, a.experts, a.rows, turn, &from, &end);
     else rows_of(a.offsets, a.experts, a.rows, expert, &from, &end);
+    expert = uniform(expert), from = uniform(from), end = uniform(end);
     uint32_t fi, si;
     grouped<4>(tile, ts, tf, &si, &fi);
     const uint32_t f0 = fi * S::kFast, s0 = si * S::kSlow;
     f32x4 acc[S::SI][S::FI] = {};
-    sum_tile<T, FL, SL, FM, SM, S, LOOSE>(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end, acc);
+    Sum<T, FL, SL, FM, SM, S, LOOSE> sum;
+    sum.begin(lds, Operand(a.fast), f0, a.fast.width, Operand(a.slow), s0, a.slow.width, from, end);
+    sum.multiply(acc);
     const int64_t at = (int64_t)expert * a.fast.width * a.slow.width;
-    const bool accumulate = a.accumulate != 0;
-    if (a.out_type == TPERM_TYPE_F32) store_tile_rows<float, S>(lds, (float*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, accumulate);
-    else if (a.out_type == TPERM_TYPE_F16) store_tile<_Float16, S>((_Float16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
-    else store_tile<__bf16, S>((__bf16*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, accumulate, acc);
+    const auto store = [&](auto o) {
+        using O = decltype(o);
+        store_tile<O, float, S>(lds, (O*)a.out + at, a.fast.width, f0, a.fast.width, s0, a.slow.width, acc, a.accumulate != 0);
+    };
+    if (a.out_type == TPERM_TYPE_F32) store(0.0f);
+    else if (a.out_type == TPERM_TYPE_F16) store((_Float16)0);
+    else store((__bf16)0);
 }
 
 template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream);

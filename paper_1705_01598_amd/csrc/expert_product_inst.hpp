@@ -6,10 +6,10 @@
 
 namespace tperm {
 
-using TinyTile = TileShape<64, 64, 4, 2, 2, 2>;
-using SmallTile = TileShape<128, 128, 4, 2, 2>;
-using NarrowTile = TileShape<128, 64, 4, 2, 2>;    // 32-bit elements, which the matrix cores bound: finer rounds of tiles
-using WideTile = TileShape<256, 256, 8, 4, 2>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
+using TinyTile = TileShape<64, 64, 4, 2, 2>;
+using SmallTile = TileShape<128, 128, 4, 2>;
+using NarrowTile = TileShape<128, 64, 4, 2>;    // 32-bit elements, which the matrix cores bound: finer rounds of tiles
+using WideTile = TileShape<256, 256, 8, 4>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
 
 // Workgroups with more than 64 KiB of LDS have to be allowed it, once on each device.
 template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
@@ -72,8 +72,12 @@ template <typename T> hipError_t product_of(const ExpertProductArgs& a, bool w_k
 
 template <typename T, typename S, bool LOOSE> hipError_t gradient_tiles(const WeightGradientArgs& a, hipStream_t stream) {
     const uint64_t blocks = over(over(a.fast.width, S::kFast) * over(a.slow.width, S::kSlow), kXcds) * kXcds * a.experts;
-    if (a.fast.scales != nullptr) return go<weight_gradient_kernel<T, kCodes, kFreeFast, false, false, S, LOOSE>, S>(blocks, a, stream);
-    if (a.slow.scales != nullptr) return go<weight_gradient_kernel<T, kFreeFast, kCodes, false, false, S, LOOSE>, S>(blocks, a, stream);
+    if (a.fast.scales != nullptr)
+        return a.fast.source != nullptr ? go<weight_gradient_kernel<T, kCodes, kFreeFast, true, false, S, LOOSE>, S>(blocks, a, stream)
+                                        : go<weight_gradient_kernel<T, kCodes, kFreeFast, false, false, S, LOOSE>, S>(blocks, a, stream);
+    if (a.slow.scales != nullptr)
+        return a.slow.source != nullptr ? go<weight_gradient_kernel<T, kFreeFast, kCodes, false, true, S, LOOSE>, S>(blocks, a, stream)
+                                        : go<weight_gradient_kernel<T, kFreeFast, kCodes, false, false, S, LOOSE>, S>(blocks, a, stream);
     if constexpr (!LOOSE) {
         if (a.fast.source != nullptr) return go<weight_gradient_kernel<T, kFreeFast, kFreeFast, true, false, S, false>, S>(blocks, a, stream);
         if (a.slow.source != nullptr) return go<weight_gradient_kernel<T, kFreeFast, kFreeFast, false, true, S, false>, S>(blocks, a, stream);
