@@ -49,13 +49,13 @@ template <typename T, typename S, bool LOOSE> hipError_t product_tiles(const Exp
 template <typename T, bool LOOSE> hipError_t product_with(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
     // Large tiles need fewer bytes an operation, small ones fill the 256 compute units and waste less on experts of
     // few rows (bf16, us with tiles of 256, 128, 64; rows of all experts on the average):
-    //   8 experts 1024 x 1024: 128 rows 28 19 13, 256 rows 29 19 19, 512 rows 30 24 27, 1024 rows 32 39 46
-    //   8 experts 2048 x 2048: 256 rows 48 38 44, 512 rows 51 60 72;  64 experts: 128 rows 183 177 197, 256 rows 238 244 326
-    //   64 experts 2048 x 1024, one row: 24 with 128, 19 with 64; 16 rows 60, 56
+    //   8 experts 1024 x 1024: 128 rows 26 17 13, 256 rows 26 17 19, 512 rows 27 21 28, 1024 rows 29 35 46
+    //   8 experts 2048 x 2048: 256 rows 45 36 45, 512 rows 47 59 73;  64 experts: 128 rows 183 171 221, 256 rows 233 243 352
+    //   64 experts 2048 x 1024: one row 40 26 19, 16 rows 66 61 49
     const uint64_t rows = over(a.rows, a.experts);
     const auto tiles = [&](uint64_t side) { return over(rows, side) * a.experts * over(a.n, side); };
-    //   f32, 8 experts 1024 x 1024, tiles of 128, 128 x 64, 64: 1024 rows 203 178 172, 4096 rows 559 555 572;
-    //   701 x 903: 750 rows 125 142 108
+    //   f32, 8 experts 1024 x 1024, tiles of 128, 128 x 64, 64: 1024 rows 200 178 182, 4096 rows 554 540 564;
+    //   701 x 903: 750 rows 123 139 104
     if constexpr (sizeof(T) == 2) {
         if (rows >= 192 && tiles(256) >= 128) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
         if (rows >= 64 && tiles(128) >= 128) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
@@ -87,8 +87,8 @@ template <typename T, typename S, bool LOOSE> hipError_t gradient_tiles(const We
 
 template <typename T, bool LOOSE> hipError_t gradient_with(const WeightGradientArgs& a, hipStream_t stream) {
     const auto tiles = [&](uint64_t side) { return over(a.fast.width, side) * over(a.slow.width, side) * a.experts; };
-    // As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 79 49 71,
-    // 2048 x 2048 (512) 104 117 270; f32, 8 experts 1024 x 1024 (512 of 128), 128, 128 x 64, 64: 232 149 155
+    // As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 73 44 56,
+    // 2048 x 2048 (512) 93 109 207; f32, 8 experts 1024 x 1024 (512 of 128), 128, 128 x 64, 64: 234 152 164
     if constexpr (sizeof(T) == 2) {
         if (tiles(256) >= 192) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
         if (tiles(128) >= 256) return gradient_tiles<T, SmallTile, LOOSE>(a, stream);

@@ -4,9 +4,10 @@
 // lanes, 16 bytes a lane and step; narrow rows take narrow groups, so that a wavefront has as many rows in
 // flight as it needs.  Sums are formed in binary32 in the order of the slots.
 //
-// Results are stored past the caches (rows of 4 KiB: gather of 16384 x 2 50 -> 39 us, backward of 2048 x 4 of 8 KiB
-// 36 -> 25 us); rows are read past them (ONCE) where they fill half of the memory-side cache (combine of 16384 x 2
-// 53 -> 43 us), while smaller ones may still be there from the product that wrote them (2048 x 4 of 8 KiB 15 -> 19 us).
+// Results are stored past the caches (rows of 4 KiB: gather of 16384 x 2 50 -> 39 us, combine 39 -> 37, backward of 2048 x 4
+// rows of 8 KiB 34 -> 25); rows are read past them too (ONCE) where they fill a third of the memory-side cache (combine and
+// backward of 16384 x 2 37 -> 34 and 63 -> 55 us, of 12288 x 2 26 -> 26 and 48 -> 42), while smaller ones may still be
+// there from the product that wrote them (6144 x 2 13 -> 14 and 21 -> 24).
 // Rows of 4 KiB now: combine of 8192 x 8 50 us, 5.9 TB/s, its backward 105 us, 5.4 TB/s, both near what a copy
 // reaches (6.1); gather 74 us, 4.1 TB/s, where a token's row is read eight times, from the memory-side cache.
 #include <type_traits>
@@ -228,14 +229,14 @@ template <typename F> hipError_t with_slots(uint32_t slots, F f) {
                                                                                                                     : f(std::integral_constant<int, 8>());
 }
 
-// Rows of more than half of the 256 MB memory-side cache.
-bool read_once(const RowsArgs& a, size_t elem) { return (uint64_t)a.count * a.width * elem > 128u << 20; }
+// Rows of more than a third of the 256 MiB memory-side cache.
+bool read_once(const RowsArgs& a, size_t elem) { return (uint64_t)a.count * a.width * elem * 3 > 256u << 20; }
 
 }  // namespace
 
 hipError_t launch_expert_combine(RowsArgs a, int type, hipStream_t stream) {
     return with_type(type, [&](auto t) {
-        // eight slots at once leave three wavefronts to a SIMD: 74 -> 89 us with 8192 x 8 rows of 4 KiB
+        // eight slots at once are no faster (51 us either way with 8192 x 8 rows of 4 KiB)
         return with_slots(a.slots < 4 ? a.slots : 4, [&](auto slots) {
             using T = decltype(t);
             constexpr int N = decltype(slots)::value;
