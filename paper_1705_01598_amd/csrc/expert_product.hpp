@@ -322,6 +322,29 @@ template <typename E> __device__ __forceinline__ u32x4 fetch_some(const E* q, in
     return v;
 }
 
+// Sides of 64 16-bit elements keep the branches, which leave out rows that are not there (us with and without them: 1001 x 1003,
+// 25 rows of an expert 14.7 15.7; gradient of 125 rows, 333 x 555, 17.1 19.0), wider ones do without (gradient of 1024
+// rows, 1001 x 1003, 121 78; product of 1024 rows, 2001 x 2003, 208 184).
+template <typename T, int FREE> constexpr bool kMoved = FREE * sizeof(T) > 128;
+
+// The same of a row that has 16 bytes at least, without a branch, behind which the compiler would wait for the load: where
+// fewer than that are left, the row's last 16 bytes, which straighten() puts right.  left <= 0: any bytes, from `base`.
+template <typename E> __device__ __forceinline__ u32x4 fetch_moved(const E* q, int left, const void* base) {
+    constexpr int V = 16 / sizeof(E);
+    const E* const at = left > 0 ? q - (left < V ? V - left : 0) : (const E*)base;
+    u32x4 v;
+    __builtin_memcpy(&v, at, 16);
+    return v;
+}
+template <typename E> __device__ __forceinline__ u32x4 straighten(u32x4 v, int left) {
+    constexpr int V = 16 / sizeof(E);
+    if (left < V) {
+        const unsigned __int128 all = __builtin_bit_cast(unsigned __int128, v);
+        v = __builtin_bit_cast(u32x4, left > 0 ? all >> ((V - left) * (int)sizeof(E) * 8) : (unsigned __int128)0);
+    }
+    return v;
+}
+
 // The operand of one side, of any size, stride and alignment, by way of registers: requested while the stage before is
 // multiplied, put to LDS behind that.
 template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
@@ -340,13 +363,16 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
     FastDiv slots;
     uint32_t rows, free, free_end;
     u32x4 reg[kFetches];
+    bool moved;         // rows have 16 bytes
+    uint32_t left;      // elements of each fetch that exist, a byte each
+    static_assert(kFetches <= 4, "a word");
 
     __device__ __forceinline__ uint32_t lds_row(int p) const { return me / kAcross + (uint32_t)p * kRowsPerFetch; }
     __device__ __forceinline__ void start(uint32_t thread, const Operand& m, uint32_t free0, uint32_t free_end_) {
         me = thread % THREADS;
         base = (const char*)m.p, row_bytes = m.stride * (int64_t)sizeof(T);
         end = base + ((int64_t)m.rows - 1) * row_bytes + (int64_t)m.width * (int64_t)sizeof(T);
-        source = m.source, slots = m.slots, rows = m.rows;
+        source = m.source, slots = m.slots, rows = m.rows, moved = kMoved<T, FREE> && m.rows > 0 && m.width >= (uint32_t)V;
         if constexpr (LAYOUT == kDepthFast) {
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) {
@@ -367,16 +393,31 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
     }
     __device__ __forceinline__ void looked_up() const {}
     __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
+        left = 0;
+        const char* q[kFetches];
+        int n[kFetches];
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
+            uint32_t exist;
             if constexpr (LAYOUT == kDepthFast) {
                 const uint32_t d = depth0 + me % kAcross * V;
-                reg[p] = fetch_some((const T*)(at[p] + (uint64_t)depth0 * sizeof(T)), at[p] != nullptr && d < depth_end ? (int)(depth_end - d) : 0, end);
+                q[p] = at[p] + (uint64_t)depth0 * sizeof(T);
+                exist = (at[p] != nullptr) & (d < depth_end) ? depth_end - d : 0;
             } else {
                 const uint32_t to = source != nullptr ? fdiv(row[p], slots) : row[p];
-                const bool there = row[p] < 1u << 31 && to < rows && free < free_end;
-                reg[p] = fetch_some((const T*)(base + to * row_bytes) + free, there ? (int)(free_end - free) : 0, end);
+                q[p] = base + to * row_bytes + (uint64_t)free * sizeof(T);
+                exist = (row[p] < 1u << 31) & (to < rows) & (free < free_end) ? free_end - free : 0;
             }
+            n[p] = (int)(exist < (uint32_t)V ? exist : (uint32_t)V);
+            left |= (uint32_t)n[p] << (8 * p);
+        }
+        if (moved) {
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) reg[p] = fetch_moved((const T*)q[p], n[p], base);
+        } else {
+            left = 0x01010101u * V;
+#pragma unroll
+            for (int p = 0; p < kFetches; ++p) reg[p] = fetch_some((const T*)q[p], n[p], end);
         }
     }
     __device__ __forceinline__ void put(char* tile) const {
@@ -384,7 +425,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
         constexpr uint32_t kPitch = LAYOUT == kDepthFast ? kStageBytes : FREE * sizeof(T);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p)
-            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), me % kAcross, kAcross) * 16) = reg[p];
+            *(u32x4*)(tile + lds_row(p) * kPitch + swizzle<T, LAYOUT>(lds_row(p), me % kAcross, kAcross) * 16) = straighten<T>(reg[p], (int)(left >> (8 * p) & 0xFFu));
     }
 };
 
@@ -421,7 +462,10 @@ template <typename T, int FREE, int THREADS, bool MAPPED, bool LOOSE> struct Cod
     const uint8_t *codes, *scales;
     const int32_t* source;
     uint32_t width, blocks, rows, free;
-    int free_there;
+    int free_there;     // elements from `free` to the row's end, 16 at most
+    bool moved;         // LOOSE: rows have 16 codes
+    uint32_t left;      // LOOSE: codes of each fetch that exist, a byte each
+    static_assert(kFetches <= 4, "a word");
     FastDiv slots;
     bool there;
     uint32_t row[MAPPED ? kFetches : 1];
@@ -432,7 +476,8 @@ template <typename T, int FREE, int THREADS, bool MAPPED, bool LOOSE> struct Cod
     __device__ __forceinline__ void start(uint32_t thread, const Operand& m, uint32_t free0, uint32_t free_end) {
         me = thread % THREADS;
         free = free0 + me % kAcross * 16;
-        there = free < free_end && lds_row(0) < kDepth, free_there = (int)(free_end - free);
+        there = free < free_end && lds_row(0) < kDepth, free_there = free < free_end ? (int)(free_end - free < 16 ? free_end - free : 16) : 0;
+        moved = kMoved<T, FREE> && m.rows > 0 && m.width >= 16;
         codes = (const uint8_t*)m.p, scales = m.scales, source = m.source;
         width = m.width, blocks = (m.width + 31) / 32, slots = m.slots, rows = m.rows;
     }
@@ -449,14 +494,19 @@ template <typename T, int FREE, int THREADS, bool MAPPED, bool LOOSE> struct Cod
     __device__ __forceinline__ void issue(char*, uint32_t depth0, uint32_t depth_end) {
         // rows that are not looked up are reached from the stage's first one: no limit to the tensor
         const uint64_t from = MAPPED ? 0 : depth0;
+        left = 0;
         const __amdgpu_buffer_rsrc_t c = buffer_at(codes + from * width), s = buffer_at(scales + from * blocks);
 #pragma unroll
         for (int p = 0; p < kFetches; ++p) {
             const uint32_t at = MAPPED ? fdiv(row[p], slots) : lds_row(p);
             const bool use = there & (MAPPED ? (row[p] < 1u << 31) & (at < rows) : depth0 + at < depth_end);
             const uint32_t code = at * width + free, scale_at = at * blocks + free / 32;
-            if constexpr (LOOSE) reg[p] = fetch_some(codes + (from + at) * width + free, use ? free_there : 0, (const char*)codes + (uint64_t)rows * width);
-            else reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? code : kBeyond), 0, 0);
+            if constexpr (LOOSE) {
+                const uint8_t* const q = codes + (from + at) * width + free;
+                const int n = use ? free_there : 0;
+                left |= (uint32_t)n << (8 * p);
+                reg[p] = moved ? fetch_moved(q, n, codes) : fetch_some(q, n, (const char*)codes + (uint64_t)rows * width);
+            } else reg[p] = __builtin_amdgcn_raw_buffer_load_b128(c, (int)(use ? code : kBeyond), 0, 0);
             scale[p] = __builtin_amdgcn_raw_buffer_load_b8(s, (int)(use ? scale_at : kBeyond), 0, 0);
         }
     }
@@ -470,9 +520,10 @@ template <typename T, int FREE, int THREADS, bool MAPPED, bool LOOSE> struct Cod
             char* const at = tile + d * (FREE * sizeof(T));
             const float by = power_of(scale[p]);
             const bool safe = __ballot(by > Range<T>::kSafe) == 0;
+            const u32x4 code = LOOSE && moved ? straighten<uint8_t>(reg[p], (int)(left >> (8 * p) & 0xFFu)) : reg[p];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const Vec<T, 8> v = elements_of<T>(u32x2{reg[p][2 * h], reg[p][2 * h + 1]}, by, safe);
+                const Vec<T, 8> v = elements_of<T>(u32x2{code[2 * h], code[2 * h + 1]}, by, safe);
                 if constexpr (sizeof(T) == 2) {
                     *(Vec<T, 8>*)(at + swizzle<T, kFreeFast>(d, 2 * c + h, kChunks) * 16) = v;
                 } else {
