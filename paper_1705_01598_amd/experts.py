@@ -9,8 +9,8 @@ expert, the two products with the gated activation between them and the combinat
 reads tokens through the sorted order, so rows are never gathered into a buffer.  For the backward pass the layer
 keeps the input and the gates in 8 bits (``tperm_checkpoint_store``, ``tperm_gated_forward``); the input's rows
 are multiplied out of their codes.  Everything here is argument bookkeeping around the calls of
-``include/tperm_experts.h``; tensors are dense and contiguous, on one GPU, and work
-is enqueued on the current stream (a layer is used on one stream at a time).
+``include/tperm_experts.h``; tensors are dense and contiguous, on the layer's GPU, and work is enqueued on
+that GPU's current stream, whichever GPU is the current one (a layer is used on one stream at a time).
 """
 from __future__ import annotations
 
@@ -21,7 +21,8 @@ _NAMES = {"torch.float32": "f32", "torch.float16": "f16", "torch.bfloat16": "bf1
 
 class ExpertLayer:
     """The operators of one layer shape, and the buffers between them, which are kept and reused for the largest number
-    of tokens met so far: a forward pass overwrites what the one before it kept."""
+    of tokens met so far: a forward pass overwrites what the one before it kept.  ``device`` without a number ("cuda")
+    becomes that of the first tensors; from then on tensors of another device are refused."""
 
     def __init__(self, experts: int, slots: int, width: int, hidden: int, dtype, device="cuda"):
         import torch
@@ -51,9 +52,15 @@ class ExpertLayer:
             self._room = tokens
         return {k: t.data_ptr() for k, t in self._b.items()}
 
-    def _check(self, name: str, t, shape: Tuple[int, ...], dtype) -> None:
-        if tuple(t.shape) != shape or t.dtype != dtype or t.device.type != self._device.type or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on {self._device} is wanted")
+    def _check(self, name: str, t, shape: Tuple[int, ...], dtype, device) -> None:
+        if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on {device} is wanted")
+
+    def _gpu(self):
+        """The layer's GPU as the current one, while calls are enqueued."""
+        if self._device.type != "cuda":
+            raise ValueError("the layer computes on a GPU: no host tensors")
+        return self._torch.cuda.device(self._device)
 
     def forward(self, x, expert, weights, w_in, w_out):
         """The layer's result for x [tokens, width]; expert [tokens, slots] int32 (a number outside 0 .. experts-1 names
@@ -62,23 +69,26 @@ class ExpertLayer:
         e, k, w, h, t = self.experts, self.slots, self.width, self.hidden, self._type
         tokens = x.shape[0]
         rows = tokens * k
-        self._check("x", x, (tokens, w), self.dtype)
-        self._check("expert", expert, (tokens, k), torch.int32)
-        self._check("weights", weights, (tokens, k), torch.float32)
-        self._check("w_in", w_in, (e, 2 * h, w), self.dtype)
-        self._check("w_out", w_out, (e, w, h), self.dtype)
+        device = x.device if self._device.index is None and x.device.type == self._device.type else self._device
+        self._check("x", x, (tokens, w), self.dtype, device)
+        self._check("expert", expert, (tokens, k), torch.int32, device)
+        self._check("weights", weights, (tokens, k), torch.float32, device)
+        self._check("w_in", w_in, (e, 2 * h, w), self.dtype, device)
+        self._check("w_out", w_out, (e, w, h), self.dtype, device)
+        self._device = device
         out = torch.empty_like(x)
         if tokens == 0:
             self._kept = (x, weights, w_in, w_out)
             return out
-        b = self._buffers(tokens)
-        s = torch.cuda.current_stream().cuda_stream
-        B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], b["sort"], self._b["sort"].numel(), s)
-        B.tperm_checkpoint_store(x.data_ptr(), w, b["x_codes"], b["x_scales"], tokens, w, t, s)
-        B.tperm_expert_product(x.data_ptr(), w, tokens, b["source"], k, b["offsets"], w_in.data_ptr(), True, b["gates"], 2 * h, rows, e, w, 2 * h, t, s)
-        B.tperm_gated_forward(b["gates"], 2 * h, b["hidden"], h, b["gate_codes"], b["gate_scales"], rows, h, t, s)
-        B.tperm_expert_product(b["hidden"], h, rows, None, 1, b["offsets"], w_out.data_ptr(), True, b["rows"], w, rows, e, h, w, t, s)
-        B.tperm_expert_combine(b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), out.data_ptr(), w, tokens, k, e, w, t, s)
+        with self._gpu():
+            b = self._buffers(tokens)
+            s = torch.cuda.current_stream().cuda_stream
+            B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], b["sort"], self._b["sort"].numel(), s)
+            B.tperm_checkpoint_store(x.data_ptr(), w, b["x_codes"], b["x_scales"], tokens, w, t, s)
+            B.tperm_expert_product(x.data_ptr(), w, tokens, b["source"], k, b["offsets"], w_in.data_ptr(), True, b["gates"], 2 * h, rows, e, w, 2 * h, t, s)
+            B.tperm_gated_forward(b["gates"], 2 * h, b["hidden"], h, b["gate_codes"], b["gate_scales"], rows, h, t, s)
+            B.tperm_expert_product(b["hidden"], h, rows, None, 1, b["offsets"], w_out.data_ptr(), True, b["rows"], w, rows, e, h, w, t, s)
+            B.tperm_expert_combine(b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), out.data_ptr(), w, tokens, k, e, w, t, s)
         self._kept = (x, weights, w_in, w_out)
         return out
 
@@ -92,29 +102,30 @@ class ExpertLayer:
         x, weights, w_in, w_out = self._kept
         tokens = x.shape[0]
         rows = tokens * k
-        self._check("grad", grad, (tokens, w), self.dtype)
-        self._check("grad_w_in", grad_w_in, (e, 2 * h, w), torch.float32)
-        self._check("grad_w_out", grad_w_out, (e, w, h), torch.float32)
+        self._check("grad", grad, (tokens, w), self.dtype, self._device)
+        self._check("grad_w_in", grad_w_in, (e, 2 * h, w), torch.float32, self._device)
+        self._check("grad_w_out", grad_w_out, (e, w, h), torch.float32, self._device)
         grad_x, grad_weights = torch.empty_like(x), torch.empty_like(weights)
         if tokens == 0:
             if not accumulate:
                 grad_w_in.zero_(), grad_w_out.zero_()
             return grad_x, grad_weights
-        b = self._buffers(tokens)
-        s = torch.cuda.current_stream().cuda_stream
-        B.tperm_expert_combine_backward(grad.data_ptr(), w, b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), b["grad_rows"], w,
-                                        grad_weights.data_ptr(), tokens, k, e, w, t, s)
-        # to the hidden rows: the same matrices, the other index summed
-        B.tperm_expert_product(b["grad_rows"], w, rows, None, 1, b["offsets"], w_out.data_ptr(), False, b["hidden"], h, rows, e, w, h, t, s)
-        # the gates' gradient takes the gates' place; the hidden rows again, for their matrix, in the rows' place
-        again = b["rows"] if h <= w else self._again(rows)
-        B.tperm_gated_backward(b["hidden"], h, b["gate_codes"], b["gate_scales"], b["gates"], 2 * h, again, h, rows, h, t, s)
-        B.tperm_expert_weight_gradient(again, h, None, rows, None, 1, b["grad_rows"], w, b["offsets"], grad_w_out.data_ptr(), f32, True, accumulate,
-                                       rows, e, h, w, t, s)
-        B.tperm_expert_weight_gradient(b["x_codes"], w, b["x_scales"], tokens, b["source"], k, b["gates"], 2 * h, b["offsets"], grad_w_in.data_ptr(), f32, True,
-                                       accumulate, rows, e, w, 2 * h, t, s)
-        B.tperm_expert_product(b["gates"], 2 * h, rows, None, 1, b["offsets"], w_in.data_ptr(), False, b["grad_rows"], w, rows, e, 2 * h, w, t, s)
-        B.tperm_expert_combine(b["grad_rows"], w, b["place"], b["offsets"], None, grad_x.data_ptr(), w, tokens, k, e, w, t, s)
+        with self._gpu():
+            b = self._buffers(tokens)
+            s = torch.cuda.current_stream().cuda_stream
+            B.tperm_expert_combine_backward(grad.data_ptr(), w, b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), b["grad_rows"], w,
+                                            grad_weights.data_ptr(), tokens, k, e, w, t, s)
+            # to the hidden rows: the same matrices, the other index summed
+            B.tperm_expert_product(b["grad_rows"], w, rows, None, 1, b["offsets"], w_out.data_ptr(), False, b["hidden"], h, rows, e, w, h, t, s)
+            # the gates' gradient takes the gates' place; the hidden rows again, for their matrix, in the rows' place
+            again = b["rows"] if h <= w else self._again(rows)
+            B.tperm_gated_backward(b["hidden"], h, b["gate_codes"], b["gate_scales"], b["gates"], 2 * h, again, h, rows, h, t, s)
+            B.tperm_expert_weight_gradient(again, h, None, rows, None, 1, b["grad_rows"], w, b["offsets"], grad_w_out.data_ptr(), f32, True, accumulate,
+                                           rows, e, h, w, t, s)
+            B.tperm_expert_weight_gradient(b["x_codes"], w, b["x_scales"], tokens, b["source"], k, b["gates"], 2 * h, b["offsets"], grad_w_in.data_ptr(), f32, True,
+                                           accumulate, rows, e, w, 2 * h, t, s)
+            B.tperm_expert_product(b["gates"], 2 * h, rows, None, 1, b["offsets"], w_in.data_ptr(), False, b["grad_rows"], w, rows, e, 2 * h, w, t, s)
+            B.tperm_expert_combine(b["grad_rows"], w, b["place"], b["offsets"], None, grad_x.data_ptr(), w, tokens, k, e, w, t, s)
         self._kept = None
         return grad_x, grad_weights
 
@@ -129,11 +140,13 @@ class ExpertLayer:
             raise RuntimeError("no forward pass is kept")
         torch, B = self._torch, self._B
         rows, h = self._kept[0].shape[0] * self.slots, self.hidden
-        b, blocks = self._buffers(self._kept[0].shape[0]), B.checkpoint_blocks(h)
+        blocks = B.checkpoint_blocks(h)
         # g and u of a row are checkpoints beside each other: as 2 * rows rows of h
         out = torch.empty(rows, 2 * h, dtype=torch.float32, device=self._device)
         assert self._b["gate_scales"].numel() >= rows * 2 * blocks
-        B.tperm_checkpoint_load(b["gate_codes"], b["gate_scales"], out.data_ptr(), h, 2 * rows, h, B.TYPE_F32, torch.cuda.current_stream().cuda_stream)
+        with self._gpu():
+            b = self._buffers(self._kept[0].shape[0])
+            B.tperm_checkpoint_load(b["gate_codes"], b["gate_scales"], out.data_ptr(), h, 2 * rows, h, B.TYPE_F32, torch.cuda.current_stream().cuda_stream)
         return out
 
 
