@@ -81,6 +81,7 @@ class ExpertLayer:
             self._kept = (x, weights, w_in, w_out)
             return out
         with self._gpu():
+            self._kept = None       # the buffers of the pass before are overwritten from here on, whether this one succeeds or not
             b = self._buffers(tokens)
             s = torch.cuda.current_stream().cuda_stream
             B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], b["sort"], self._b["sort"].numel(), s)
@@ -106,6 +107,7 @@ class ExpertLayer:
         self._check("grad_w_in", grad_w_in, (e, 2 * h, w), torch.float32, self._device)
         self._check("grad_w_out", grad_w_out, (e, w, h), torch.float32, self._device)
         grad_x, grad_weights = torch.empty_like(x), torch.empty_like(weights)
+        self._kept = None           # what it reads is overwritten, and the matrices' gradients must not be added to twice
         if tokens == 0:
             if not accumulate:
                 grad_w_in.zero_(), grad_w_out.zero_()
@@ -126,7 +128,6 @@ class ExpertLayer:
                                            accumulate, rows, e, w, 2 * h, t, s)
             B.tperm_expert_product(b["gates"], 2 * h, rows, None, 1, b["offsets"], w_in.data_ptr(), False, b["grad_rows"], w, rows, e, 2 * h, w, t, s)
             B.tperm_expert_combine(b["grad_rows"], w, b["place"], b["offsets"], None, grad_x.data_ptr(), w, tokens, k, e, w, t, s)
-        self._kept = None
         return grad_x, grad_weights
 
     def _again(self, rows: int) -> int:

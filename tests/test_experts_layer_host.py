@@ -147,3 +147,51 @@ def test_host_memory_goes_to_no_kernel():
     with pytest.raises(ValueError):
         layer.forward(*inputs("cpu"))
     assert not layer._B.calls
+
+
+def test_nothing_is_left_of_a_forward_pass_that_fails():
+    """Its first calls, or larger buffers, have taken the place of what the pass before it kept."""
+    for failing in ("tperm_expert_sort", "tperm_expert_product", "tperm_expert_combine"):
+        for tokens in (5, 50):
+            layer = layer_on("cuda:1")
+            layer.forward(*inputs("cuda:1"))
+            layer._B.failing = failing
+            with pytest.raises(binding.TpermError):
+                layer.forward(*inputs("cuda:1", tokens))
+            layer._B.failing = None
+            for late in (lambda: layer.backward(*gradients("cuda:1")), lambda: layer.backward(*gradients("cuda:1", tokens)), layer.kept_gates):
+                with pytest.raises(RuntimeError, match="forward"):
+                    late()
+
+
+def test_a_refused_forward_pass_leaves_the_one_before():
+    layer = layer_on("cuda:1")
+    layer.forward(*inputs("cuda:1"))
+    with pytest.raises(ValueError):
+        layer.forward(*inputs("cuda:0"))
+    layer.backward(*gradients("cuda:1"))
+
+
+def test_a_backward_pass_that_fails_is_not_run_again():
+    """It has written over the kept rows, and may have added to the gradients."""
+    for failing in ("tperm_expert_combine_backward", "tperm_expert_weight_gradient", "tperm_expert_combine"):
+        layer = layer_on("cuda:1")
+        layer.forward(*inputs("cuda:1"))
+        layer._B.failing = failing
+        with pytest.raises(binding.TpermError):
+            layer.backward(*gradients("cuda:1"))
+        layer._B.failing = None
+        with pytest.raises(RuntimeError, match="forward"):
+            layer.backward(*gradients("cuda:1"))
+    layer.forward(*inputs("cuda:1"))
+    with pytest.raises(ValueError):             # arguments are looked at first: this one may be run again
+        layer.backward(*gradients("cuda:0"))
+    layer.backward(*gradients("cuda:1"))
+
+
+def test_one_backward_pass_to_a_forward_pass_without_tokens_too():
+    layer = layer_on("cuda:1")
+    layer.forward(*inputs("cuda:1", 0))
+    layer.backward(*gradients("cuda:1", 0))
+    with pytest.raises(RuntimeError, match="forward"):
+        layer.backward(*gradients("cuda:1", 0))
