@@ -144,6 +144,8 @@ class ExpertLayer:
         blocks = B.checkpoint_blocks(h)
         # g and u of a row are checkpoints beside each other: as 2 * rows rows of h
         out = torch.empty(rows, 2 * h, dtype=torch.float32, device=self._device)
+        if rows == 0:
+            return out
         assert self._b["gate_scales"].numel() >= rows * 2 * blocks
         with self._gpu():
             b = self._buffers(self._kept[0].shape[0])

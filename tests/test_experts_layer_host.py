@@ -195,3 +195,9 @@ def test_one_backward_pass_to_a_forward_pass_without_tokens_too():
     layer.backward(*gradients("cuda:1", 0))
     with pytest.raises(RuntimeError, match="forward"):
         layer.backward(*gradients("cuda:1", 0))
+
+
+def test_kept_gates_of_no_tokens():
+    layer = layer_on("cuda:1")
+    layer.forward(*inputs("cuda:1", 0))
+    assert layer.kept_gates().shape == (0, 2 * HIDDEN)
