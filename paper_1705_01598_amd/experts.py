@@ -20,8 +20,10 @@ _NAMES = {"torch.float32": "f32", "torch.float16": "f16", "torch.bfloat16": "bf1
 
 
 class ExpertLayer:
-    """The operators of one layer shape, and the buffers between them, which are kept and reused for the largest number
-    of tokens met so far: a forward pass overwrites what the one before it kept.  ``device`` without a number ("cuda")
+    """The operators of one layer shape, and what a forward pass keeps for the backward pass: the maps, the input and the
+    gates in 8 bits and the rows that the experts gave, in buffers that are reused for the largest number of tokens met so far, so that a
+    forward pass overwrites what the one before it kept.  What a pass needs beside that goes back to the allocator
+    at its end.  ``device`` without a number ("cuda")
     becomes that of the first tensors; from then on tensors of another device are refused."""
 
     def __init__(self, experts: int, slots: int, width: int, hidden: int, dtype, device="cuda"):
@@ -43,14 +45,27 @@ class ExpertLayer:
             torch, B = self._torch, self._B
             rows, w, h = tokens * self.slots, self.width, self.hidden
             new = lambda *shape, dtype=self.dtype: torch.empty(*shape, dtype=dtype, device=self._device)  # noqa: E731
-            need = B.expert_sort_workspace_bytes(rows, self.experts)
             i32, u8 = torch.int32, torch.uint8
             self._b = {"offsets": new(self.experts + 1, dtype=i32), "source": new(rows, dtype=i32), "place": new(rows, dtype=i32),
-                       "sort": new(need, dtype=u8), "x_codes": new(tokens * w, dtype=u8), "x_scales": new(tokens * B.checkpoint_blocks(w), dtype=u8),
-                       "gates": new(rows, 2 * h), "gate_codes": new(rows * 2 * h, dtype=u8), "gate_scales": new(rows * 2 * B.checkpoint_blocks(h), dtype=u8),
-                       "hidden": new(rows, h), "rows": new(rows, w), "grad_rows": new(rows, w)}
+                       "x_codes": new(tokens * w, dtype=u8), "x_scales": new(tokens * B.checkpoint_blocks(w), dtype=u8),
+                       "gate_codes": new(rows * 2 * h, dtype=u8), "gate_scales": new(rows * 2 * B.checkpoint_blocks(h), dtype=u8),
+                       "rows": new(rows, w)}
             self._room = tokens
         return {k: t.data_ptr() for k, t in self._b.items()}
+
+    def _scratch(self, *sizes: int):
+        """One buffer for a pass's own arrays of so many bytes each: the buffer, and where each of them starts in it."""
+        starts, end = [], 0
+        for n in sizes:
+            starts.append(end)
+            end += -(-n // 256) * 256
+        buffer = self._torch.empty(end, dtype=self._torch.uint8, device=self._device)
+        at = buffer.data_ptr()
+        return (buffer, *(at + start for start in starts))
+
+    def kept_bytes(self) -> int:
+        """Bytes of GPU memory that the layer holds between its passes."""
+        return sum(t.numel() * t.element_size() for t in self._b.values())
 
     def _check(self, name: str, t, shape: Tuple[int, ...], dtype, device) -> None:
         if tuple(t.shape) != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
@@ -78,19 +93,21 @@ class ExpertLayer:
         self._device = device
         out = torch.empty_like(x)
         if tokens == 0:
-            self._kept = (x, weights, w_in, w_out)
+            self._kept = (tokens, weights, w_in, w_out)
             return out
         with self._gpu():
             self._kept = None       # the buffers of the pass before are overwritten from here on, whether this one succeeds or not
             b = self._buffers(tokens)
+            need = B.expert_sort_workspace_bytes(rows, e)
+            scratch, gates, hidden, sort = self._scratch(rows * 2 * h * x.element_size(), rows * h * x.element_size(), need)    # held to the last call
             s = torch.cuda.current_stream().cuda_stream
-            B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], b["sort"], self._b["sort"].numel(), s)
+            B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], sort, need, s)
             B.tperm_checkpoint_store(x.data_ptr(), w, b["x_codes"], b["x_scales"], tokens, w, t, s)
-            B.tperm_expert_product(x.data_ptr(), w, tokens, b["source"], k, b["offsets"], w_in.data_ptr(), True, b["gates"], 2 * h, rows, e, w, 2 * h, t, s)
-            B.tperm_gated_forward(b["gates"], 2 * h, b["hidden"], h, b["gate_codes"], b["gate_scales"], rows, h, t, s)
-            B.tperm_expert_product(b["hidden"], h, rows, None, 1, b["offsets"], w_out.data_ptr(), True, b["rows"], w, rows, e, h, w, t, s)
+            B.tperm_expert_product(x.data_ptr(), w, tokens, b["source"], k, b["offsets"], w_in.data_ptr(), True, gates, 2 * h, rows, e, w, 2 * h, t, s)
+            B.tperm_gated_forward(gates, 2 * h, hidden, h, b["gate_codes"], b["gate_scales"], rows, h, t, s)
+            B.tperm_expert_product(hidden, h, rows, None, 1, b["offsets"], w_out.data_ptr(), True, b["rows"], w, rows, e, h, w, t, s)
             B.tperm_expert_combine(b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), out.data_ptr(), w, tokens, k, e, w, t, s)
-        self._kept = (x, weights, w_in, w_out)
+        self._kept = (tokens, weights, w_in, w_out)
         return out
 
     def backward(self, grad, grad_w_in, grad_w_out, accumulate: bool = True):
@@ -100,13 +117,12 @@ class ExpertLayer:
             raise RuntimeError("backward() without a forward()")
         torch, B = self._torch, self._B
         e, k, w, h, t, f32 = self.experts, self.slots, self.width, self.hidden, self._type, self._B.TYPE_F32
-        x, weights, w_in, w_out = self._kept
-        tokens = x.shape[0]
+        tokens, weights, w_in, w_out = self._kept
         rows = tokens * k
         self._check("grad", grad, (tokens, w), self.dtype, self._device)
         self._check("grad_w_in", grad_w_in, (e, 2 * h, w), torch.float32, self._device)
         self._check("grad_w_out", grad_w_out, (e, w, h), torch.float32, self._device)
-        grad_x, grad_weights = torch.empty_like(x), torch.empty_like(weights)
+        grad_x, grad_weights = torch.empty_like(grad), torch.empty_like(weights)
         self._kept = None           # what it reads is overwritten, and the matrices' gradients must not be added to twice
         if tokens == 0:
             if not accumulate:
@@ -114,33 +130,30 @@ class ExpertLayer:
             return grad_x, grad_weights
         with self._gpu():
             b = self._buffers(tokens)
+            # the hidden rows again, for their matrix, take the rows' place where they fit
+            size, fits = grad.element_size(), h <= w
+            scratch, grad_rows, hidden, gates, again = self._scratch(rows * w * size, rows * h * size, rows * 2 * h * size, 0 if fits else rows * h * size)
+            again = b["rows"] if fits else again
             s = torch.cuda.current_stream().cuda_stream
-            B.tperm_expert_combine_backward(grad.data_ptr(), w, b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), b["grad_rows"], w,
+            B.tperm_expert_combine_backward(grad.data_ptr(), w, b["rows"], w, b["place"], b["offsets"], weights.data_ptr(), grad_rows, w,
                                             grad_weights.data_ptr(), tokens, k, e, w, t, s)
             # to the hidden rows: the same matrices, the other index summed
-            B.tperm_expert_product(b["grad_rows"], w, rows, None, 1, b["offsets"], w_out.data_ptr(), False, b["hidden"], h, rows, e, w, h, t, s)
-            # the gates' gradient takes the gates' place; the hidden rows again, for their matrix, in the rows' place
-            again = b["rows"] if h <= w else self._again(rows)
-            B.tperm_gated_backward(b["hidden"], h, b["gate_codes"], b["gate_scales"], b["gates"], 2 * h, again, h, rows, h, t, s)
-            B.tperm_expert_weight_gradient(again, h, None, rows, None, 1, b["grad_rows"], w, b["offsets"], grad_w_out.data_ptr(), f32, True, accumulate,
+            B.tperm_expert_product(grad_rows, w, rows, None, 1, b["offsets"], w_out.data_ptr(), False, hidden, h, rows, e, w, h, t, s)
+            B.tperm_gated_backward(hidden, h, b["gate_codes"], b["gate_scales"], gates, 2 * h, again, h, rows, h, t, s)
+            B.tperm_expert_weight_gradient(again, h, None, rows, None, 1, grad_rows, w, b["offsets"], grad_w_out.data_ptr(), f32, True, accumulate,
                                            rows, e, h, w, t, s)
-            B.tperm_expert_weight_gradient(b["x_codes"], w, b["x_scales"], tokens, b["source"], k, b["gates"], 2 * h, b["offsets"], grad_w_in.data_ptr(), f32, True,
+            B.tperm_expert_weight_gradient(b["x_codes"], w, b["x_scales"], tokens, b["source"], k, gates, 2 * h, b["offsets"], grad_w_in.data_ptr(), f32, True,
                                            accumulate, rows, e, w, 2 * h, t, s)
-            B.tperm_expert_product(b["gates"], 2 * h, rows, None, 1, b["offsets"], w_in.data_ptr(), False, b["grad_rows"], w, rows, e, 2 * h, w, t, s)
-            B.tperm_expert_combine(b["grad_rows"], w, b["place"], b["offsets"], None, grad_x.data_ptr(), w, tokens, k, e, w, t, s)
+            B.tperm_expert_product(gates, 2 * h, rows, None, 1, b["offsets"], w_in.data_ptr(), False, grad_rows, w, rows, e, 2 * h, w, t, s)
+            B.tperm_expert_combine(grad_rows, w, b["place"], b["offsets"], None, grad_x.data_ptr(), w, tokens, k, e, w, t, s)
         return grad_x, grad_weights
-
-    def _again(self, rows: int) -> int:
-        if "again" not in self._b:
-            self._b["again"] = self._torch.empty(self._room * self.slots, self.hidden, dtype=self.dtype, device=self._device)
-        return self._b["again"].data_ptr()
 
     def kept_gates(self):
         """[g, u] of the sorted rows as the backward pass will see them, in float32 (the values that the codes stand for)."""
         if self._kept is None:
             raise RuntimeError("no forward pass is kept")
         torch, B = self._torch, self._B
-        rows, h = self._kept[0].shape[0] * self.slots, self.hidden
+        rows, h = self._kept[0] * self.slots, self.hidden
         blocks = B.checkpoint_blocks(h)
         # g and u of a row are checkpoints beside each other: as 2 * rows rows of h
         out = torch.empty(rows, 2 * h, dtype=torch.float32, device=self._device)
@@ -148,7 +161,7 @@ class ExpertLayer:
             return out
         assert self._b["gate_scales"].numel() >= rows * 2 * blocks
         with self._gpu():
-            b = self._buffers(self._kept[0].shape[0])
+            b = self._buffers(self._kept[0])
             B.tperm_checkpoint_load(b["gate_codes"], b["gate_scales"], out.data_ptr(), h, 2 * rows, h, B.TYPE_F32, torch.cuda.current_stream().cuda_stream)
         return out
 
@@ -199,7 +212,7 @@ def _bench(argv=None):
     print(json.dumps({"metric": "mixture-of-experts layer, forward and backward", "tokens": a.tokens, "experts": a.experts, "slots": a.slots, "width": a.width,
                       "hidden": a.hidden, "dtype": a.dtype, "forward_ms": round(forward, 4), "forward_backward_ms": round(total, 4),
                       "forward_tflops": round(flops / forward / 1e9, 1), "forward_backward_tflops": round(3 * flops / total / 1e9, 1),
-                      "kept_bytes_per_token": round((a.width + a.slots * 2 * a.hidden) * 33 / 32 + a.slots * a.width * x.element_size())}), flush=True)
+                      "kept_bytes_per_token": round(layer.kept_bytes() / a.tokens)}), flush=True)
 
 
 if __name__ == "__main__":

@@ -1,6 +1,8 @@
 """What the mixture-of-experts layer does around its calls, with stand-ins for torch and the library that record
 them: on which GPU and stream they are enqueued, and what is left of a pass that fails.  No GPU is needed."""
 import contextlib
+import gc
+import weakref
 
 import pytest
 
@@ -32,11 +34,6 @@ class Tensor:
 
     def element_size(self):
         return self.dtype.itemsize
-
-    def __getitem__(self, piece):       # a piece of a buffer of bytes
-        t = Tensor(piece.stop - (piece.start or 0), dtype=self.dtype, device=self.device)
-        t._at = self._at + (piece.start or 0)
-        return t
 
     def zero_(self):
         return self
@@ -201,3 +198,32 @@ def test_kept_gates_of_no_tokens():
     layer = layer_on("cuda:1")
     layer.forward(*inputs("cuda:1", 0))
     assert layer.kept_gates().shape == (0, 2 * HIDDEN)
+
+
+def test_what_stays_between_the_passes_is_in_8_bits():
+    """Input and gates stay as codes and scales, the rows that the experts gave and the maps as they are; the input itself,
+    the gates and the hidden rows go back to the allocator."""
+    tokens = 500
+    layer = layer_on("cuda:1")
+    made = []
+    empty = layer._torch.empty
+
+    def recorded(*shape, dtype, device):
+        t = empty(*shape, dtype=dtype, device=device)
+        made.append(weakref.ref(t))
+        return t
+
+    layer._torch.empty = recorded
+    given = inputs("cuda:1", tokens)
+    x = weakref.ref(given[0])
+    layer.forward(*given)
+    del given
+    gc.collect()
+    assert x() is None
+    alive = sum(t().numel() * t().element_size() for t in made if t() is not None)
+    rows, blocks = tokens * SLOTS, binding.checkpoint_blocks
+    kept = tokens * (WIDTH + blocks(WIDTH)) + rows * 2 * (HIDDEN + blocks(HIDDEN)) + rows * WIDTH * 2 + (2 * rows + EXPERTS + 1) * 4
+    assert alive == kept == layer.kept_bytes()
+    layer.backward(*gradients("cuda:1", tokens))
+    gc.collect()
+    assert sum(t().numel() * t().element_size() for t in made if t() is not None) == kept
