@@ -1,0 +1,28 @@
+"""Inline assembly of the device code tells the compiler what it changes (read from the sources; no GPU)."""
+import glob
+import os
+import re
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def _blocks():
+    for path in sorted(glob.glob(os.path.join(ROOT, "paper_1705_01598_amd", "csrc", "*.h*"))):
+        text = open(path).read()
+        for start in re.finditer(r"\basm\s+volatile\s*\(|\basm\s*\(", text):
+            depth, at = 1, start.end()
+            while depth:
+                depth += {"(": 1, ")": -1}.get(text[at], 0)
+                at += 1
+            yield os.path.basename(path), text[start.end():at - 1]
+
+
+def test_loads_in_assembly_keep_their_distance_from_the_scalars_they_read():
+    """Five wait states between a vector instruction that writes a scalar register (a broadcast of a lane) and a
+    vector memory instruction that reads it; inside an assembly block the compiler puts in none."""
+    found = 0
+    for name, block in _blocks():
+        if re.search(r"(buffer|global|flat|scratch)_(load|store|atomic)", block):
+            found += 1
+            assert re.search(r's_nop 4\\n\\t(buffer|global|flat|scratch)_', block), (name, block)
+    assert found
