@@ -170,13 +170,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
 
 // 16 bytes a lane from base + offset + scalar to 1 KiB of LDS from `to` on.  Written out: behind the builtin the
 // compiler lets the next transposing read, of another image, wait for all loads (2.1 us a stage instead of 1.4).  It
-// has no result for the compiler to see; arrive() waits for it.  A scalar register that a vector instruction wrote, as
+// has no result for the compiler to see: arrive() waits for it, and what keeps it behind the reads of the image that it
+// overwrites is the "memory" of arrive() alone.  A scalar register that a vector instruction wrote, as
 // uniform() does, may be read by a vector memory instruction five wait states later at the earliest: s_nop 4 is those, since
 // the compiler counts none for what is written out here.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t to, uint32_t offset, uint32_t scalar) {
     const uint64_t p = (uint64_t)base;
     const u32x4 buffer = {uniform((uint32_t)p), uniform((uint32_t)(p >> 32)) & 0xFFFFu, kBeyond, 0x00020000u};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(offset), "s"(buffer), "s"(scalar));
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(to), "v"(offset), "s"(buffer), "s"(scalar));
 }
 
 // Waits until at most LOADS of this wavefront's loads are under way and its LDS accesses are done, then for the other

@@ -26,3 +26,12 @@ def test_loads_in_assembly_keep_their_distance_from_the_scalars_they_read():
             found += 1
             assert re.search(r's_nop 4\\n\\t(buffer|global|flat|scratch)_', block), (name, block)
     assert found
+
+
+def test_assembly_leaves_m0_to_the_compiler():
+    """A block that needs a value in m0 takes it as an operand: written inside, the compiler would not know."""
+    found = 0
+    for name, block in _blocks():
+        assert not re.search(r"\bm0\s*,", block), (name, block)
+        found += '"{m0}"' in block
+    assert found
