@@ -171,13 +171,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void* p) {
 // 16 bytes a lane from base + offset + scalar to 1 KiB of LDS from `to` on.  Written out: behind the builtin the
 // compiler lets the next transposing read, of another image, wait for all loads (2.1 us a stage instead of 1.4).  It
 // has no result for the compiler to see: arrive() waits for it, and what keeps it behind the reads of the image that it
-// overwrites is the "memory" of arrive() alone.  A scalar register that a vector instruction wrote, as
-// uniform() does, may be read by a vector memory instruction five wait states later at the earliest: s_nop 4 is those, since
-// the compiler counts none for what is written out here.
-__device__ __forceinline__ void load_to_lds(const void* base, uint32_t to, uint32_t offset, uint32_t scalar) {
-    const uint64_t p = (uint64_t)base;
-    const u32x4 buffer = {uniform((uint32_t)p), uniform((uint32_t)(p >> 32)) & 0xFFFFu, kBeyond, 0x00020000u};
-    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(to), "v"(offset), "s"(buffer), "s"(scalar));
+// overwrites is the "memory" of arrive() alone.  What it reads comes from settled() and scalar arithmetic.
+__device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t to, uint32_t offset, uint32_t scalar) {
+    const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, kBeyond, 0x00020000u};
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"{m0}"(to), "v"(offset), "s"(buffer), "s"(scalar));
+}
+
+// Values that all lanes have, in scalar registers that such a load may read: five wait states after a vector instruction wrote
+// them at the earliest, and the compiler counts none for instructions that are written out.  Here they pass once for a
+// tile; with every load, or every stage, the products lose 1 to 4 % of a call.
+__device__ __forceinline__ void settled(uint64_t& base, uint32_t& row_bytes, uint32_t& to) {
+    base = (uint64_t)uniform((uint32_t)(base >> 32)) << 32 | uniform((uint32_t)base), row_bytes = uniform(row_bytes), to = uniform(to);
+    asm volatile("s_nop 4" : "+s"(base), "+s"(row_bytes), "+s"(to));
 }
 
 // Waits until at most LOADS of this wavefront's loads are under way and its LDS accesses are done, then for the other
@@ -198,8 +203,8 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     static constexpr uint32_t kAcross = LAYOUT == kDepthFast ? 8 : FREE * sizeof(T) / 16;   // chunks of an LDS row
     static constexpr uint32_t kRowsPerFetch = THREADS / kAcross;
     static_assert(kFetches * THREADS * 16 == FREE * kStageBytes && kRowsPerFetch * kAcross == THREADS, "whole passes");
-    const char* base;
-    uint32_t row_bytes;
+    uint64_t base;
+    uint32_t row_bytes, to;             // to: of the wavefront's part of an image
     uint32_t off[kFetches];             // from base (kDepthFast: + depth; kFreeFast: + stage, MAPPED: of the column alone)
     // MAPPED: memory rows that a wavefront's lanes read in each fetch; two are kept in scalar registers (the 16 a
     // stage of narrower tiles take longer than a look-up by every lane: 35 us against 25, 2048 rows of 8 experts)
@@ -219,7 +224,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
         row_bytes = (uint32_t)(m.stride * sizeof(T));
         source = m.source, slots = m.slots, rows = m.rows;
         if constexpr (LAYOUT == kDepthFast) {
-            base = (const char*)m.p + (m.source != nullptr ? 0 : (int64_t)free0 * row_bytes);
+            base = (uint64_t)m.p + (m.source != nullptr ? 0 : (uint64_t)free0 * row_bytes);
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) {
                 uint32_t r = free0 + lds_row(p), at;
@@ -227,13 +232,15 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
                 if (r < free_end && m.find(r, &at)) off[p] = (m.source != nullptr ? at : at - free0) * row_bytes + chunk(p) * 16;
             }
         } else {
-            base = (const char*)m.p;
+            base = (uint64_t)m.p;
 #pragma unroll
             for (int p = 0; p < kFetches; ++p) {
                 const uint32_t f = free0 + chunk(p) * V;
                 off[p] = f < free_end ? f * (uint32_t)sizeof(T) + (MAPPED ? 0u : lds_row(p) * row_bytes) : kBeyond;
             }
         }
+        to = (me & ~63u) * 16;
+        settled(base, row_bytes, to);
     }
     // MAPPED: entries of source for the stage at `depth0`.
     __device__ __forceinline__ void look_up(uint32_t depth0, uint32_t depth_end) {
@@ -264,8 +271,8 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
     }
     __device__ __forceinline__ void issue(char* tile, uint32_t depth0, uint32_t depth_end, int part = 0, int parts = 1) {
         const uint32_t left = depth0 < depth_end ? depth_end - depth0 : 0;      // beyond the end: zeros
-        const uint32_t to = uniform((uint32_t)(uintptr_t)(TPERM_LDS char*)tile + (me & ~63u) * 16);
-        const char* from = base;
+        const uint32_t at_lds = (uint32_t)(uintptr_t)(TPERM_LDS char*)tile + to;
+        uint64_t from = base;
         uint32_t scalar = 0;
         if constexpr (LAYOUT == kDepthFast) scalar = depth0 * (uint32_t)sizeof(T);
         else if constexpr (!MAPPED) from += (uint64_t)depth0 * row_bytes;
@@ -294,7 +301,7 @@ template <typename T, int LAYOUT, int FREE, int THREADS, bool MAPPED> struct Dir
             } else {
                 if (left < kDepth) o = lds_row(p) < left ? o : kBeyond;
             }
-            load_to_lds(from, to + p * THREADS * 16, o, scalar);
+            load_to_lds(from, at_lds + p * THREADS * 16, o, scalar);
         }
     }
     __device__ __forceinline__ void put(char*) const {}     // it goes there by itself

@@ -17,17 +17,6 @@ def _blocks():
             yield os.path.basename(path), text[start.end():at - 1]
 
 
-def test_loads_in_assembly_keep_their_distance_from_the_scalars_they_read():
-    """Five wait states between a vector instruction that writes a scalar register (a broadcast of a lane) and a
-    vector memory instruction that reads it; inside an assembly block the compiler puts in none."""
-    found = 0
-    for name, block in _blocks():
-        if re.search(r"(buffer|global|flat|scratch)_(load|store|atomic)", block):
-            found += 1
-            assert re.search(r's_nop 4\\n\\t(buffer|global|flat|scratch)_', block), (name, block)
-    assert found
-
-
 def test_assembly_leaves_m0_to_the_compiler():
     """A block that needs a value in m0 takes it as an operand: written inside, the compiler would not know."""
     found = 0
