@@ -412,11 +412,11 @@ template <typename T, int LAYOUT, int FREE, int THREADS> struct Loose {
             if constexpr (LAYOUT == kDepthFast) {
                 const uint32_t d = depth0 + me % kAcross * V;
                 q[p] = at[p] + (uint64_t)depth0 * sizeof(T);
-                exist = (at[p] != nullptr) & (d < depth_end) ? depth_end - d : 0;
+                exist = ((at[p] != nullptr) & (d < depth_end)) ? depth_end - d : 0;
             } else {
                 const uint32_t to = source != nullptr ? fdiv(row[p], slots) : row[p];
                 q[p] = base + to * row_bytes + (uint64_t)free * sizeof(T);
-                exist = (row[p] < 1u << 31) & (to < rows) & (free < free_end) ? free_end - free : 0;
+                exist = ((row[p] < 1u << 31) & (to < rows) & (free < free_end)) ? free_end - free : 0;
             }
             n[p] = (int)(exist < (uint32_t)V ? exist : (uint32_t)V);
             left |= (uint32_t)n[p] << (8 * p);
