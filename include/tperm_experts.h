@@ -134,7 +134,9 @@ tperm_status_t tperm_checkpoint_load(const uint8_t *codes, const uint8_t *scales
 /* The gated activation of rows [g, u] (g the first `width` elements, u the next):
  *   out = g * sigmoid(g) * u
  * and the same rows in 8 bits: codes rows * 2 * width bytes, scales rows * 2 * TPERM_CHECKPOINT_BLOCKS(width),
- * g's first, as two checkpoints beside each other.  codes and scales may both be NULL: nothing is kept. */
+ * g's first, as two checkpoints beside each other.  codes and scales may both be NULL: nothing is kept.
+ * In front of its rounding a result is within 9 * 2^-23 of its value, 16-bit ones within (9 + |g| / 2) * 2^-23, down to the
+ * smallest numbers of the type: a sigmoid that is no normal number does not become zero. */
 tperm_status_t tperm_gated_forward(const void *gates, int64_t gates_stride, void *out, int64_t out_stride, uint8_t *codes,
                                    uint8_t *scales, int64_t rows, int64_t width, int type, void *hip_stream);
 
