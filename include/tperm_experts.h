@@ -15,7 +15,7 @@
  * All other calls take these maps, so a program that makes its own order can use them too.  Maps are read
  * on the GPU and not checked on the host: offsets have to rise from 0 to at most `rows`, source and place
  * have to be permutations of 0 .. rows-1.  An entry of source or place outside that range is treated as
- * unused; nothing is read or written outside the tensors for it.
+ * unused, by the products as a row of zeros; nothing is read or written outside the tensors for it.
  *
  * Element types are a tperm_type_t.  Sums, products of the gates and scales are formed in binary32 and
  * rounded once, to nearest even, where they are stored.  A matrix of rows is given by a pointer to its first
@@ -97,7 +97,7 @@ tperm_status_t tperm_expert_combine_backward(const void *grad, int64_t grad_stri
  * matrices of one type with x and out, w(i, j) at j + n * i, or with w_k_first at i + k * j (the summed index
  * first, the layout of a linear layer's weight).  The gradient to the rows is the same call with k and n
  * changed for each other, the same w and the other w_k_first.
- * TOO_LARGE: with source, x of 2^32 - 256 bytes or more; one expert's matrix of 2^32 - 256 bytes or more. */
+ * TOO_LARGE: with source, x of more than 2^32 - 256 bytes; one expert's matrix of more than that. */
 tperm_status_t tperm_expert_product(const void *x, int64_t x_stride, int64_t x_rows, const int32_t *source, int64_t slots,
                                     const int32_t *offsets, const void *w, int w_k_first, void *out, int64_t out_stride,
                                     int64_t rows, int64_t experts, int64_t k, int64_t n, int type, void *hip_stream);
@@ -108,7 +108,7 @@ tperm_status_t tperm_expert_product(const void *x, int64_t x_stride, int64_t x_r
  * x_scales NULL: x is of `type`; else x points to the codes and x_scales to the scales of a
  * tperm_checkpoint_store of x_rows rows of width k (x_stride is not looked at), and the values that they stand
  * for, rounded to `type` and held to its finite range, are multiplied.
- * TOO_LARGE: as above, for grad too. */
+ * TOO_LARGE: as above, the matrix being of out_type and x in the form it has; grad may be of any size. */
 tperm_status_t tperm_expert_weight_gradient(const void *x, int64_t x_stride, const uint8_t *x_scales, int64_t x_rows,
                                             const int32_t *source, int64_t slots, const void *grad, int64_t grad_stride,
                                             const int32_t *offsets, void *out, int out_type, int w_k_first, int accumulate,

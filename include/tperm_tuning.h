@@ -133,6 +133,12 @@ typedef struct {
 } tperm_launch_info_t;
 tperm_status_t tperm_plan_launch_info(tperm_plan_t plan, int accumulate, int workgroups, tperm_launch_info_t *info);
 
+/* The tile of the result that a workgroup of tperm_expert_product, or with gradient != 0 of
+ * tperm_expert_weight_gradient, computes for calls of such sizes: results along out's memory by results across.
+ * Host only.  DIMS, ELEM_SIZE and TOO_LARGE as in those calls; NULL for along or across. */
+tperm_status_t tperm_expert_tile(int gradient, int type, int w_k_first, int64_t rows, int64_t experts, int64_t k,
+                                 int64_t n, int *along, int *across);
+
 /* What the current HIP device reports about itself, for the benchmark's record next to the
  * vendor's 8 TB/s figure that Section 3's STREAM-style normalisation is replaced by here: memory
  * bus width in bits, peak memory clock in kHz, compute units.  Any pointer may be NULL.

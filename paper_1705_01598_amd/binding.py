@@ -12,7 +12,7 @@ import ctypes
 import functools
 import os
 import sysconfig
-from typing import Optional, Sequence
+from typing import Optional, Sequence, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtperm.so")
@@ -46,7 +46,7 @@ EXPERT_EXPORTS = ["tperm_expert_sort", "tperm_expert_gather", "tperm_expert_comb
 # include/tperm_tuning.h
 TUNING_EXPORTS = ["tperm_plan_create_ex", "tperm_plan_candidate_count", "tperm_plan_create_candidate",
                   "tperm_plan_index_map", "tperm_plan_model", "tperm_plan_launch_info", "tperm_multiset_compare",
-                  "tperm_device_memory_info"]
+                  "tperm_expert_tile", "tperm_device_memory_info"]
 
 
 class PlanOpts(ctypes.Structure):
@@ -152,6 +152,7 @@ def lib() -> ctypes.CDLL:
         L.tperm_product_accumulate.argtypes = [vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.tperm_product_describe.argtypes = [vp, ctypes.POINTER(ProductInfo)]
         L.tperm_product_destroy.argtypes = [vp]
+        L.tperm_expert_tile.argtypes = [ctypes.c_int] * 3 + [ctypes.c_int64] * 4 + [ip, ip]
         L.tperm_status_string.argtypes = [ctypes.c_int]
         L.tperm_status_string.restype = ctypes.c_char_p
         for name in EXPORTS + EXPERT_EXPORTS + TUNING_EXPORTS:
@@ -585,6 +586,14 @@ def tperm_gated_backward(grad_ptr: int, grad_stride: int, codes_ptr: int, scales
                                             out_ptr, out_stride, rows, width, dtype, stream)
     if st != OK:
         raise TpermError(st, "tperm_gated_backward")
+
+
+def tperm_expert_tile(gradient: bool, dtype: int, w_k_first: bool, rows: int, experts: int, k: int, n: int) -> Tuple[int, int]:
+    along, across = ctypes.c_int(), ctypes.c_int()
+    st = lib().tperm_expert_tile(int(gradient), dtype, int(w_k_first), rows, experts, k, n, ctypes.byref(along), ctypes.byref(across))
+    if st != OK:
+        raise TpermError(st, "tperm_expert_tile")
+    return along.value, across.value
 
 
 def tperm_plan_destroy(plan: Plan) -> None:

@@ -6,10 +6,14 @@
 
 namespace tperm {
 
+// The tiles of Tile.
 using TinyTile = TileShape<64, 64, 4, 2, 2>;
 using SmallTile = TileShape<128, 128, 4, 2>;
 using NarrowTile = TileShape<128, 64, 4, 2>;    // 32-bit elements, which the matrix cores bound: finer rounds of tiles
 using WideTile = TileShape<256, 256, 8, 4>;     // 64 x 128 results to a wavefront: fewer transposing reads than 128 x 64 of a free-fast matrix
+
+template <typename S> constexpr bool is(Tile t) { return S::kFast == kTileFast[(int)t] && S::kSlow == kTileSlow[(int)t]; }
+static_assert(is<TinyTile>(Tile::kTiny) && is<SmallTile>(Tile::kSmall) && is<NarrowTile>(Tile::kNarrow) && is<WideTile>(Tile::kWide), "as the query says");
 
 // Workgroups with more than 64 KiB of LDS have to be allowed it, once on each device.
 template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
@@ -39,28 +43,18 @@ inline bool on_chunks(size_t elem, const void* p, int64_t stride, uint32_t width
     return width * elem % 16 == 0 && ((uintptr_t)p | (uintptr_t)stride * elem) % 16 == 0 && stride < (int64_t)1 << 22;
 }
 
-inline uint64_t over(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
-
 template <typename T, typename S, bool LOOSE> hipError_t product_tiles(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
     const uint64_t tiles = ((uint64_t)a.rows / S::kSlow + a.experts + 1) * over(a.n, S::kFast), blocks = over(tiles, kXcds) * kXcds;
     return w_k_first ? go<expert_product_kernel<T, kDepthFast, S, LOOSE>, S>(blocks, a, stream) : go<expert_product_kernel<T, kFreeFast, S, LOOSE>, S>(blocks, a, stream);
 }
 
 template <typename T, bool LOOSE> hipError_t product_with(const ExpertProductArgs& a, bool w_k_first, hipStream_t stream) {
-    // Large tiles need fewer bytes an operation, small ones fill the 256 compute units and waste less on experts of
-    // few rows (bf16, us with tiles of 256, 128, 64; rows of all experts on the average):
-    //   8 experts 1024 x 1024: 128 rows 26 17 13, 256 rows 26 17 19, 512 rows 27 21 28, 1024 rows 29 35 46
-    //   8 experts 2048 x 2048: 256 rows 45 36 45, 512 rows 47 59 73;  64 experts: 128 rows 183 171 221, 256 rows 233 243 352
-    //   64 experts 2048 x 1024: one row 40 26 19, 16 rows 66 61 49
-    const uint64_t rows = over(a.rows, a.experts);
-    const auto tiles = [&](uint64_t side) { return over(rows, side) * a.experts * over(a.n, side); };
-    //   f32, 8 experts 1024 x 1024, tiles of 128, 128 x 64, 64: 1024 rows 200 178 182, 4096 rows 554 540 564;
-    //   701 x 903: 750 rows 123 139 104
+    const Tile tile = product_tile(sizeof(T), a.rows, a.experts, a.n);
     if constexpr (sizeof(T) == 2) {
-        if (rows >= 192 && tiles(256) >= 128) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
-        if (rows >= 64 && tiles(128) >= 128) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
+        if (tile == Tile::kWide) return product_tiles<T, WideTile, LOOSE>(a, w_k_first, stream);
+        if (tile == Tile::kSmall) return product_tiles<T, SmallTile, LOOSE>(a, w_k_first, stream);
     } else {
-        if (rows >= 64 && tiles(128) >= 512) return product_tiles<T, NarrowTile, LOOSE>(a, w_k_first, stream);
+        if (tile == Tile::kNarrow) return product_tiles<T, NarrowTile, LOOSE>(a, w_k_first, stream);
     }
     return product_tiles<T, TinyTile, LOOSE>(a, w_k_first, stream);
 }
@@ -86,14 +80,12 @@ template <typename T, typename S, bool LOOSE> hipError_t gradient_tiles(const We
 }
 
 template <typename T, bool LOOSE> hipError_t gradient_with(const WeightGradientArgs& a, hipStream_t stream) {
-    const auto tiles = [&](uint64_t side) { return over(a.fast.width, side) * over(a.slow.width, side) * a.experts; };
-    // As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 73 44 56,
-    // 2048 x 2048 (512) 93 109 207; f32, 8 experts 1024 x 1024 (512 of 128), 128, 128 x 64, 64: 234 152 164
+    const Tile tile = gradient_tile(sizeof(T), a.fast.width, a.slow.width, a.experts);
     if constexpr (sizeof(T) == 2) {
-        if (tiles(256) >= 192) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
-        if (tiles(128) >= 256) return gradient_tiles<T, SmallTile, LOOSE>(a, stream);
+        if (tile == Tile::kWide) return gradient_tiles<T, WideTile, LOOSE>(a, stream);
+        if (tile == Tile::kSmall) return gradient_tiles<T, SmallTile, LOOSE>(a, stream);
     } else {
-        if (tiles(128) >= 512) return gradient_tiles<T, NarrowTile, LOOSE>(a, stream);
+        if (tile == Tile::kNarrow) return gradient_tiles<T, NarrowTile, LOOSE>(a, stream);
     }
     return gradient_tiles<T, TinyTile, LOOSE>(a, stream);
 }

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(1024) void place_kernel(const int32_t* __restrict__
             total[b] = all;
         }
     __syncthreads();
-    // first row of every bin: up to three neighbouring bins to a thread
+    // first row of every bin: neighbouring bins to a thread, up to five (1025 bins and 256 threads)
     const uint32_t per = (bins + blockDim.x - 1) / blockDim.x, b0 = threadIdx.x * per;
     uint32_t mine_total = 0;
     for (uint32_t i = 0; i < per; ++i) mine_total += b0 + i < bins ? total[b0 + i] : 0u;

@@ -46,6 +46,34 @@ hipError_t launch_checkpoint_load(CheckpointArgs a, int type, hipStream_t stream
 hipError_t launch_gated_forward(CheckpointArgs a, int type, hipStream_t stream);
 hipError_t launch_gated_backward(CheckpointArgs a, int type, hipStream_t stream);
 
+// Tile of the result that a workgroup computes: results along memory x across.
+enum class Tile { kTiny, kSmall, kNarrow, kWide };      // 64 x 64, 128 x 128, 128 x 64, 256 x 256
+constexpr int kTileFast[] = {64, 128, 128, 256}, kTileSlow[] = {64, 128, 64, 256};
+
+inline uint64_t over(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// Large tiles need fewer bytes an operation, small ones fill the 256 compute units and waste less on experts of
+// few rows (bf16, us with tiles of 256, 128, 64; rows of all experts on the average):
+//   8 experts 1024 x 1024: 128 rows 26 17 13, 256 rows 26 17 19, 512 rows 27 21 28, 1024 rows 29 35 46
+//   8 experts 2048 x 2048: 256 rows 45 36 45, 512 rows 47 59 73;  64 experts: 128 rows 183 171 221, 256 rows 233 243 352
+//   64 experts 2048 x 1024: one row 40 26 19, 16 rows 66 61 49
+//   f32, 8 experts 1024 x 1024, tiles of 128, 128 x 64, 64: 1024 rows 200 178 182, 4096 rows 554 540 564;
+//   701 x 903: 750 rows 123 139 104
+inline Tile product_tile(size_t elem, uint64_t all_rows, uint64_t experts, uint64_t n) {
+    const uint64_t rows = over(all_rows, experts);
+    const auto tiles = [&](uint64_t side) { return over(rows, side) * experts * over(n, side); };
+    if (elem == 4) return rows >= 64 && tiles(128) >= 512 ? Tile::kNarrow : Tile::kTiny;
+    return rows >= 192 && tiles(256) >= 128 ? Tile::kWide : rows >= 64 && tiles(128) >= 128 ? Tile::kSmall : Tile::kTiny;
+}
+
+// As for the products (bf16 in 8 bits, us with tiles of 256, 128, 64): 8 experts 1024 x 1024 (128 tiles of 256) 73 44 56,
+// 2048 x 2048 (512) 93 109 207; f32, 8 experts 1024 x 1024 (512 of 128), 128, 128 x 64, 64: 234 152 164
+inline Tile gradient_tile(size_t elem, uint64_t fast, uint64_t slow, uint64_t experts) {
+    const auto tiles = [&](uint64_t side) { return over(fast, side) * over(slow, side) * experts; };
+    if (elem == 4) return tiles(128) >= 512 ? Tile::kNarrow : Tile::kTiny;
+    return tiles(256) >= 192 ? Tile::kWide : tiles(128) >= 256 ? Tile::kSmall : Tile::kTiny;
+}
+
 // One side of an experts' product.
 struct ProductSide {
     const void* p;              // elements, or codes

@@ -1,6 +1,8 @@
-// C-ABI entry points declared in include/tperm_experts.h: checks of the arguments, then one launch.
+// C-ABI entry points declared in include/tperm_experts.h: checks of the arguments, then one launch; and the query
+// of their tiles in include/tperm_tuning.h.
 #include <hip/hip_runtime.h>
 
+#include "../../include/tperm_tuning.h"
 #include "experts.hpp"
 #include "plan.hpp"
 
@@ -220,6 +222,20 @@ tperm_status_t tperm_expert_weight_gradient(const void* x, int64_t x_stride, con
     a.fast = w_k_first ? xs : gs, a.slow = w_k_first ? gs : xs;
     a.out = out, a.offsets = offsets, a.rows = (uint32_t)rows, a.experts = (uint32_t)experts, a.out_type = out_type, a.accumulate = accumulate != 0;
     return launched(launch_weight_gradient(a, type, (hipStream_t)hip_stream));
+}
+
+tperm_status_t tperm_expert_tile(int gradient, int type, int w_k_first, int64_t rows, int64_t experts, int64_t k, int64_t n, int* along, int* across) {
+    int64_t assigned = 0;
+    const tperm_status_t st = count_rows(0, 1, experts, &assigned);
+    if (st != TPERM_OK) return st;
+    if (rows < 0 || !known_width(k) || !known_width(n)) return TPERM_ERR_DIMS;
+    if (!known_type(type)) return TPERM_ERR_ELEM_SIZE;
+    if (rows > kRowsMax) return TPERM_ERR_TOO_LARGE;
+    if (along == nullptr || across == nullptr) return TPERM_ERR_NULL;
+    const size_t elem = type_bytes(type);
+    const int t = (int)(gradient ? gradient_tile(elem, w_k_first ? k : n, w_k_first ? n : k, experts) : product_tile(elem, rows, experts, n));
+    *along = kTileFast[t], *across = kTileSlow[t];
+    return TPERM_OK;
 }
 
 tperm_status_t tperm_checkpoint_store(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int64_t width, int type, void* hip_stream) {
