@@ -14,8 +14,11 @@ that GPU's current stream, whichever GPU is the current one (a layer is used on 
 """
 from __future__ import annotations
 
+import contextlib
+import itertools
 from typing import Dict, Tuple
 
+_HERE = contextlib.nullcontext()
 _NAMES = {"torch.float32": "f32", "torch.float16": "f16", "torch.bfloat16": "bf16"}
 
 
@@ -37,10 +40,11 @@ class ExpertLayer:
         self.experts, self.slots, self.width, self.hidden, self.dtype = experts, slots, width, hidden, dtype
         self._type = B.TYPES[_NAMES[str(dtype)]]
         self._device = torch.device(device)
-        self._room, self._b = -1, {}
+        self._size = dtype.itemsize
+        self._room, self._b, self._at = -1, {}, {}
         self._kept = None
 
-    def _buffers(self, tokens: int) -> Dict[str, object]:
+    def _buffers(self, tokens: int) -> Dict[str, int]:
         if tokens > self._room:
             torch, B = self._torch, self._B
             rows, w, h = tokens * self.slots, self.width, self.hidden
@@ -50,18 +54,15 @@ class ExpertLayer:
                        "x_codes": new(tokens * w, dtype=u8), "x_scales": new(tokens * B.checkpoint_blocks(w), dtype=u8),
                        "gate_codes": new(rows * 2 * h, dtype=u8), "gate_scales": new(rows * 2 * B.checkpoint_blocks(h), dtype=u8),
                        "rows": new(rows, w)}
+            self._at = {k: t.data_ptr() for k, t in self._b.items()}
             self._room = tokens
-        return {k: t.data_ptr() for k, t in self._b.items()}
+        return self._at
 
     def _scratch(self, *sizes: int):
         """One buffer for a pass's own arrays of so many bytes each: the buffer, and where each of them starts in it."""
-        starts, end = [], 0
-        for n in sizes:
-            starts.append(end)
-            end += -(-n // 256) * 256
-        buffer = self._torch.empty(end, dtype=self._torch.uint8, device=self._device)
-        at = buffer.data_ptr()
-        return (buffer, *(at + start for start in starts))
+        room = [n + 255 & ~255 for n in sizes]
+        buffer = self._torch.empty(sum(room), dtype=self._torch.uint8, device=self._device)
+        return buffer, *itertools.accumulate(room[:-1], initial=buffer.data_ptr())
 
     def kept_bytes(self) -> int:
         """Bytes of GPU memory that the layer holds between its passes."""
@@ -75,7 +76,7 @@ class ExpertLayer:
         """The layer's GPU as the current one, while calls are enqueued."""
         if self._device.type != "cuda":
             raise ValueError("the layer computes on a GPU: no host tensors")
-        return self._torch.cuda.device(self._device)
+        return _HERE if self._torch.cuda.current_device() == self._device.index else self._torch.cuda.device(self._device)
 
     def forward(self, x, expert, weights, w_in, w_out):
         """The layer's result for x [tokens, width]; expert [tokens, slots] int32 (a number outside 0 .. experts-1 names
@@ -99,7 +100,7 @@ class ExpertLayer:
             self._kept = None       # the buffers of the pass before are overwritten from here on, whether this one succeeds or not
             b = self._buffers(tokens)
             need = B.expert_sort_workspace_bytes(rows, e)
-            scratch, gates, hidden, sort = self._scratch(rows * 2 * h * x.element_size(), rows * h * x.element_size(), need)    # held to the last call
+            scratch, gates, hidden, sort = self._scratch(rows * 2 * h * self._size, rows * h * self._size, need)    # held to the last call
             s = torch.cuda.current_stream().cuda_stream
             B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, b["offsets"], b["source"], b["place"], sort, need, s)
             B.tperm_checkpoint_store(x.data_ptr(), w, b["x_codes"], b["x_scales"], tokens, w, t, s)
@@ -131,7 +132,7 @@ class ExpertLayer:
         with self._gpu():
             b = self._buffers(tokens)
             # the hidden rows again, for their matrix, take the rows' place where they fit
-            size, fits = grad.element_size(), h <= w
+            size, fits = self._size, h <= w
             scratch, grad_rows, hidden, gates, again = self._scratch(rows * w * size, rows * h * size, rows * 2 * h * size, 0 if fits else rows * h * size)
             again = b["rows"] if fits else again
             s = torch.cuda.current_stream().cuda_stream

@@ -55,6 +55,9 @@ class Torch:
     def empty_like(self, t):
         return Tensor(*t.shape, dtype=t.dtype, device=t.device)
 
+    def current_device(self):
+        return self.current
+
     def device(self, d):
         d = torch.device(d)
 
