@@ -7,8 +7,8 @@
 // LDS atomics (whole numbers, so their order does not matter), scanned over wavefronts, then placed 64 at a time in
 // order: a lane's rank among the lanes of its expert comes from one ballot per bit of the expert number.
 //
-// Latency is the bound: 132 assignments 3.1 us, 524288 of 128 experts 2.8 us for the counts and 14 for the placing, with 6 MB
-// to move; 7 and 16.4 us a call.
+// Latency is the bound: 132 assignments 3.2 us, 524288 of 128 experts 2.7 us for the counts and 14.5 for the placing, with 6 MB
+// to move; 3.4 and 16.4 us a call, one behind the other.
 #include "experts.hpp"
 
 namespace tperm {
