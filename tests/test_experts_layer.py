@@ -116,3 +116,33 @@ def test_no_tokens():
     y = layer.forward(empty, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"), w_in, w_out)
     gx, gw = layer.backward(empty, w_in, w_out, accumulate=False)
     assert y.shape == (0, 16) and gx.shape == (0, 16) and gw.shape == (0, 2) and not bool(w_in.any()) and not bool(w_out.any())
+
+
+@pytest.mark.gpu
+def test_layer_in_a_graph():
+    """Both passes captured, then replayed between eager passes of other tokens: the same bits every time."""
+    tokens, experts, slots, width, hidden = 150, 6, 2, 96, 128
+    g = torch.Generator().manual_seed(3)
+    randn = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+    layer = ExpertLayer(experts, slots, width, hidden, torch.bfloat16)
+    x, grad = randn(tokens, width).bfloat16().cuda(), randn(tokens, width).bfloat16().cuda()
+    other = randn(tokens, width).bfloat16().cuda()
+    w_in, w_out = (randn(experts, 2 * hidden, width) / width ** 0.5).bfloat16().cuda(), (randn(experts, width, hidden) / hidden ** 0.5).bfloat16().cuda()
+    expert, weights = torch.randint(-1, experts, (tokens, slots), generator=g).to(torch.int32).cuda(), torch.rand(tokens, slots, generator=g).cuda()
+    grad_in, grad_out = torch.empty(w_in.shape, device="cuda"), torch.empty(w_out.shape, device="cuda")
+
+    def both(x):
+        y = layer.forward(x, expert, weights, w_in, w_out)
+        return [y, *layer.backward(grad, grad_in, grad_out, accumulate=False), grad_in, grad_out]
+
+    want = [t.clone() for t in both(x)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        results = both(x)
+    for _ in range(4):
+        both(other)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results, want))
