@@ -1,6 +1,6 @@
 """ctypes binding of libtperm.so: same names as the C ABI in include/tperm.h (the product
-boundary), include/tperm_experts.h (the operators of a mixture-of-experts layer) and
-include/tperm_tuning.h (overrides, candidate enumeration and the host-side index map, for tests and
+boundary), include/tperm_experts.h (the operators of a mixture-of-experts layer), include/tperm_decode.h
+(its router, matrices in 4 bits, and the layer for a few tokens) and include/tperm_tuning.h (overrides, candidate enumeration and the host-side index map, for tests and
 sweeps).
 
 Argument marshalling only.  Every step of the transpose runs in the library's kernels;
@@ -43,6 +43,9 @@ EXPORTS = ["tperm_plan_create", "tperm_plan_create_forced", "tperm_plan_create_m
 EXPERT_EXPORTS = ["tperm_expert_sort", "tperm_expert_gather", "tperm_expert_combine", "tperm_expert_combine_backward",
                   "tperm_expert_product", "tperm_expert_weight_gradient", "tperm_checkpoint_store",
                   "tperm_checkpoint_load", "tperm_gated_forward", "tperm_gated_backward"]
+# include/tperm_decode.h: the calls that are enqueued on a stream
+DECODE_EXPORTS = ["tperm_expert_route", "tperm_expert_route_backward", "tperm_four_bit_store", "tperm_four_bit_load",
+                  "tperm_four_bit_product", "tperm_expert_few"]
 # include/tperm_tuning.h
 TUNING_EXPORTS = ["tperm_plan_create_ex", "tperm_plan_candidate_count", "tperm_plan_create_candidate",
                   "tperm_plan_index_map", "tperm_plan_model", "tperm_plan_launch_info", "tperm_multiset_compare",
@@ -155,7 +158,9 @@ def lib() -> ctypes.CDLL:
         L.tperm_expert_tile.argtypes = [ctypes.c_int] * 3 + [ctypes.c_int64] * 4 + [ip, ip]
         L.tperm_status_string.argtypes = [ctypes.c_int]
         L.tperm_status_string.restype = ctypes.c_char_p
-        for name in EXPORTS + EXPERT_EXPORTS + TUNING_EXPORTS:
+        L.tperm_expert_few_workspace.argtypes = [ctypes.c_int64] * 5 + [ctypes.c_int] * 2
+        L.tperm_expert_few_workspace.restype = ctypes.c_size_t
+        for name in EXPORTS + EXPERT_EXPORTS + DECODE_EXPORTS + TUNING_EXPORTS:
             if name != "tperm_status_string":
                 getattr(L, name).restype = ctypes.c_int
         from . import _fastcall
@@ -163,6 +168,7 @@ def lib() -> ctypes.CDLL:
             "tperm_execute", "tperm_execute_accumulate", "tperm_execute_verified", "tperm_transpose",
             "tperm_transpose_accumulate", "tperm_product_accumulate")))
         _fastcall.bind_experts(*(ctypes.cast(getattr(L, name), vp).value for name in EXPERT_EXPORTS))
+        _fastcall.bind_decode(*(ctypes.cast(getattr(L, name), vp).value for name in DECODE_EXPORTS))
         _fast = _fastcall
         _lib = L
     return _lib
@@ -586,6 +592,68 @@ def tperm_gated_backward(grad_ptr: int, grad_stride: int, codes_ptr: int, scales
                                             out_ptr, out_stride, rows, width, dtype, stream)
     if st != OK:
         raise TpermError(st, "tperm_gated_backward")
+
+
+# include/tperm_decode.h
+FEW_TOKENS = 64
+
+
+def four_bit_groups(width: int) -> int:
+    """TPERM_FOUR_BIT_GROUPS of the header."""
+    return (int(width) + 31) // 32
+
+
+def expert_few_workspace_bytes(tokens: int, slots: int, experts: int, width: int, hidden: int, dtype: int, four_bits: bool = False) -> int:
+    """tperm_expert_few_workspace of the header; 0 for no tokens and for sizes outside the limits."""
+    return int(lib().tperm_expert_few_workspace(tokens, slots, experts, width, hidden, dtype, int(four_bits)))
+
+
+def tperm_expert_route(scores_ptr: int, scores_stride: int, expert_ptr: int, weights_ptr: int, tokens: int, slots: int, experts: int,
+                       over_all: bool, dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_route(scores_ptr, scores_stride, expert_ptr, weights_ptr, tokens, slots, experts, over_all, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_route")
+
+
+def tperm_expert_route_backward(grad_weights_ptr: int, scores_ptr: Optional[int], scores_stride: int, expert_ptr: int, weights_ptr: int,
+                                grad_scores_ptr: int, grad_scores_stride: int, tokens: int, slots: int, experts: int, over_all: bool,
+                                dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_route_backward(grad_weights_ptr, scores_ptr, scores_stride, expert_ptr, weights_ptr, grad_scores_ptr,
+                                                   grad_scores_stride, tokens, slots, experts, over_all, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_route_backward")
+
+
+def tperm_four_bit_store(x_ptr: int, x_stride: int, codes_ptr: int, scales_ptr: int, rows: int, width: int, dtype: int,
+                         stream: int = 0) -> None:
+    st = (_fast or _calls()).four_bit_store(x_ptr, x_stride, codes_ptr, scales_ptr, rows, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_four_bit_store")
+
+
+def tperm_four_bit_load(codes_ptr: int, scales_ptr: int, out_ptr: int, out_stride: int, rows: int, width: int, dtype: int,
+                        stream: int = 0) -> None:
+    st = (_fast or _calls()).four_bit_load(codes_ptr, scales_ptr, out_ptr, out_stride, rows, width, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_four_bit_load")
+
+
+def tperm_four_bit_product(x_ptr: int, x_stride: int, codes_ptr: int, scales_ptr: int, out_ptr: int, out_stride: int, rows: int, k: int,
+                           n: int, dtype: int, stream: int = 0) -> None:
+    st = (_fast or _calls()).four_bit_product(x_ptr, x_stride, codes_ptr, scales_ptr, out_ptr, out_stride, rows, k, n, dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_four_bit_product")
+
+
+def tperm_expert_few(x_ptr: int, x_stride: int, expert_ptr: int, weights_ptr: Optional[int], w_in_ptr: int, w_in_scales_ptr: Optional[int],
+                     w_out_ptr: int, w_out_scales_ptr: Optional[int], out_ptr: int, out_stride: int, workspace_ptr: int,
+                     workspace_bytes: int, tokens: int, slots: int, experts: int, width: int, hidden: int, dtype: int,
+                     stream: int = 0) -> None:
+    st = (_fast or _calls()).expert_few(x_ptr, x_stride, expert_ptr, weights_ptr, w_in_ptr, w_in_scales_ptr, w_out_ptr, w_out_scales_ptr,
+                                        out_ptr, out_stride, workspace_ptr, workspace_bytes, tokens, slots, experts, width, hidden,
+                                        dtype, stream)
+    if st != OK:
+        raise TpermError(st, "tperm_expert_few")
 
 
 def tperm_expert_tile(gradient: bool, dtype: int, w_k_first: bool, rows: int, experts: int, k: int, n: int) -> Tuple[int, int]:

@@ -1,0 +1,78 @@
+// Launch interface between the C-ABI layer and the kernels of tperm_decode.h.  Arguments have been checked: sizes are
+// within the limits of the header, strides at least the widths.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/tperm_decode.h"
+#include "experts.hpp"
+
+namespace tperm {
+
+struct RouteArgs {
+    const void* scores;
+    const float* grad_weights;      // backward
+    int32_t* expert;                // backward: read
+    float* weights;
+    void* grad_scores;
+    int64_t scores_stride, grad_stride;
+    uint32_t tokens, slots, experts;
+};
+hipError_t launch_route(const RouteArgs& a, bool over_all, int type, hipStream_t stream);
+hipError_t launch_route_backward(const RouteArgs& a, bool over_all, int type, hipStream_t stream);
+
+struct FourBitArgs {
+    const void* in;                 // store: x
+    void* out;                      // load: out
+    uint8_t *codes, *scales;
+    int64_t stride;
+    uint32_t rows, width;
+    FastDiv per_row;                // by the threads of a row, for thread numbers below 2^31 (set by the launcher)
+};
+hipError_t launch_four_bit_store(FourBitArgs a, int type, hipStream_t stream);
+hipError_t launch_four_bit_load(FourBitArgs a, int type, hipStream_t stream);
+
+struct FourBitProductArgs {
+    const void* x;
+    const uint8_t *codes, *scales;
+    void* out;
+    int64_t x_stride, out_stride;
+    uint32_t rows, k, n;
+};
+hipError_t launch_four_bit_product(const FourBitProductArgs& a, int type, hipStream_t stream);
+
+struct FewArgs {
+    const void* x;
+    const int32_t* expert;
+    const float* weights;           // or NULL
+    const void *w_in, *w_out;       // elements or codes
+    const uint8_t *in_scales, *out_scales;
+    void* out;
+    int64_t x_stride, out_stride;
+    uint32_t tokens, slots, experts, width, hidden;
+    // the workspace: tables that the first kernel makes for the second, then the hidden rows
+    int32_t* tables;
+    void* rows;
+};
+hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
+
+// Workspace of a few tokens' layer.  Named experts (in the order of their numbers) are at most `most`; their tokens
+// lie one behind the other in that order.
+struct FewRoom {
+    uint32_t most;          // named experts at most
+    uint32_t pitch;         // elements of a hidden row
+    size_t tables, rows;    // bytes
+};
+inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t hidden, int type, bool four_bits) {
+    FewRoom r;
+    const int64_t count = tokens * slots;
+    r.most = (uint32_t)(experts < count ? experts : count);
+    r.pitch = (uint32_t)((hidden + 31) / 32 * 32);
+    // how many experts are named; by named expert its number and how many tokens name it (<< 16), and its first row; by row its token
+    r.tables = ((size_t)(1 + 2 * r.most + count) * 4 + 15) / 16 * 16;
+    // one part of 4 bytes an element, two of 2, or three of 2
+    r.rows = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
+    return r;
+}
+
+}  // namespace tperm

@@ -16,7 +16,7 @@
 #include <type_traits>
 #include <utility>
 
-#include "../../include/tperm_experts.h"
+#include "../../include/tperm_decode.h"
 
 namespace {
 
@@ -101,7 +101,7 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
-// The calls of tperm_experts.h: pointers, 64-bit sizes and ints, converted by the type of the parameter.
+// The calls of tperm_experts.h and tperm_decode.h: pointers, 64-bit sizes and ints, converted by the type of the parameter.
 template <typename A> bool to_argument(PyObject* o, A* a) {
     if constexpr (std::is_pointer_v<A>) {
         void* p;
@@ -138,10 +138,13 @@ template <typename... A> PyObject* call(const char* name, tperm_status_t (*f)(A.
 #define TPERM_EXPERT_CALLS(X)                                                                                     \
     X(expert_sort) X(expert_gather) X(expert_combine) X(expert_combine_backward) X(expert_product)                \
     X(expert_weight_gradient) X(checkpoint_store) X(checkpoint_load) X(gated_forward) X(gated_backward)
+#define TPERM_DECODE_CALLS(X)                                                                                     \
+    X(expert_route) X(expert_route_backward) X(four_bit_store) X(four_bit_load) X(four_bit_product) X(expert_few)
 #define TPERM_CALL(name)                                                                                          \
     decltype(&tperm_##name) g_##name;                                                                             \
     PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t n) { return call(#name, g_##name, args, n); }
 TPERM_EXPERT_CALLS(TPERM_CALL)
+TPERM_DECODE_CALLS(TPERM_CALL)
 
 // Addresses of the calls above, in their order.
 PyObject* bind_experts(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -150,6 +153,13 @@ PyObject* bind_experts(PyObject*, PyObject* const* args, Py_ssize_t n) {
     int i = 0;
 #define TPERM_BIND(name) g_##name = (decltype(g_##name))p[i++];
     TPERM_EXPERT_CALLS(TPERM_BIND)
+    Py_RETURN_NONE;
+}
+PyObject* bind_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    void* p[6];
+    if (!count_is("bind_decode", n, 6) || !pointers(args, 6, p)) return nullptr;
+    int i = 0;
+    TPERM_DECODE_CALLS(TPERM_BIND)
     Py_RETURN_NONE;
 }
 
@@ -229,8 +239,9 @@ PyMethodDef methods[] = {
     {"product", (PyCFunction)(void (*)(void))product, METH_FASTCALL, nullptr},
     {"transpose", (PyCFunction)(void (*)(void))transpose, METH_FASTCALL, nullptr},
     {"bind_experts", (PyCFunction)(void (*)(void))bind_experts, METH_FASTCALL, nullptr},
+    {"bind_decode", (PyCFunction)(void (*)(void))bind_decode, METH_FASTCALL, nullptr},
 #define TPERM_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr},
-    TPERM_EXPERT_CALLS(TPERM_METHOD)
+    TPERM_EXPERT_CALLS(TPERM_METHOD) TPERM_DECODE_CALLS(TPERM_METHOD)
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
