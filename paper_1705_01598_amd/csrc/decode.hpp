@@ -50,28 +50,25 @@ struct FewArgs {
     void* out;
     int64_t x_stride, out_stride;
     uint32_t tokens, slots, experts, width, hidden;
-    // the workspace: tables that the first kernel makes for the second, then the hidden rows
-    int32_t* tables;
-    void* rows;
+    void* rows;                     // the workspace: the hidden rows
+    FastDiv by_slots;               // this and the next set by the launcher
+    uint32_t images;                // 16 x 16 products of the first kernel that a workgroup joins at most
 };
 hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
 
-// Workspace of a few tokens' layer.  Named experts (in the order of their numbers) are at most `most`; their tokens
-// lie one behind the other in that order.
+// Workspace of a few tokens' layer: hidden rows of named experts, in the order of their numbers.
 struct FewRoom {
     uint32_t most;          // named experts at most
     uint32_t pitch;         // elements of a hidden row
-    size_t tables, rows;    // bytes
+    size_t bytes;
 };
 inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t hidden, int type, bool four_bits) {
     FewRoom r;
     const int64_t count = tokens * slots;
     r.most = (uint32_t)(experts < count ? experts : count);
     r.pitch = (uint32_t)((hidden + 31) / 32 * 32);
-    // how many experts are named; by named expert its number and how many tokens name it (<< 16), and its first row; by row its token
-    r.tables = ((size_t)(1 + 2 * r.most + count) * 4 + 15) / 16 * 16;
     // one part of 4 bytes an element, two of 2, or three of 2
-    r.rows = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
+    r.bytes = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
     return r;
 }
 

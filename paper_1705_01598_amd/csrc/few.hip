@@ -1,22 +1,26 @@
 // A whole mixture-of-experts layer for a few tokens, in two kernels.
 //
-// The first: a workgroup to 16 hidden channels of one named expert multiplies their g and u rows with the tokens that name
-// the expert, applies the gated activation and the token's weight, and stores the hidden row in parts.  Every workgroup finds its
-// expert and its tokens from the numbers themselves (at most 64 x 64 of them), so no order has to be made first;
-// one workgroup an expert writes down what it found for the second kernel.  The second: a workgroup to 16 channels of the result goes through all
-// named experts, its wavefronts share experts and pieces of their sums, and adds up by token in LDS, one
-// array for each wavefront, joined in their order: no atomics, and no rows of the experts in memory.
+// The first multiplies the g and u rows of 8 hidden channels of a named expert (an item) with the tokens that name it, applies the gated
+// activation and the token's weight, and stores the hidden rows in parts; a workgroup goes through every so-many-th
+// item.  The second: a workgroup to 8 channels of the result goes through all named experts, its wavefronts share
+// experts and pieces of their sums, and add up by token in LDS, one array for each wavefront, joined in their order: no
+// atomics on numbers that round, and no rows of the experts in memory.
+// Every workgroup of both finds the named experts and their tokens from the numbers themselves (at most 64 x 64 of
+// them), so no order has to be made first.
 #include <type_traits>
 
 #include "decode.hpp"
 #include "few.hpp"
 #include "gated.hpp"
+#include "plan.hpp"
 
 namespace tperm {
 
 namespace {
 
-constexpr uint32_t kChannels = 16;      // of a workgroup
+constexpr uint32_t kChannels = 8;       // of a tile
+constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit
+static_assert(kFewWaves * 4 * 64 * 16 + (TPERM_FEW_TOKENS * TPERM_SLOTS_MAX * 7 + TPERM_EXPERTS_MAX * 18 + 16) <= 81920, "LDS of two workgroups");
 
 // What the second product's columns are: how a hidden row is held between the kernels.
 template <typename T, bool FOUR> struct Hidden {
@@ -41,59 +45,136 @@ template <typename M> __device__ __forceinline__ M matrix_of(const void* p, cons
     return m;
 }
 
-// Bit number `rank` of 1024 in LDS, and how many there are.
-__device__ __forceinline__ uint32_t find_bit(const uint32_t* bits, uint32_t rank, uint32_t* total) {
-    const uint32_t lane = threadIdx.x & 63u, word = lane < 32 ? bits[lane] : 0u;
-    const uint32_t mine = (uint32_t)__builtin_popcount(word);
-    uint32_t upto = mine;
-    for (uint32_t d = 1; d < 32; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_up((int)upto, d);
-        if (lane >= d) upto += o;
-    }
-    *total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 31);
-    const uint64_t here = __ballot(lane < 32 && rank < upto && rank >= upto - mine);
-    if (here == 0) return 0;
-    const uint32_t at = (uint32_t)__builtin_ctzll(here);
-    uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)word, at), skip = rank - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), at);
-    while (skip-- != 0) w &= w - 1;
-    return at * 32 + (uint32_t)__builtin_ctz(w);
+// What the numbers say, in LDS: by named expert, in the order of their numbers, its number and how many tokens name it (<< 16), and its
+// first hidden row; by hidden row its token and, for the first kernel, its weight.
+struct Named {
+    uint32_t* mask;         // two words an expert, a bit to a token
+    uint32_t *entry, *first;
+    float* weight;
+    uint16_t *number, *start;
+    uint8_t* token;
+    uint32_t total;
+};
+constexpr size_t named_bytes(size_t count, size_t experts, size_t most, bool weights) {
+    return (experts * 8 + most * 8 + (weights ? count * 4 : 0) + count * 2 + experts * 2 + count + 15) / 16 * 16;
 }
 
-template <typename T, bool FOUR, int STEPS, bool ALIGNED, int M>
-__device__ __forceinline__ void hidden_channels(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint32_t* token, const float* weight,
-                                                uint32_t first_row, f32x4* sums) {
+// Sums over the lanes up to this one.
+__device__ __forceinline__ uint32_t upto(uint32_t v) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);     // the last lane of a row to the next one
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);     // of the first half to the second
+    return v;
+}
+
+template <uint32_t THREADS, bool WEIGHTS> __device__ __forceinline__ Named find_named(const FewArgs& a, void* lds, uint32_t most) {
+    static_assert(2 * THREADS >= TPERM_EXPERTS_MAX, "two experts to a thread");
+    __shared__ uint32_t wave_total[THREADS / 64], twice;
+    const uint32_t count = a.tokens * a.slots, wave = threadIdx.x >> 6;
+    Named n;
+    n.mask = (uint32_t*)lds, n.entry = n.mask + 2 * a.experts, n.first = n.entry + most, n.weight = (float*)(n.first + most);
+    n.number = (uint16_t*)(n.weight + (WEIGHTS ? count : 0)), n.start = n.number + count, n.token = (uint8_t*)(n.start + a.experts);
+    int32_t own = -1;
+    float own_weight = 1.0f;
+    if (threadIdx.x < count) {
+        own = a.expert[threadIdx.x];
+        if (WEIGHTS && a.weights != nullptr) own_weight = a.weights[threadIdx.x];
+    }
+    for (uint32_t i = threadIdx.x; i < 2 * a.experts; i += THREADS) n.mask[i] = 0;
+    if (threadIdx.x == 0) twice = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        const uint32_t e = (uint32_t)(i < THREADS ? own : a.expert[i]), t = fdiv(i, a.by_slots);
+        const bool there = e < a.experts;
+        n.number[i] = (uint16_t)(there ? e : 0xFFFFu);
+        if (there) {
+            const uint32_t bit = 1u << t % 32, before = atomicOr(&n.mask[2 * e + t / 32], bit);
+            if (WEIGHTS && (before & bit)) twice = 1;
+        }
+    }
+    __syncthreads();
+    // experts and rows before each expert: experts in the low half
+    const uint32_t each = a.experts <= THREADS ? 1 : 2, e0 = threadIdx.x * each;
+    uint32_t names[2] = {};
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+        if (k < each && e0 + k < a.experts) names[k] = (uint32_t)__builtin_popcount(n.mask[2 * (e0 + k)]) + (uint32_t)__builtin_popcount(n.mask[2 * (e0 + k) + 1]);
+    const uint32_t mine = (names[0] + names[1]) << 16 | ((names[0] != 0) + (names[1] != 0));
+    const uint32_t up = upto(mine);
+    if ((threadIdx.x & 63u) == 63) wave_total[wave] = up;
+    __syncthreads();
+    uint32_t before = up - mine, all = 0;
+#pragma unroll
+    for (uint32_t v = 0; v < THREADS / 64; ++v) {
+        before += v < wave ? wave_total[v] : 0u;
+        all += wave_total[v];
+    }
+    n.total = (uint32_t)__builtin_amdgcn_readfirstlane((int)(all & 0xFFFFu));
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+        if (names[k] != 0) {
+            n.entry[before & 0xFFFFu] = (e0 + k) | names[k] << 16;
+            n.first[before & 0xFFFFu] = before >> 16;
+            n.start[e0 + k] = (uint16_t)(before >> 16);
+            before += names[k] << 16 | 1u;
+        }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        const uint32_t e = n.number[i], t = fdiv(i, a.by_slots);
+        if (e == 0xFFFFu) continue;
+        const uint64_t named = n.mask[2 * e] | (uint64_t)n.mask[2 * e + 1] << 32;
+        const uint32_t row = n.start[e] + (uint32_t)__builtin_popcountll(named & ((1ull << t) - 1));
+        n.token[row] = (uint8_t)t;
+        if constexpr (WEIGHTS) {
+            float w = i < THREADS ? own_weight : a.weights != nullptr ? a.weights[i] : 1.0f;
+            if (twice) {        // all slots of the token that name this expert write the same sum
+                w = 0.0f;
+                for (uint32_t s = t * a.slots; s < (t + 1) * a.slots; ++s)
+                    if (n.number[s] == e) w += a.weights != nullptr ? a.weights[s] : 1.0f;
+            }
+            n.weight[row] = w;
+        }
+    }
+    __syncthreads();
+    return n;
+}
+
+template <typename T, bool FOUR, typename S, int STEPS, bool ALIGNED>
+__device__ __forceinline__ void hidden_channels(const FewArgs& a, uint32_t pitch, const Named& n, uint32_t entry, uint32_t first_row, uint32_t channel, f32x4* sums) {
     typedef Matrix<T, FOUR> W;
     typedef Hidden<T, FOUR> H;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, channel = blockIdx.x * kChannels;
+    constexpr int M = S::M;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, e = entry & 0xFFFFu, named = entry >> 16;
+    const uint8_t* const token = n.token + first_row;
     const W w = matrix_of<W>(a.w_in, a.in_scales, e, 2 * a.hidden, a.width);
-    const uint32_t g = channel + lane % 16 < a.hidden ? channel + lane % 16 : a.hidden - 1;
+    const uint32_t g = channel + S::row() < a.hidden ? channel + S::row() : a.hidden - 1;
     const uint32_t row[2] = {g, g + a.hidden};
     const T* x[M];
-    for (int m = 0; m < M; ++m) {
-        const uint32_t c = m * 16 + lane % 16;
-        x[m] = (const T*)a.x + (int64_t)token[c < named ? c : 0] * a.x_stride;
-    }
+    for (int m = 0; m < M; ++m) x[m] = (const T*)a.x + (int64_t)token[S::column(m) < named ? S::column(m) : 0] * a.x_stride;
     const Tokens<T, FOUR> cols = {};
-    f32x4 sum[2][M] = {};
-    rows_by_columns<STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, wave, (uint32_t)kFewWaves, sum);
-    const uint32_t c = wave * 16 + lane % 16;       // of those who join: one wavefront for 16 columns
+    f32x4 sum[S::kSums][M] = {};
+    rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, wave, (uint32_t)kFewWaves, sum);
+    constexpr int kEach = S::kSums * M;
+    __syncthreads();        // what was in this place has been read
+    for (int r = 0; r < S::kSums; ++r)
+        for (int m = 0; m < M; ++m) sums[(wave * kEach + r * M + m) * 64 + lane] = sum[r][m];
+    __syncthreads();
+    // four channels of one column to a lane
+    const uint32_t m = threadIdx.x / (2 * S::kColumns), half = threadIdx.x / S::kColumns % 2, c = threadIdx.x % S::kColumns, column = m * S::kColumns + c;
+    if (column >= named) return;
     f32x4 gu[2] = {};
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        __syncthreads();        // what was in this place has been read
-        for (int m = 0; m < M; ++m) sums[(wave * M + m) * 64 + lane] = sum[r][m];
-        __syncthreads();
-        if (wave < M)
-            for (uint32_t v = 0; v < kFewWaves; ++v) gu[r] += sums[(v * M + wave) * 64 + lane];
-    }
-    if (wave >= M || c >= named) return;
+    for (uint32_t v = 0; v < kFewWaves; ++v)
+        for (int r = 0; r < 2; ++r) gu[r] += sums_at<S>(sums + v * kEach * 64, r, m, half, c);
     f32x4 h;
     for (int i = 0; i < 4; ++i) {
         const Sigmoid s = sigmoid<float>(gu[0][i]);
-        h[i] = gu[0][i] * s.p * gu[1][i] * s.last * weight[c];
+        h[i] = gu[0][i] * s.p * gu[1][i] * s.last * n.weight[first_row + column];
     }
     const int64_t rows = (int64_t)a.tokens * a.slots;
-    typename H::E* const out = (typename H::E*)a.rows + (int64_t)(first_row + c) * pitch + channel + lane / 16 * 4;
+    typename H::E* const out = (typename H::E*)a.rows + (int64_t)(first_row + column) * pitch + channel + half * 4;
     for (int p = 0; p < H::kParts; ++p) {
         const Vec<typename H::E, 4> part = narrow<typename H::E, 4>(h);
         store_vec<typename H::E, 4, true>(out + p * rows * pitch, part);
@@ -104,125 +185,90 @@ __device__ __forceinline__ void hidden_channels(const FewArgs& a, uint32_t pitch
 
 template <typename T, bool FOUR, bool ALIGNED> __global__ __launch_bounds__(kFewThreads) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
     extern __shared__ f32x4 dynamic[];
-    __shared__ uint32_t bits[32], token[TPERM_FEW_TOKENS];
-    __shared__ float weight[TPERM_FEW_TOKENS];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, count = a.tokens * a.slots;
-    int32_t* const number = (int32_t*)dynamic;
-    float* const given = (float*)dynamic + count;
-    if (threadIdx.x < 32) bits[threadIdx.x] = 0;
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < count; i += kFewThreads) {
-        const int32_t e = a.expert[i];
-        given[i] = a.weights != nullptr ? a.weights[i] : 1.0f;
-        number[i] = e;
-        if ((uint32_t)e < a.experts) atomicOr(&bits[(uint32_t)e / 32], 1u << (uint32_t)e % 32);
+    const Named n = find_named<kFewThreads, true>(a, dynamic + kFewWaves * a.images * 64, most);
+    const uint32_t channels = (a.hidden + kChannels - 1) / kChannels;
+    for (uint32_t item = blockIdx.x; item < n.total * channels; item += gridDim.x) {
+        const uint32_t rank = item / channels, channel = (item - rank * channels) * kChannels;
+        const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]), first = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]);
+        if (entry >> 16 <= 8) hidden_channels<T, FOUR, Shape<2, 1, false>, FOUR ? 2 : 4, ALIGNED>(a, pitch, n, entry, first, channel, dynamic);
+        else if (entry >> 16 <= 16) hidden_channels<T, FOUR, Shape<2, 1, true>, FOUR ? 1 : 4, ALIGNED>(a, pitch, n, entry, first, channel, dynamic);
+        else if (entry >> 16 <= 32) hidden_channels<T, FOUR, Shape<2, 2, true>, FOUR ? 1 : 2, ALIGNED>(a, pitch, n, entry, first, channel, dynamic);
+        else hidden_channels<T, FOUR, Shape<2, 4, true>, 1, ALIGNED>(a, pitch, n, entry, first, channel, dynamic);
     }
-    __syncthreads();
-    uint32_t total;
-    const uint32_t rank = blockIdx.y;
-    const uint32_t e = find_bit(bits, rank, &total);
-    if (blockIdx.x == 0 && rank == 0 && threadIdx.x == 0) a.tables[0] = (int32_t)total;
-    if (rank >= total) return;
-    // every wavefront: a lane to a token
-    uint32_t before = 0;
-    float w = 0.0f;
-    bool names = false;
-    if (lane < a.tokens)
-        for (uint32_t s = 0; s < a.slots; ++s) {
-            const uint32_t v = (uint32_t)number[lane * a.slots + s];
-            before += v < e;
-            if (v == e) w += given[lane * a.slots + s], names = true;
-        }
-    for (uint32_t d = 1; d < 64; d <<= 1) before += (uint32_t)__shfl_xor((int)before, d);
-    const uint64_t all = __ballot(names);
-    const uint32_t named = (uint32_t)__builtin_popcountll(all), first_row = (uint32_t)__builtin_amdgcn_readfirstlane((int)before);
-    if (wave == 0 && names) {
-        const uint32_t c = (uint32_t)__builtin_popcountll(all & ((1ull << lane) - 1));
-        token[c] = lane, weight[c] = w;
-        if (blockIdx.x == 0) a.tables[1 + 2 * most + first_row + c] = (int32_t)lane;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.tables[1 + rank] = (int32_t)(e | named << 16), a.tables[1 + most + rank] = (int32_t)first_row;
-    __syncthreads();
-    if (named <= 16) hidden_channels<T, FOUR, FOUR ? 2 : 4, ALIGNED, 1>(a, pitch, e, named, token, weight, first_row, dynamic);
-    else if (named <= 32) hidden_channels<T, FOUR, 2, ALIGNED, 2>(a, pitch, e, named, token, weight, first_row, dynamic);
-    else hidden_channels<T, FOUR, 1, ALIGNED, 4>(a, pitch, e, named, token, weight, first_row, dynamic);
 }
+
+constexpr uint32_t kOutWaves = 16, kOutThreads = 64 * kOutWaves, kTokenPitch = kChannels;     // kTokenPitch: of a token in a wavefront's array
 
 template <typename T, bool FOUR, int STEPS, bool ALIGNED, int M>
 __device__ __forceinline__ void result_channels(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
-                                                uint32_t to, float* sums, uint32_t sums_pitch) {
+                                                uint32_t to, float* sums) {
     typedef Matrix<T, FOUR> W;
     typedef Hidden<T, FOUR> H;
+    typedef Shape<1, M, false> S;
     const uint32_t lane = threadIdx.x & 63u, channel = blockIdx.x * kChannels;
     const W w = matrix_of<W>(a.w_out, a.out_scales, e, a.width, a.hidden);
-    const uint32_t row[1] = {channel + lane % 16 < a.width ? channel + lane % 16 : a.width - 1};
+    const uint32_t row[1] = {channel + S::row() < a.width ? channel + S::row() : a.width - 1};
     const typename H::E* x[M];
-    for (int m = 0; m < M; ++m) {
-        const uint32_t c = m * 16 + lane % 16;
-        x[m] = (const typename H::E*)a.rows + (int64_t)(first_row + (c < named ? c : 0)) * pitch;
-    }
+    for (int m = 0; m < M; ++m) x[m] = (const typename H::E*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
     const typename H::Columns cols = {(int64_t)a.tokens * a.slots * pitch};
     f32x4 sum[1][M] = {};
-    rows_by_columns<STEPS, ALIGNED>(w, row, cols, x, from, to, 0u, 1u, sum);
+    rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, from, to, 0u, 1u, sum);
+    // the diagonal: even pieces in lanes 0 .. 7 of the first two sixteens, odd ones 40 lanes on
     for (int m = 0; m < M; ++m) {
-        const uint32_t c = m * 16 + lane % 16;
-        if (c < named) {
-            f32x4* const at = (f32x4*)(sums + token[first_row + c] * sums_pitch + lane / 16 * 4);
-            *at += sum[0][m];
-        }
+        f32x4 y = sum[0][m];
+        for (int i = 0; i < 4; ++i) y[i] += __shfl(y[i], (int)(lane + 40));
+        if (lane < 32 && lane % 16 < 8 && S::column(m) < named) *(f32x4*)(sums + token[first_row + S::column(m)] * kTokenPitch + lane / 16 * 4) += y;
     }
 }
 
-template <typename T, bool FOUR, bool ALIGNED> __global__ __launch_bounds__(kFewThreads) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
+template <typename T, bool FOUR, bool ALIGNED> __global__ __launch_bounds__(kOutThreads) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
     extern __shared__ f32x4 dynamic[];
-    constexpr uint32_t kPitch = kChannels + 4, kSteps = FOUR ? 2 : 4, kBlock = kSteps * Matrix<T, FOUR>::kDepth;
-    const uint32_t wave = threadIdx.x >> 6, count = a.tokens * a.slots, words = 1 + 2 * most;
+    constexpr uint32_t kSteps = FOUR ? 2 : 8, kBlock = kSteps * Matrix<T, FOUR>::kDepth;
+    const uint32_t wave = threadIdx.x >> 6;
     float* const sums = (float*)dynamic;
-    int32_t* const tables = (int32_t*)(sums + kFewWaves * a.tokens * kPitch);
-    uint8_t* const token = (uint8_t*)(tables + words);
-    for (uint32_t i = threadIdx.x; i < words; i += kFewThreads) tables[i] = a.tables[i];
-    for (uint32_t i = threadIdx.x; i < count; i += kFewThreads) token[i] = (uint8_t)a.tables[words + i];
-    for (uint32_t i = threadIdx.x; i < kFewWaves * a.tokens * kPitch; i += kFewThreads) sums[i] = 0.0f;
-    __syncthreads();
-    const uint32_t total = (uint32_t)tables[0];
-    float* const mine = sums + wave * a.tokens * kPitch;
-    if (total != 0) {
+    for (uint32_t i = threadIdx.x; i < kOutWaves * a.tokens * kTokenPitch; i += kOutThreads) sums[i] = 0.0f;
+    const Named n = find_named<kOutThreads, false>(a, sums + kOutWaves * a.tokens * kTokenPitch, most);
+    float* const mine = sums + wave * a.tokens * kTokenPitch;
+    if (n.total != 0) {
         // an item: an expert and a piece of its sum
-        const uint32_t blocks = (a.hidden + kBlock - 1) / kBlock, want = (2 * kFewWaves + total - 1) / total, per = (blocks + want - 1) / want, pieces = (blocks + per - 1) / per;
-        for (uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane((int)wave); item < total * pieces; item += kFewWaves) {
+        const uint32_t blocks = (a.hidden + kBlock - 1) / kBlock, want = (2 * kOutWaves + n.total - 1) / n.total, per = (blocks + want - 1) / want, pieces = (blocks + per - 1) / per;
+        for (uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane((int)wave); item < n.total * pieces; item += kOutWaves) {
             const uint32_t rank = item / pieces, from = (item - rank * pieces) * per * kBlock, end = from + per * kBlock;
-            const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane(tables[1 + rank]), first_row = (uint32_t)__builtin_amdgcn_readfirstlane(tables[1 + most + rank]);
+            const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]), first_row = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]);
             const uint32_t e = entry & 0xFFFFu, named = entry >> 16, to = end < a.hidden ? end : a.hidden;
-            if (named <= 16) result_channels<T, FOUR, kSteps, ALIGNED, 1>(a, pitch, e, named, token, first_row, from, to, mine, kPitch);
-            else if (named <= 32) result_channels<T, FOUR, 2, ALIGNED, 2>(a, pitch, e, named, token, first_row, from, to, mine, kPitch);
-            else result_channels<T, FOUR, 1, ALIGNED, 4>(a, pitch, e, named, token, first_row, from, to, mine, kPitch);
+            if (named <= 8) result_channels<T, FOUR, kSteps, ALIGNED, 1>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            else if (named <= 16) result_channels<T, FOUR, FOUR ? 1 : 4, ALIGNED, 2>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            else if (named <= 32) result_channels<T, FOUR, FOUR ? 1 : 2, ALIGNED, 4>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            else result_channels<T, FOUR, 1, ALIGNED, 8>(a, pitch, e, named, n.token, first_row, from, to, mine);
         }
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < a.tokens * kChannels; i += kFewThreads) {
+    for (uint32_t i = threadIdx.x; i < a.tokens * kChannels; i += kOutThreads) {
         const uint32_t t = i / kChannels, c = i % kChannels;
         if (blockIdx.x * kChannels + c >= a.width) continue;
         float y = 0.0f;
-        for (uint32_t v = 0; v < kFewWaves; ++v) y += sums[(v * a.tokens + t) * kPitch + c];
+        for (uint32_t v = 0; v < kOutWaves; ++v) y += sums[(v * a.tokens + t) * kTokenPitch + c];
         ((T*)a.out)[(int64_t)t * a.out_stride + blockIdx.x * kChannels + c] = (T)y;
     }
 }
 
-template <typename T, bool FOUR> hipError_t go(const FewArgs& a, int type, hipStream_t stream) {
+template <typename T, bool FOUR> hipError_t go(FewArgs a, int type, hipStream_t stream) {
     const FewRoom room = few_room(a.tokens, a.slots, a.experts, a.hidden, type, FOUR);
-    const uint32_t count = a.tokens * a.slots, columns = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+    const uint32_t count = a.tokens * a.slots;
     const bool x_aligned = ((uintptr_t)a.x | (uintptr_t)a.x_stride * sizeof(T)) % 16 == 0 && a.width % 8 == 0;
     const bool in_aligned = x_aligned && (FOUR || ((uintptr_t)a.w_in | (uintptr_t)a.width * sizeof(T)) % 16 == 0);
     const bool out_aligned = a.hidden % 8 == 0 && (FOUR || ((uintptr_t)a.w_out | (uintptr_t)a.hidden * sizeof(T)) % 16 == 0);
-    const size_t joined = (size_t)kFewWaves * columns * 64 * 16, numbers = (size_t)count * 8;
-    const dim3 in_grid((a.hidden + kChannels - 1) / kChannels, room.most);
+    a.by_slots = make_fastdiv(a.slots);
+    a.images = a.tokens <= 32 ? 2 : 4;
+    const uint64_t items = (uint64_t)room.most * ((a.hidden + kChannels - 1) / kChannels);
     const auto in = in_aligned ? few_in_kernel<T, FOUR, true> : few_in_kernel<T, FOUR, false>;
-    hipLaunchKernelGGL(in, in_grid, dim3(kFewThreads), joined > numbers ? joined : numbers, stream, a, room.most, room.pitch);
+    hipLaunchKernelGGL(in, dim3((uint32_t)(items < kInGroups ? items : kInGroups)), dim3(kFewThreads),
+                       (size_t)kFewWaves * a.images * 64 * 16 + named_bytes(count, a.experts, room.most, true), stream, a, room.most, room.pitch);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const size_t sums = (size_t)kFewWaves * a.tokens * (kChannels + 4) * 4;
     const auto out = out_aligned ? few_out_kernel<T, FOUR, true> : few_out_kernel<T, FOUR, false>;
-    hipLaunchKernelGGL(out, dim3((a.width + kChannels - 1) / kChannels), dim3(kFewThreads), sums + (size_t)(1 + 2 * room.most) * 4 + count, stream, a, room.most, room.pitch);
+    hipLaunchKernelGGL(out, dim3((a.width + kChannels - 1) / kChannels), dim3(kOutThreads),
+                       (size_t)kOutWaves * a.tokens * kTokenPitch * 4 + named_bytes(count, a.experts, room.most, false), stream, a, room.most, room.pitch);
     return hipGetLastError();
 }
 
