@@ -51,21 +51,24 @@ struct FewArgs {
     int64_t x_stride, out_stride;
     uint32_t tokens, slots, experts, width, hidden;
     void* rows;                     // the workspace: the hidden rows
-    FastDiv by_slots;               // this and the next set by the launcher
-    uint32_t images;                // 16 x 16 products of the first kernel that a workgroup joins at most
+    FastDiv by_slots;               // set by the launcher
 };
 hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
 
 // Workspace of a few tokens' layer: hidden rows of named experts, in the order of their numbers.
+constexpr uint32_t few_most(int64_t tokens, int64_t slots, int64_t experts) {
+    const int64_t count = tokens * slots;
+    return (uint32_t)((experts < count ? experts : count) + count / 33);
+}
 struct FewRoom {
-    uint32_t most;          // named experts at most
+    uint32_t most;          // entries at most: one for every 32 tokens that name the same expert
     uint32_t pitch;         // elements of a hidden row
     size_t bytes;
 };
 inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t hidden, int type, bool four_bits) {
     FewRoom r;
     const int64_t count = tokens * slots;
-    r.most = (uint32_t)(experts < count ? experts : count);
+    r.most = few_most(tokens, slots, experts);
     r.pitch = (uint32_t)((hidden + 31) / 32 * 32);
     // one part of 4 bytes an element, two of 2, or three of 2
     r.bytes = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);

@@ -1,8 +1,7 @@
 // Choice and launch of the experts' product kernels for one element type; included once for each.
 #pragma once
-#include <atomic>
-
 #include "expert_product.hpp"
+#include "launch.hpp"
 
 namespace tperm {
 
@@ -14,19 +13,6 @@ using WideTile = TileShape<256, 256, 8, 4>;     // 64 x 128 results to a wavefro
 
 template <typename S> constexpr bool is(Tile t) { return S::kFast == kTileFast[(int)t] && S::kSlow == kTileSlow[(int)t]; }
 static_assert(is<TinyTile>(Tile::kTiny) && is<SmallTile>(Tile::kSmall) && is<NarrowTile>(Tile::kNarrow) && is<WideTile>(Tile::kWide), "as the query says");
-
-// Workgroups with more than 64 KiB of LDS have to be allowed it, once on each device.
-template <auto KERNEL> hipError_t allow_lds(size_t bytes) {
-    static std::atomic<uint64_t> done{0};
-    int device = 0;
-    hipError_t e = hipGetDevice(&device);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = 1ull << (device & 63);
-    if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
-    e = hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == hipSuccess) done.fetch_or(bit, std::memory_order_release);
-    return e;
-}
 
 template <auto KERNEL, typename S, typename A> hipError_t go(uint64_t blocks, const A& a, hipStream_t stream) {
     constexpr size_t kLds = S::kLds;

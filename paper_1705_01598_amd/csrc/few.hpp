@@ -70,6 +70,33 @@ __device__ __forceinline__ void pair_words(u32x4& a, u32x4& b) {
     }
 }
 
+// Which of a step's elements exist: all of them; those in front of the row's end; the same where a row is shorter than a lane's load.
+enum class Reach { kAll, kEnd, kShort };
+
+// N elements of a row of `depth` from element i on, zeros for those behind its end: without a branch around the load, behind which the
+// compiler would wait for it.  ALIGNED: depth is a multiple of N, and so is i; else elements that hang over the end are the row's
+// last N, moved down.
+template <Reach REACH, typename T, int N, bool ALIGNED> __device__ __forceinline__ Vec<T, N> load_reach(const T* row, uint32_t i, uint32_t depth) {
+    static_assert(N * sizeof(T) == 16, "a lane's load");
+    if constexpr (REACH == Reach::kAll) {
+        return load_vec<T, N, ALIGNED>(row + i);
+    } else if constexpr (REACH == Reach::kShort) {
+        return load_some<T, N, false>(i < depth ? row + i : row, (int)depth - (int)i);
+    } else if constexpr (ALIGNED) {
+        const Vec<T, N> v = load_vec<T, N, true>(row + (i < depth ? i : 0u));
+        u32x4 w = __builtin_bit_cast(u32x4, v);
+        for (int k = 0; k < 4; ++k) w[k] = i < depth ? w[k] : 0u;
+        return __builtin_bit_cast(Vec<T, N>, w);
+    } else {
+        const uint32_t from = i < depth - N ? i : depth - N, over = i - from;
+        const Vec<uint64_t, 2> v = __builtin_bit_cast(Vec<uint64_t, 2>, load_vec<T, N, false>(row + from));
+        const uint32_t bits = over * 8 * (uint32_t)sizeof(T);
+        const uint64_t high = bits < 64 ? v[1] >> bits : 0u;
+        const uint64_t low = bits == 0 ? v[0] : bits < 64 ? v[0] >> bits | v[1] << (64 - bits) : bits < 128 ? v[1] >> (bits - 64) : 0u;
+        return __builtin_bit_cast(Vec<T, N>, Vec<uint64_t, 2>{low, high});
+    }
+}
+
 // A matrix of elements of T: 16 bytes to a lane and step.
 template <typename T> struct Elements {
     static constexpr int kEach = 16 / sizeof(T), kDepth = 8 * kEach, kSub = 1;      // elements of a lane and of a row in a step; products of a step
@@ -77,13 +104,11 @@ template <typename T> struct Elements {
     const T* rows;
     uint32_t stride;                    // bytes from row to row
     struct Step { Part v; };
-    template <bool ALIGNED> __device__ __forceinline__ Step load(uint32_t row, uint32_t i) const {
-        return {load_vec<T, kEach, ALIGNED>((const T*)((const char*)rows + (row * stride + i * (uint32_t)sizeof(T))))};
+    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Step load(uint32_t row, uint32_t i, uint32_t depth) const {
+        if constexpr (REACH == Reach::kAll) return {load_vec<T, kEach, ALIGNED>((const T*)((const char*)rows + (row * stride + i * (uint32_t)sizeof(T))))};
+        else return {load_reach<REACH, T, kEach, ALIGNED>((const T*)((const char*)rows + row * stride), i, depth)};
     }
-    template <bool ALIGNED> __device__ __forceinline__ Step load_some_of(uint32_t row, uint32_t i, int there) const {
-        return {load_some<T, kEach, ALIGNED>((const T*)((const char*)rows + (row * stride + (there > 0 ? i : 0u) * (uint32_t)sizeof(T))), there)};
-    }
-    static __device__ __forceinline__ void open(const Step& s, Part (&part)[kSub]) { part[0] = s.v; }
+    static __device__ __forceinline__ Part open(const Step& s, int) { return s.v; }
     static __device__ __forceinline__ void pair(Step& a, Step& b) {
         u32x4 p = __builtin_bit_cast(u32x4, a.v), q = __builtin_bit_cast(u32x4, b.v);
         pair_words(p, q);
@@ -99,22 +124,20 @@ struct FourBits {
     const uint8_t *rows, *scales;
     uint32_t groups;                    // of a row
     struct Step { u32x4 codes; uint32_t scale; };
-    template <bool ALIGNED> __device__ __forceinline__ Step load(uint32_t row, uint32_t i) const {
-        const uint32_t g = row * groups + i / 32;
-        return {*(const u32x4*)(rows + (uint64_t)(g * 16u)), scales[g]};
+    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Step load(uint32_t row, uint32_t i, uint32_t depth) const {
+        const bool there = REACH == Reach::kAll || i < depth;
+        const uint32_t g = row * groups + (there ? i / 32 : 0u);
+        Step s = {*(const u32x4*)(rows + (uint64_t)(g * 16u)), scales[g]};
+        for (int k = 0; k < 4; ++k) s.codes[k] = there ? s.codes[k] : 0u;
+        s.scale = there ? s.scale : 127u;
+        return s;
     }
-    template <bool ALIGNED> __device__ __forceinline__ Step load_some_of(uint32_t row, uint32_t i, int there) const {
-        if (there > 0) return load<ALIGNED>(row, i);
-        return {u32x4{}, 127u};
-    }
-    static __device__ __forceinline__ void open(const Step& s, Part (&part)[kSub]) {
+    static __device__ __forceinline__ Part open(const Step& s, int j) {
         const float scale = scale_value(s.scale);
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t w = s.codes[j];
-            const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
-            const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
-            part[j] = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-        }
+        const uint32_t w = s.codes[j];
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+        return {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
     static __device__ __forceinline__ void pair(Step& a, Step& b) {
         pair_words(a.codes, b.codes);
@@ -128,25 +151,32 @@ template <typename E, int P> struct Ready {
     static constexpr int kParts = P, N = 16 / sizeof(E);
     int64_t apart;
     typedef Vec<E, N> Part;
-    // sub-product j of a step in which a lane has EACH elements from i on, `there` of which exist
-    template <int EACH, bool ALIGNED, bool ALL> __device__ __forceinline__ void get(const E* x, uint32_t i, int there, int j, Part (&part)[P]) const {
-        for (int p = 0; p < P; ++p) {
-            const E* const at = x + p * apart + i + j * N;
-            part[p] = ALL ? load_vec<E, N, ALIGNED>(at) : load_some<E, N, ALIGNED>(there - j * N > 0 ? at : x, there - j * N);
-        }
+    struct Raw { Part part[P]; };
+    // sub-product j of a lane's elements from i on
+    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const E* x, uint32_t i, uint32_t depth, int j) const {
+        Raw r;
+        for (int p = 0; p < P; ++p) r.part[p] = load_reach<REACH, E, N, ALIGNED>(x + p * apart, i + j * N, depth);
+        return r;
+    }
+    static __device__ __forceinline__ void open(const Raw& r, Part (&part)[P]) {
+        for (int p = 0; p < P; ++p) part[p] = r.part[p];
     }
 };
 // Columns of T that become bfloat16 parts on their way.
 template <typename T> struct Split {
     static constexpr int kParts = sizeof(T) == 4 ? 3 : std::is_same_v<T, _Float16> ? 2 : 1;
     typedef bf16x8 Part;
-    template <int EACH, bool ALIGNED, bool ALL> __device__ __forceinline__ void get(const T* x, uint32_t i, int there, int j, Part (&part)[kParts]) const {
-        const T* const at = x + i + j * 8;
-        Vec<T, 8> v;
-        if constexpr (ALL) v = load_vec<T, 8, ALIGNED>(at);
-        else v = load_some<T, 8, ALIGNED>(there - j * 8 > 0 ? at : x, there - j * 8);
-        if constexpr (kParts == 1) part[0] = __builtin_bit_cast(bf16x8, v);
-        else parts_of<kParts>(widen<T, 8>(v), part);
+    typedef Vec<T, 8> Eight;
+    static constexpr int kLoads = sizeof(T) / 2, N = 16 / sizeof(T);
+    struct Raw { Vec<T, N> v[kLoads]; };
+    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const T* x, uint32_t i, uint32_t depth, int j) const {
+        Raw r;
+        for (int k = 0; k < kLoads; ++k) r.v[k] = load_reach<REACH, T, N, ALIGNED>(x, i + j * 8 + k * N, depth);
+        return r;
+    }
+    static __device__ __forceinline__ void open(const Raw& r, Part (&part)[kParts]) {
+        if constexpr (kParts == 1) part[0] = __builtin_bit_cast(bf16x8, r.v[0]);
+        else parts_of<kParts>(widen<T, 8>(__builtin_bit_cast(Eight, r.v)), part);
     }
 };
 
@@ -170,9 +200,8 @@ template <typename S> __device__ __forceinline__ f32x4 sums_at(const f32x4* wave
     else return wave_sums[(tile * S::M + m) * 64 + 16 * half + c] + wave_sums[(tile * S::M + m) * 64 + 16 * (2 + half) + 8 + c];
 }
 
-// STEPS steps of one wavefront from element `i` on: sum += rows row[r] by columns x[m].  ALL: every element of the steps
-// exists, else those below `depth`.
-template <typename S, int STEPS, bool ALIGNED, bool ALL, typename W, typename X, typename E>
+// STEPS steps of one wavefront from element `i` on: sum += rows row[r] by columns x[m], rows of `depth` elements.
+template <typename S, int STEPS, bool ALIGNED, Reach REACH, typename W, typename X, typename E>
 __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], const X& cols, const E* const (&x)[S::M], uint32_t i, uint32_t depth,
                                       f32x4 (&sum)[S::kSums][S::M]) {
     constexpr int R = S::R, M = S::M;
@@ -182,8 +211,7 @@ __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], c
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint32_t at = i + t * W::kDepth + S::piece() * W::kEach;
-            if constexpr (ALL) s[t][r] = w.template load<ALIGNED>(row[r], at);
-            else s[t][r] = w.template load_some_of<ALIGNED>(row[r], at, (int)depth - (int)at);
+            s[t][r] = w.template load<REACH, ALIGNED>(row[r], at, depth);
         }
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) {
@@ -195,34 +223,47 @@ __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], c
 #pragma unroll
         for (int turn = 0; turn < kTurns; ++turn) {
             const uint32_t at = i + t * W::kDepth + (S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece()) * W::kEach;
-            typename W::Part part[S::kSums][W::kSub];
+            // columns are requested in front of the products, as many as 64 registers hold
+            constexpr int kHeld = 64 / (M * (int)sizeof(typename X::Raw) / 4), kAhead = kHeld < 2 ? 1 : kHeld < W::kSub ? 2 : W::kSub;
 #pragma unroll
-            for (int r = 0; r < S::kSums; ++r) W::open(s[t][S::kPaired ? 2 * r + turn : r], part[r]);
+            for (int j0 = 0; j0 < W::kSub; j0 += kAhead) {
+                typename X::Raw raw[kAhead][M];
 #pragma unroll
-            for (int m = 0; m < M; ++m)
+                for (int j = 0; j < kAhead; ++j)
 #pragma unroll
-                for (int j = 0; j < W::kSub; ++j) {
-                    typename X::Part c[X::kParts];
-                    cols.template get<W::kEach, ALIGNED, ALL>(x[m], at, (int)depth - (int)at, j, c);
+                    for (int m = 0; m < M; ++m)
+                        raw[j][m] = cols.template load<REACH, ALIGNED>(x[m], at, depth, j0 + j);
 #pragma unroll
-                    for (int p = 0; p < X::kParts; ++p)
+                for (int j = 0; j < kAhead; ++j) {
+                    typename X::Part c[M][X::kParts];
 #pragma unroll
-                        for (int r = 0; r < S::kSums; ++r) sum[r][m] = multiply(part[r][j], c[p], sum[r][m]);
+                    for (int m = 0; m < M; ++m) X::open(raw[j][m], c[m]);
+#pragma unroll
+                    for (int r = 0; r < S::kSums; ++r) {
+                        const typename W::Part part = W::open(s[t][S::kPaired ? 2 * r + turn : r], j0 + j);
+#pragma unroll
+                        for (int m = 0; m < M; ++m)
+#pragma unroll
+                            for (int p = 0; p < X::kParts; ++p) sum[r][m] = multiply(part, c[m][p], sum[r][m]);
+                    }
                 }
+            }
         }
     }
 }
 
 // The piece of the sum from `from` to `to` (a multiple of the steps' depth away, or the row's end) that falls to wavefront `wave`
-// of `waves`.
+// of `waves`: blocks of that depth in turn.
 template <typename S, int STEPS, bool ALIGNED, typename W, typename X, typename E>
 __device__ __forceinline__ void rows_by_columns(const W& w, const uint32_t (&row)[S::R], const X& cols, const E* const (&x)[S::M], uint32_t from, uint32_t to,
                                                 uint32_t wave, uint32_t waves, f32x4 (&sum)[S::kSums][S::M]) {
     constexpr uint32_t kBlock = STEPS * W::kDepth;
     uint32_t i = from + wave * kBlock;
-    for (; i + kBlock <= to; i += waves * kBlock) steps<S, STEPS, ALIGNED, true>(w, row, cols, x, i, to, sum);
-    for (int t = 0; t < STEPS; ++t, i += W::kDepth)
-        if (i < to) steps<S, 1, ALIGNED, false>(w, row, cols, x, i, to, sum);
+    for (; i + kBlock <= to; i += waves * kBlock) steps<S, STEPS, ALIGNED, Reach::kAll>(w, row, cols, x, i, to, sum);
+    if (i >= to) return;
+    if (!ALIGNED && to < 8) steps<S, 1, ALIGNED, Reach::kShort>(w, row, cols, x, i, to, sum);
+    else if (STEPS > 2 && to - i <= W::kDepth) steps<S, 1, ALIGNED, Reach::kEnd>(w, row, cols, x, i, to, sum);
+    else steps<S, STEPS, ALIGNED, Reach::kEnd>(w, row, cols, x, i, to, sum);
 }
 
 }  // namespace tperm

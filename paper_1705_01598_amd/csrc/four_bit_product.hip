@@ -41,6 +41,7 @@ template <typename T, bool ALIGNED, int STEPS, typename S> __global__ __launch_b
 }
 
 template <typename T, bool ALIGNED, int STEPS, typename S> hipError_t go(const FourBitProductArgs& a, hipStream_t stream) {
+    static_assert(S::kSums * S::M <= 8, "LDS that needs no leave");
     const uint32_t chunks = (a.rows + 63) / 64;
     // a launch has at most 65535 workgroups along the second dimension of its grid here
     FourBitProductArgs part = a;
@@ -56,10 +57,19 @@ template <typename T, bool ALIGNED, int STEPS, typename S> hipError_t go(const F
     return hipSuccess;
 }
 template <typename T, bool ALIGNED> hipError_t product_of(const FourBitProductArgs& a, hipStream_t stream) {
-    if (a.rows <= 8) return a.n <= 4096 ? go<T, ALIGNED, 2, Shape<1, 1, false>>(a, stream) : go<T, ALIGNED, 2, Shape<2, 1, false>>(a, stream);
-    if (a.rows <= 16) return a.n <= 8192 ? go<T, ALIGNED, 1, Shape<2, 1, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 1, true>>(a, stream);
-    if (a.rows <= 32) return go<T, ALIGNED, 1, Shape<2, 2, true>>(a, stream);
-    return go<T, ALIGNED, 1, Shape<2, 4, true>>(a, stream);
+    // 256 compute units want a workgroup each
+    const uint32_t tiles = (a.n + 7) / 8;
+    if (a.rows <= 8) return tiles < 512 ? go<T, ALIGNED, 2, Shape<1, 1, false>>(a, stream) : tiles < 1024 ? go<T, ALIGNED, 2, Shape<2, 1, false>>(a, stream)
+                          : tiles < 2048 ? go<T, ALIGNED, 1, Shape<4, 1, false>>(a, stream) : go<T, ALIGNED, 1, Shape<8, 1, false>>(a, stream);
+    if (a.rows <= 16) return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 1, true>>(a, stream) : tiles < 2048 ? go<T, ALIGNED, 1, Shape<4, 1, true>>(a, stream)
+                           : tiles < 4096 ? go<T, ALIGNED, 1, Shape<8, 1, true>>(a, stream) : go<T, ALIGNED, 1, Shape<16, 1, true>>(a, stream);
+    if (a.rows <= 32) {
+        if constexpr (sizeof(T) == 2)
+            if (tiles >= 2048) return go<T, ALIGNED, 1, Shape<8, 2, true>>(a, stream);
+        return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 2, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 2, true>>(a, stream);
+    }
+    if (a.rows <= 48) return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 3, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 3, true>>(a, stream);
+    return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 4, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 4, true>>(a, stream);
 }
 
 }  // namespace
