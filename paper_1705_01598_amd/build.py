@@ -18,11 +18,11 @@ SOURCES = ["plan.cpp", "model.cpp", "product_plan.cpp", "api.cpp", "cache.cpp", 
            "tile_inst_u64_64.hip", "tile_inst_u32_64.hip", "tile_inst_big_u64.hip", "tile_inst_big_u32.hip",
            "tile_inst_lean_u64.hip", "tile_inst_lean_u32.hip",
            "tile_inst_tab_u64.hip", "tile_inst_tab_u32.hip",
-           "decode_api.cpp", "route.hip", "four_bit.hip", "four_bit_product.hip", "few.hip",
+           "decode_api.cpp", "route.hip", "four_bit.hip", "four_bit_product.hip", "few_f32.hip", "few_f16.hip", "few_bf16.hip",
            "experts_api.cpp", "expert_sort.hip", "expert_rows.hip", "checkpoint.hip",
            "expert_product_f32.hip", "expert_product_f16.hip", "expert_product_bf16.hip"]
 HEADERS = ["fastcall.cpp", "pattern_probe.hip", "latency_probe.hip", "plan.hpp", "kernels.hpp", "verify.hpp", "product.hpp", "tperm_desc.h", "tile_kernel.hpp",
-           "checks.hpp", "decode.hpp", "few.hpp", "gated.hpp", "launch.hpp", os.path.join("..", "..", "include", "tperm_decode.h"),
+           "checks.hpp", "decode.hpp", "few.hpp", "few_layer.hpp", "gated.hpp", "launch.hpp", os.path.join("..", "..", "include", "tperm_decode.h"),
            "experts.hpp", "expert_vector.hpp", "expert_product.hpp", "expert_product_inst.hpp", os.path.join("..", "..", "include", "tperm_experts.h"), os.path.join("..", "..", "include", "tperm.h"),
            os.path.join("..", "..", "include", "tperm_tuning.h")]
 

@@ -50,28 +50,44 @@ struct FewArgs {
     void* out;
     int64_t x_stride, out_stride;
     uint32_t tokens, slots, experts, width, hidden;
-    void* rows;                     // the workspace: the hidden rows
+    void* rows;                     // the workspace: the hidden rows, and behind them (set by the launcher) shares of results and counters
+    float* shares;
+    uint32_t* ended;
     FastDiv by_slots;               // set by the launcher
 };
 hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
 
-// Workspace of a few tokens' layer: hidden rows of named experts, in the order of their numbers.
+constexpr uint32_t kFewChannels = 8;        // of a tile
+constexpr uint32_t kFewShareTiles = 4;      // of a workgroup of the second kernel where workgroups share the entries of their channels
+
+// How a few tokens' layer is laid out in its workspace: hidden rows in the order of the experts that are named; the shares of the second kernel's
+// workgroups, and a counter to every group of channels that is shared.
 constexpr uint32_t few_most(int64_t tokens, int64_t slots, int64_t experts) {
     const int64_t count = tokens * slots;
     return (uint32_t)((experts < count ? experts : count) + count / 33);
 }
+// Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of matrices on.
+inline uint32_t few_shares(uint64_t blocks, uint32_t most, uint64_t matrix_bytes) {
+    const uint64_t want = over(512, blocks);
+    return most * matrix_bytes < 64 << 20 ? 1 : (uint32_t)(want < most ? want : most);
+}
 struct FewRoom {
     uint32_t most;          // entries at most: one for every 32 tokens that name the same expert
     uint32_t pitch;         // elements of a hidden row
-    size_t bytes;
+    uint32_t shares;        // workgroups that share the entries of the same channels
+    size_t rows, partial, bytes;
 };
-inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t hidden, int type, bool four_bits) {
+inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t width, int64_t hidden, int type, bool four_bits) {
     FewRoom r;
     const int64_t count = tokens * slots;
     r.most = few_most(tokens, slots, experts);
     r.pitch = (uint32_t)((hidden + 31) / 32 * 32);
     // one part of 4 bytes an element, two of 2, or three of 2
-    r.bytes = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
+    r.rows = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
+    const uint64_t blocks = over(width, kFewShareTiles * kFewChannels);
+    r.shares = few_shares(blocks, r.most, (uint64_t)width * hidden * (four_bits ? 1 : 2 * type_bytes(type)) / 2);
+    r.partial = r.shares == 1 ? 0 : (size_t)r.shares * blocks * tokens * kFewShareTiles * kFewChannels * 4;
+    r.bytes = r.rows + r.partial + (r.shares == 1 ? 0 : blocks * 4);
     return r;
 }
 

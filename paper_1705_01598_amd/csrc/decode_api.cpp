@@ -4,6 +4,13 @@
 #include "checks.hpp"
 #include "decode.hpp"
 
+namespace tperm {
+template <typename T> hipError_t few_of(const FewArgs& a, int type, hipStream_t stream);
+hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream) {
+    return type == TPERM_TYPE_F32 ? few_of<float>(a, type, stream) : type == TPERM_TYPE_F16 ? few_of<_Float16>(a, type, stream) : few_of<__bf16>(a, type, stream);
+}
+}  // namespace tperm
+
 using namespace tperm;
 
 extern "C" {
@@ -107,7 +114,7 @@ static tperm_status_t few_sizes(int64_t tokens, int64_t slots, int64_t experts, 
 
 size_t tperm_expert_few_workspace(int64_t tokens, int64_t slots, int64_t experts, int64_t width, int64_t hidden, int type, int four_bits) {
     if (few_sizes(tokens, slots, experts, width, hidden, type) != TPERM_OK || tokens == 0) return 0;
-    return few_room(tokens, slots, experts, hidden, type, four_bits != 0).bytes;
+    return few_room(tokens, slots, experts, width, hidden, type, four_bits != 0).bytes;
 }
 
 tperm_status_t tperm_expert_few(const void* x, int64_t x_stride, const int32_t* expert, const float* weights, const void* w_in,
@@ -124,7 +131,7 @@ tperm_status_t tperm_expert_few(const void* x, int64_t x_stride, const int32_t* 
     const int64_t in_bytes = four ? in_groups * 16 : 2 * hidden * width * (int64_t)elem, out_bytes = four ? out_groups * 16 : hidden * width * (int64_t)elem;
     if (in_bytes > kOperandBytes || out_bytes > kOperandBytes) return TPERM_ERR_TOO_LARGE;
     if (tokens == 0) return TPERM_OK;
-    const size_t need = few_room(tokens, slots, experts, hidden, type, four).bytes;
+    const size_t need = few_room(tokens, slots, experts, width, hidden, type, four).bytes;
     const Array arrays[] = {{x, matrix_bytes(tokens, x_stride, width, elem), elem, false},
                             {expert, tokens * slots * 4, 4, false},
                             {weights, weights ? tokens * slots * 4 : 0, 4, false},

@@ -146,8 +146,9 @@ struct FourBits {
     static __device__ __forceinline__ float scale_value(uint32_t biased) { return __uint_as_float(biased == 255u ? 0x7FC00000u : biased << 23); }
 };
 
-// Columns that are there as the products take them: kParts arrays of E, `apart` elements from each other.
-template <typename E, int P> struct Ready {
+// Columns that are there as the products take them: kParts arrays of E, `apart` elements from each other.  FILLED: they are zeros up to a whole step,
+// and start on 16 bytes.
+template <typename E, int P, bool FILLED = false> struct Ready {
     static constexpr int kParts = P, N = 16 / sizeof(E);
     int64_t apart;
     typedef Vec<E, N> Part;
@@ -155,7 +156,7 @@ template <typename E, int P> struct Ready {
     // sub-product j of a lane's elements from i on
     template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const E* x, uint32_t i, uint32_t depth, int j) const {
         Raw r;
-        for (int p = 0; p < P; ++p) r.part[p] = load_reach<REACH, E, N, ALIGNED>(x + p * apart, i + j * N, depth);
+        for (int p = 0; p < P; ++p) r.part[p] = load_reach<FILLED ? Reach::kAll : REACH, E, N, ALIGNED || FILLED>(x + p * apart, i + j * N, depth);
         return r;
     }
     static __device__ __forceinline__ void open(const Raw& r, Part (&part)[P]) {
@@ -204,50 +205,77 @@ template <typename S> __device__ __forceinline__ f32x4 sums_at(const f32x4* wave
 template <typename S, int STEPS, bool ALIGNED, Reach REACH, typename W, typename X, typename E>
 __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], const X& cols, const E* const (&x)[S::M], uint32_t i, uint32_t depth,
                                       f32x4 (&sum)[S::kSums][S::M]) {
-    constexpr int R = S::R, M = S::M;
+    constexpr int R = S::R, M = S::M, kTurns = S::kPaired ? 2 : 1;      // paired: first the even pieces of both tiles, then the odd ones
+    const auto there = [&](int t) { return REACH == Reach::kAll || i + t * W::kDepth < depth; };
     typename W::Step s[STEPS][R];
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const uint32_t at = i + t * W::kDepth + S::piece() * W::kEach;
-            s[t][r] = w.template load<REACH, ALIGNED>(row[r], at, depth);
-        }
+        for (int r = 0; r < R; ++r) s[t][r] = w.template load<REACH, ALIGNED>(row[r], i + t * W::kDepth + S::piece() * W::kEach, depth);
+    const auto columns_of = [&](int t, int turn, int j, int m) {
+        const uint32_t at = i + t * W::kDepth + (S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece()) * W::kEach;
+        return cols.template load<REACH, ALIGNED>(x[m], at, depth, j);
+    };
+    const auto products = [&](int t, int turn, int j, const typename X::Raw (&raw)[M]) {
+        typename X::Part c[M][X::kParts];
 #pragma unroll
-    for (int t = 0; t < STEPS; ++t) {
+        for (int m = 0; m < M; ++m) X::open(raw[m], c[m]);
+#pragma unroll
+        for (int r = 0; r < S::kSums; ++r) {
+            const typename W::Part part = W::open(s[t][S::kPaired ? 2 * r + turn : r], j);
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int p = 0; p < X::kParts; ++p) sum[r][m] = multiply(part, c[m][p], sum[r][m]);
+        }
+    };
+    const auto paired = [&](int t) {
         if constexpr (S::kPaired)
 #pragma unroll
             for (int r = 0; r < R; r += 2) W::pair(s[t][r], s[t][r + 1]);
-        // paired: first the even pieces of both tiles, then the odd ones
-        constexpr int kTurns = S::kPaired ? 2 : 1;
+    };
+    // Columns are requested in front of the products, all of them where they fit 32 registers, else what half of a turn needs, or less.  The
+    // fence is for the compiler, which would move the requests down to the products, until a few are under way at a time.
+    constexpr int kWords = M * (int)sizeof(typename X::Raw) / 4;
+    if constexpr (STEPS * kTurns * W::kSub * kWords <= 32) {
+        typename X::Raw raw[STEPS][kTurns][W::kSub][M];
 #pragma unroll
-        for (int turn = 0; turn < kTurns; ++turn) {
-            const uint32_t at = i + t * W::kDepth + (S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece()) * W::kEach;
-            // columns are requested in front of the products, as many as 64 registers hold
-            constexpr int kHeld = 64 / (M * (int)sizeof(typename X::Raw) / 4), kAhead = kHeld < 2 ? 1 : kHeld < W::kSub ? 2 : W::kSub;
+        for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-            for (int j0 = 0; j0 < W::kSub; j0 += kAhead) {
-                typename X::Raw raw[kAhead][M];
+            for (int turn = 0; turn < kTurns; ++turn)
 #pragma unroll
-                for (int j = 0; j < kAhead; ++j)
+                for (int j = 0; j < W::kSub; ++j)
 #pragma unroll
-                    for (int m = 0; m < M; ++m)
-                        raw[j][m] = cols.template load<REACH, ALIGNED>(x[m], at, depth, j0 + j);
+                    for (int m = 0; m < M; ++m) raw[t][turn][j][m] = columns_of(t, turn, j, m);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < kAhead; ++j) {
-                    typename X::Part c[M][X::kParts];
+        for (int t = 0; t < STEPS; ++t) {
+            if (!there(t)) break;
+            paired(t);
 #pragma unroll
-                    for (int m = 0; m < M; ++m) X::open(raw[j][m], c[m]);
+            for (int turn = 0; turn < kTurns; ++turn)
 #pragma unroll
-                    for (int r = 0; r < S::kSums; ++r) {
-                        const typename W::Part part = W::open(s[t][S::kPaired ? 2 * r + turn : r], j0 + j);
+                for (int j = 0; j < W::kSub; ++j) products(t, turn, j, raw[t][turn][j]);
+        }
+    } else {
+        constexpr int kHeld = 32 / kWords, kAhead = kHeld < 2 ? 1 : kHeld < W::kSub ? 2 : W::kSub;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int m = 0; m < M; ++m)
+        for (int t = 0; t < STEPS; ++t) {
+            if (!there(t)) break;
 #pragma unroll
-                            for (int p = 0; p < X::kParts; ++p) sum[r][m] = multiply(part, c[m][p], sum[r][m]);
-                    }
+            for (int turn = 0; turn < kTurns; ++turn)
+#pragma unroll
+                for (int j0 = 0; j0 < W::kSub; j0 += kAhead) {
+                    typename X::Raw raw[kAhead][M];
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) raw[j][m] = columns_of(t, turn, j0 + j, m);
+                    if (turn == 0 && j0 == 0) paired(t);
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j) products(t, turn, j0 + j, raw[j]);
                 }
-            }
         }
     }
 }

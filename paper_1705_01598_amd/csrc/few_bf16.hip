@@ -1,0 +1,7 @@
+#include "few_layer.hpp"
+
+namespace tperm {
+
+template hipError_t few_of<__bf16>(const FewArgs&, int, hipStream_t);
+
+}  // namespace tperm

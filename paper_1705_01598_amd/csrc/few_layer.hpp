@@ -1,0 +1,433 @@
+// A whole mixture-of-experts layer for a few tokens, in two kernels.
+//
+// The first multiplies the g and u rows of 8 hidden channels of a named expert (an item) with the tokens that name it, applies the gated
+// activation and the token's weight, and stores the hidden rows in parts; a workgroup goes through every so-many-th
+// item.  The second: a workgroup to 8 channels of the result goes through all named experts, its wavefronts share
+// experts and pieces of their sums, and add up by token in LDS, one array for each wavefront, joined in their order: no
+// atomics on numbers that round, and no rows of the experts in memory.
+// Every workgroup of both finds the named experts and their tokens from the numbers themselves (at most 64 x 64 of
+// them), so no order has to be made first.
+#pragma once
+#include <type_traits>
+
+#include "decode.hpp"
+#include "few.hpp"
+#include "gated.hpp"
+#include "launch.hpp"
+#include "plan.hpp"
+
+namespace tperm {
+
+namespace {
+
+constexpr uint32_t kChannels = kFewChannels;
+constexpr int kShareTiles = kFewShareTiles;
+constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit
+constexpr size_t kInLds = 80 * 1024, kOutLds = 112 * 1024;
+constexpr uint32_t kColumns = 32;       // tokens of an entry at most
+constexpr uint32_t kImages = 2;         // 16 x 16 products of an item of the first kernel at most
+
+// What the second product's columns are: how a hidden row is held between the kernels.
+template <typename T, bool FOUR> struct Hidden {
+    typedef std::conditional_t<FOUR, __bf16, T> E;
+    static constexpr int kParts = !FOUR && sizeof(T) == 4 ? 1 : FOUR && sizeof(T) == 4 ? 3 : 2;
+    typedef Ready<E, kParts> Columns;
+};
+template <typename T, bool FOUR> using Matrix = std::conditional_t<FOUR, FourBits, Elements<T>>;
+// The first product's columns: the tokens as they lie, or, where all of them fit it, from LDS, with rows that are filled up with zeros and
+// in the parts that a matrix in 4 bits takes.
+template <typename T, bool FOUR, bool STAGED> struct Tokens {
+    typedef std::conditional_t<FOUR, Split<T>, Ready<T, 1>> Columns;
+    typedef T E;
+};
+template <typename T, bool FOUR> struct Tokens<T, FOUR, true> {
+    typedef std::conditional_t<FOUR, __bf16, T> E;
+    static constexpr int kParts = FOUR ? Split<T>::kParts : 1;
+    typedef Ready<E, kParts, true> Columns;
+};
+// Elements of a staged row: whole steps, and 16 bytes more so that rows start at different banks.
+template <typename T, bool FOUR> constexpr uint32_t staged_pitch(uint32_t width) {
+    typedef Matrix<T, FOUR> W;
+    return (width + W::kDepth - 1) / W::kDepth * W::kDepth + 16 / sizeof(typename Tokens<T, FOUR, true>::E);
+}
+template <typename T, bool FOUR> constexpr size_t staged_bytes(uint32_t tokens, uint32_t width) {
+    return (size_t)tokens * staged_pitch<T, FOUR>(width) * sizeof(typename Tokens<T, FOUR, true>::E) * Tokens<T, FOUR, true>::kParts;
+}
+template <typename T, bool FOUR, bool ALIGNED> __device__ __forceinline__ void stage(const FewArgs& a, typename Tokens<T, FOUR, true>::E* rows) {
+    typedef typename Tokens<T, FOUR, true>::E E;
+    constexpr int kParts = Tokens<T, FOUR, true>::kParts;
+    const uint32_t pitch = staged_pitch<T, FOUR>(a.width), eights = pitch / 8;     // the 16 bytes more are left as they are
+    for (uint32_t i = threadIdx.x; i < a.tokens * eights; i += kFewThreads) {
+        const uint32_t t = i / eights, at = (i - t * eights) * 8;
+        Vec<T, 8> v = {};
+        if (at < a.width) v = load_some<T, 8, ALIGNED>((const T*)a.x + (int64_t)t * a.x_stride + at, (int)(a.width - at));
+        E* const row = rows + t * pitch + at;
+        if constexpr (!FOUR) {
+            store_vec<T, 8, true>(row, v);
+        } else {
+            bf16x8 part[kParts];
+            if constexpr (kParts == 1) part[0] = v;
+            else parts_of<kParts>(widen<T, 8>(v), part);
+            for (int p = 0; p < kParts; ++p) store_vec<__bf16, 8, true>(row + p * a.tokens * pitch, part[p]);
+        }
+    }
+}
+
+// The rows of expert e's matrix.
+template <typename M> __device__ __forceinline__ M matrix_of(const void* p, const uint8_t* scales, uint32_t e, uint32_t rows, uint32_t depth) {
+    M m;
+    if constexpr (std::is_same_v<M, FourBits>) {
+        m.groups = (depth + 31) / 32;
+        const uint64_t before = (uint64_t)e * rows * m.groups;
+        m.rows = (const uint8_t*)p + before * 16, m.scales = scales + before;
+    } else {
+        m.stride = depth * (uint32_t)sizeof(*m.rows);
+        m.rows = (decltype(m.rows))((const char*)p + (uint64_t)e * rows * m.stride);
+    }
+    return m;
+}
+
+// What the numbers say, in LDS.  An entry is up to kColumns tokens that name the same expert, in the order of experts: its number and how
+// many tokens (<< 16), and their first hidden row; by hidden row there is its token and, for the first kernel, its weight.
+struct Named {
+    uint32_t* mask;         // two words an expert, a bit to a token
+    uint32_t* entry;
+    float* weight;
+    uint16_t *first, *number, *start;
+    uint8_t* token;
+    uint32_t total;         // entries
+};
+constexpr size_t named_bytes(size_t count, size_t experts, size_t most, bool weights) {
+    return (experts * 8 + most * 4 + (weights ? count * 4 : 0) + most * 2 + count * 2 + experts * 2 + count + 15) / 16 * 16;
+}
+
+// Sums over the lanes up to this one.
+__device__ __forceinline__ uint32_t upto(uint32_t v) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, true);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);     // the last lane of a row to the next one
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);     // of the first half to the second
+    return v;
+}
+
+template <uint32_t THREADS, bool WEIGHTS> __device__ __forceinline__ Named find_named(const FewArgs& a, void* lds, uint32_t most) {
+    static_assert(2 * THREADS >= TPERM_EXPERTS_MAX, "two experts to a thread");
+    __shared__ uint32_t wave_total[THREADS / 64], twice;
+    const uint32_t count = a.tokens * a.slots, wave = threadIdx.x >> 6;
+    Named n;
+    n.mask = (uint32_t*)lds, n.entry = n.mask + 2 * a.experts, n.weight = (float*)(n.entry + most), n.first = (uint16_t*)(n.weight + (WEIGHTS ? count : 0));
+    n.number = n.first + most, n.start = n.number + count, n.token = (uint8_t*)(n.start + a.experts);
+    int32_t own = -1;
+    float own_weight = 1.0f;
+    if (threadIdx.x < count) {
+        own = a.expert[threadIdx.x];
+        if (WEIGHTS && a.weights != nullptr) own_weight = a.weights[threadIdx.x];
+    }
+    for (uint32_t i = threadIdx.x; i < 2 * a.experts; i += THREADS) n.mask[i] = 0;
+    if (threadIdx.x == 0) twice = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        const uint32_t e = (uint32_t)(i < THREADS ? own : a.expert[i]), t = fdiv(i, a.by_slots);
+        const bool there = e < a.experts;
+        n.number[i] = (uint16_t)(there ? e : 0xFFFFu);
+        if (there) {
+            const uint32_t bit = 1u << t % 32, before = atomicOr(&n.mask[2 * e + t / 32], bit);
+            if (WEIGHTS && (before & bit)) twice = 1;
+        }
+    }
+    __syncthreads();
+    // entries and rows before each expert: entries in the low half
+    const uint32_t each = a.experts <= THREADS ? 1 : 2, e0 = threadIdx.x * each;
+    uint32_t names[2] = {};
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+        if (k < each && e0 + k < a.experts) names[k] = (uint32_t)__builtin_popcount(n.mask[2 * (e0 + k)]) + (uint32_t)__builtin_popcount(n.mask[2 * (e0 + k) + 1]);
+    static_assert(TPERM_FEW_TOKENS <= 2 * kColumns, "two entries an expert at most");
+    const auto entries = [](uint32_t tokens) { return (uint32_t)(tokens != 0) + (uint32_t)(tokens > kColumns); };
+    const uint32_t mine = (names[0] + names[1]) << 16 | (entries(names[0]) + entries(names[1]));
+    const uint32_t up = upto(mine);
+    if ((threadIdx.x & 63u) == 63) wave_total[wave] = up;
+    __syncthreads();
+    uint32_t before = up - mine, all = 0;
+#pragma unroll
+    for (uint32_t v = 0; v < THREADS / 64; ++v) {
+        before += v < wave ? wave_total[v] : 0u;
+        all += wave_total[v];
+    }
+    n.total = (uint32_t)__builtin_amdgcn_readfirstlane((int)(all & 0xFFFFu));
+#pragma unroll
+    for (uint32_t k = 0; k < 2; ++k)
+        if (names[k] != 0) {
+            const uint32_t at = before & 0xFFFFu, row = before >> 16, more = names[k] > kColumns ? names[k] - kColumns : 0u;
+            n.entry[at] = (e0 + k) | (names[k] - more) << 16;
+            n.first[at] = (uint16_t)row;
+            if (more != 0) n.entry[at + 1] = (e0 + k) | more << 16, n.first[at + 1] = (uint16_t)(row + kColumns);
+            n.start[e0 + k] = (uint16_t)row;
+            before += names[k] << 16 | entries(names[k]);
+        }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        const uint32_t e = n.number[i], t = fdiv(i, a.by_slots);
+        if (e == 0xFFFFu) continue;
+        const uint64_t named = n.mask[2 * e] | (uint64_t)n.mask[2 * e + 1] << 32;
+        const uint32_t row = n.start[e] + (uint32_t)__builtin_popcountll(named & ((1ull << t) - 1));
+        n.token[row] = (uint8_t)t;
+        if constexpr (WEIGHTS) {
+            float w = i < THREADS ? own_weight : a.weights != nullptr ? a.weights[i] : 1.0f;
+            if (twice) {        // all slots of the token that name this expert write the same sum
+                w = 0.0f;
+                for (uint32_t s = t * a.slots; s < (t + 1) * a.slots; ++s)
+                    if (n.number[s] == e) w += a.weights != nullptr ? a.weights[s] : 1.0f;
+            }
+            n.weight[row] = w;
+        }
+    }
+    __syncthreads();
+    return n;
+}
+
+// An item of the first kernel: an entry and 8 hidden channels, of which wavefront `wave` of `waves` adds up its piece.
+struct Item {
+    uint32_t expert, named, first, channel, wave, waves;
+};
+template <typename T, bool FOUR, bool STAGED, typename S, int STEPS, bool ALIGNED>
+__device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, const Item& item, f32x4* sums, const typename Tokens<T, FOUR, true>::E* staged) {
+    typedef Matrix<T, FOUR> W;
+    const W w = matrix_of<W>(a.w_in, a.in_scales, item.expert, 2 * a.hidden, a.width);
+    const uint32_t g = item.channel + S::row() < a.hidden ? item.channel + S::row() : a.hidden - 1;
+    const uint32_t row[2] = {g, g + a.hidden};
+    const typename Tokens<T, FOUR, STAGED>::E* x[S::M];
+    typename Tokens<T, FOUR, STAGED>::Columns cols = {};
+    for (int m = 0; m < S::M; ++m) {
+        const uint32_t t = n.token[item.first + (S::column(m) < item.named ? S::column(m) : 0)];
+        if constexpr (STAGED) x[m] = staged + t * staged_pitch<T, FOUR>(a.width);
+        else x[m] = (const T*)a.x + (int64_t)t * a.x_stride;
+    }
+    if constexpr (STAGED) cols.apart = a.tokens * staged_pitch<T, FOUR>(a.width);
+    f32x4 sum[S::kSums][S::M] = {};
+    rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, item.wave, item.waves, sum);
+    static_assert(S::kSums * S::M <= (int)kImages, "a wavefront's place");
+    for (int r = 0; r < S::kSums; ++r)
+        for (int m = 0; m < S::M; ++m) sums[(item.wave * kImages + r * S::M + m) * 64 + threadIdx.x % 64] = sum[r][m];
+}
+// The sums of all wavefronts of an item, the activation, and the hidden rows in parts: four channels of one column to a lane.
+template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, uint32_t pitch, const Named& n, const Item& item, const f32x4* sums) {
+    typedef Hidden<T, FOUR> H;
+    for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < S::M * 2 * S::kColumns; i += item.waves * 64) {
+        const uint32_t m = i / (2 * S::kColumns), half = i / S::kColumns % 2, c = i % S::kColumns, column = m * S::kColumns + c;
+        if (column >= item.named) continue;
+        f32x4 gu[2] = {};
+        for (uint32_t v = 0; v < item.waves; ++v)
+            for (int r = 0; r < 2; ++r) gu[r] += sums_at<S>(sums + v * kImages * 64, r, m, half, c);
+        const float weight = n.weight[item.first + column];
+        f32x4 h;
+        for (int k = 0; k < 4; ++k) {
+            const Sigmoid s = sigmoid<float>(gu[0][k]);
+            h[k] = gu[0][k] * s.p * gu[1][k] * s.last * weight;
+        }
+        const int64_t rows = (int64_t)a.tokens * a.slots;
+        typename H::E* const out = (typename H::E*)a.rows + (int64_t)(item.first + column) * pitch + item.channel + half * 4;
+        for (int p = 0; p < H::kParts; ++p) {
+            const Vec<typename H::E, 4> part = narrow<typename H::E, 4>(h);
+            store_vec<typename H::E, 4, true>(out + p * rows * pitch, part);
+            const f32x4 back = widen<typename H::E, 4>(part);
+            for (int k = 0; k < 4; ++k) h[k] = __builtin_isfinite(back[k]) ? h[k] - back[k] : 0.0f;
+        }
+    }
+}
+
+template <typename T, bool FOUR, bool STAGED, bool ALIGNED, bool X_ALIGNED>
+__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch, const uint32_t shares) {
+    extern __shared__ f32x4 dynamic[];
+    typedef Matrix<T, FOUR> W;
+    typedef Shape<2, 1, false> Few;
+    typedef Shape<2, 1, true> Some;
+    typedef Shape<2, 2, true> Many;
+    constexpr uint32_t kPlace = kFewWaves * kImages * 64;      // of all wavefronts' sums; two of them, used in turn
+    typedef typename Tokens<T, FOUR, true>::E E;
+    E* const staged = (E*)(dynamic + 2 * kPlace);
+    if constexpr (STAGED) stage<T, FOUR, X_ALIGNED>(a, staged);
+    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T, FOUR>(a.tokens, a.width) : 0), most);
+    if (blockIdx.x == 0 && shares != 1)     // counters of the second kernel
+        for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
+    const uint32_t channels = (a.hidden + kChannels - 1) / kChannels, items = n.total * channels, steps = (a.width + W::kDepth - 1) / W::kDepth;
+    // Eight loads in flight a wavefront where there are more than four for each, else one step to each; a workgroup's wavefronts
+    // share as many items as that leaves them.
+    constexpr int kSteps = FOUR ? 2 : 4;
+    const bool long_steps = items * steps * 2 > 4 * 2 * kInGroups * kFewWaves;
+    const uint32_t pieces = long_steps ? (steps + kSteps - 1) / kSteps : steps, waves = pieces > 4 ? 8 : pieces > 2 ? 4 : pieces, at_once = kFewWaves / waves;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave / waves;
+    f32x4* place = dynamic + group * waves * kImages * 64;
+    for (uint32_t base = blockIdx.x * at_once; base < items; base += gridDim.x * at_once) {
+        Item item = {};
+        if (base + group < items) {
+            const uint32_t rank = (base + group) / channels, entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]);
+            item = {entry & 0xFFFFu, entry >> 16, (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]), (base + group - rank * channels) * kChannels, wave % waves, waves};
+            if (item.named <= 8 && long_steps) hidden_sums<T, FOUR, STAGED, Few, kSteps, ALIGNED>(a, n, item, place, staged);
+            else if (item.named <= 8) hidden_sums<T, FOUR, STAGED, Few, 1, ALIGNED>(a, n, item, place, staged);
+            else if (item.named <= 16) hidden_sums<T, FOUR, STAGED, Some, FOUR ? 1 : 4, ALIGNED>(a, n, item, place, staged);
+            else hidden_sums<T, FOUR, STAGED, Many, FOUR ? 1 : 2, ALIGNED>(a, n, item, place, staged);
+        }
+        __syncthreads();
+        if (item.named == 0) {
+        } else if (item.named <= 8) hidden_rows<T, FOUR, Few>(a, pitch, n, item, place);
+        else if (item.named <= 16) hidden_rows<T, FOUR, Some>(a, pitch, n, item, place);
+        else hidden_rows<T, FOUR, Many>(a, pitch, n, item, place);
+        place = place < dynamic + kPlace ? place + kPlace : place - kPlace;
+    }
+}
+
+// What lane l + 40 holds, for the lanes l of the first half whose l % 16 is below 8.
+__device__ __forceinline__ float forty_on(float v) {
+    const uint32_t w = (uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x128, 0xF, 0xF, true);      // row_ror:8
+    return __uint_as_float(__builtin_amdgcn_permlane32_swap(w, w, false, false)[1]);
+}
+
+// Workgroups of the second kernel.  With one tile of 8 channels: 16 wavefronts, all entries.  With four: 8 wavefronts and a share of
+// the entries, the shares of the same channels added by the workgroup that comes to its end last.
+template <int R> constexpr uint32_t kOutWaves = R == 1 ? 16 : 8;
+
+template <typename T, bool FOUR, typename S, int STEPS, bool ALIGNED>
+__device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
+                                            uint32_t to, float* sums) {
+    typedef Matrix<T, FOUR> W;
+    typedef Hidden<T, FOUR> H;
+    constexpr int R = S::R, M = S::M;
+    const uint32_t lane = threadIdx.x & 63u, channel = blockIdx.x * (R * kChannels);
+    const W w = matrix_of<W>(a.w_out, a.out_scales, e, a.width, a.hidden);
+    uint32_t row[R];
+    for (int r = 0; r < R; ++r) {
+        const uint32_t j = channel + r * kChannels + S::row();
+        row[r] = j < a.width ? j : a.width - 1;
+    }
+    const typename H::E* x[M];
+    for (int m = 0; m < M; ++m) x[m] = (const typename H::E*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
+    const typename H::Columns cols = {(int64_t)a.tokens * a.slots * pitch};
+    f32x4 sum[S::kSums][M] = {};
+    rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, from, to, 0u, 1u, sum);
+    for (int m = 0; m < M; ++m) {
+        if constexpr (!S::kPaired)
+            for (int r = 0; r < R; ++r)
+                for (int i = 0; i < 4; ++i) sum[r][m][i] += forty_on(sum[r][m][i]);
+        if ((!S::kPaired && (lane >= 32 || lane % 16 >= 8)) || S::column(m) >= named) continue;
+        float* const at = sums + token[first_row + S::column(m)] * (R * kChannels) + lane / 16 * 4;
+        for (int r = 0; r < S::kSums; ++r) *(f32x4*)(at + r * (S::kPaired ? 2 : 1) * kChannels) += sum[r][m];
+    }
+}
+
+template <typename T, bool FOUR, bool ALIGNED, int R>
+__global__ __launch_bounds__(64 * kOutWaves<R>, 4) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
+    extern __shared__ f32x4 dynamic[];
+    constexpr uint32_t kWaves = kOutWaves<R>, kThreads = 64 * kWaves, kSteps = R == 1 ? (FOUR ? 2 : 8) : (FOUR ? 1 : 2), kBlock = kSteps * Matrix<T, FOUR>::kDepth;
+    constexpr uint32_t kRows = R * kChannels;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    float* const sums = (float*)dynamic;
+    for (uint32_t i = threadIdx.x; i < kWaves * a.tokens * kRows; i += kThreads) sums[i] = 0.0f;
+    const Named n = find_named<kThreads, false>(a, sums + kWaves * a.tokens * kRows, most);
+    float* const mine = sums + wave * a.tokens * kRows;
+    const uint32_t begin = n.total * blockIdx.y / gridDim.y, entries = n.total * (blockIdx.y + 1) / gridDim.y - begin;
+    if (entries != 0) {
+        // an item: an entry and a piece of its sum
+        const uint32_t blocks = (a.hidden + kBlock - 1) / kBlock, want = (2 * kWaves + entries - 1) / entries, per = (blocks + want - 1) / want, pieces = (blocks + per - 1) / per;
+        for (uint32_t item = wave; item < entries * pieces; item += kWaves) {
+            const uint32_t rank = begin + item / pieces, from = item % pieces * per * kBlock, end = from + per * kBlock;
+            const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]), first_row = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]);
+            const uint32_t e = entry & 0xFFFFu, named = entry >> 16, to = end < a.hidden ? end : a.hidden;
+            if (named <= 8) result_sums<T, FOUR, Shape<R, 1, false>, kSteps, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            else if constexpr (R == 1) {
+                if (named <= 16) result_sums<T, FOUR, Shape<R, 2, false>, FOUR ? 1 : 4, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+                else result_sums<T, FOUR, Shape<R, 4, false>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            } else {
+                if (named <= 16) result_sums<T, FOUR, Shape<R, 1, true>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+                else result_sums<T, FOUR, Shape<R, 2, true>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t first = blockIdx.x * kRows, channels = a.width - first < kRows ? a.width - first : kRows;
+    const auto joined = [&](uint32_t t, uint32_t c) {
+        float y = 0.0f;
+        for (uint32_t v = 0; v < kWaves; ++v) y += sums[(v * a.tokens + t) * kRows + c];
+        return y;
+    };
+    if (gridDim.y == 1) {
+        for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads)
+            if (i % kRows < channels) ((T*)a.out)[(int64_t)(i / kRows) * a.out_stride + first + i % kRows] = (T)joined(i / kRows, i % kRows);
+        return;
+    }
+    // The share goes out, the workgroup counts itself, and the one that finds all others counted adds up the shares in their order.  Shares are stored
+    // and loaded at agent scope, past every cache that not all compute units see, and a wavefront waits until its stores are complete before
+    // the barrier behind which one thread counts; so who sees the count sees the shares.  A release at agent scope would also write back
+    // the L2 with all that is in it, for each workgroup: 64 tokens x 8 of 128 experts 86 -> 102 us.
+    float* const shares = a.shares + (int64_t)blockIdx.x * gridDim.y * a.tokens * kRows;
+    for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads)
+        __hip_atomic_store(shares + (int64_t)blockIdx.y * a.tokens * kRows + i, joined(i / kRows, i % kRows), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __shared__ uint32_t before;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) before = __hip_atomic_fetch_add(a.ended + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (before + 1 != gridDim.y) return;
+    for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads) {
+        float y = 0.0f;
+        for (uint32_t v = 0; v < gridDim.y; ++v) y += __hip_atomic_load(shares + (int64_t)v * a.tokens * kRows + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (i % kRows < channels) ((T*)a.out)[(int64_t)(i / kRows) * a.out_stride + first + i % kRows] = (T)y;
+    }
+}
+
+template <bool B> using Bool = std::integral_constant<bool, B>;
+
+template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream_t stream) {
+    const FewRoom room = few_room(a.tokens, a.slots, a.experts, a.width, a.hidden, type, FOUR);
+    a.shares = (float*)((char*)a.rows + room.rows), a.ended = (uint32_t*)((char*)a.shares + room.partial);
+    const uint32_t count = a.tokens * a.slots;
+    const auto on_eights = [](const void* p, uint64_t stride, uint32_t width) { return ((uintptr_t)p | stride * sizeof(T)) % 16 == 0 && width % 8 == 0; };
+    const bool x_aligned = on_eights(a.x, a.x_stride, a.width);
+    const bool in_aligned = FOUR || on_eights(a.w_in, a.width, a.width), out_aligned = FOUR ? a.hidden % 8 == 0 : on_eights(a.w_out, a.hidden, a.hidden);
+    a.by_slots = make_fastdiv(a.slots);
+    const uint64_t items = (uint64_t)room.most * ((a.hidden + kChannels - 1) / kChannels);
+    const size_t in_lds = (size_t)2 * kFewWaves * kImages * 64 * 16 + named_bytes(count, a.experts, room.most, true), staged = staged_bytes<T, FOUR>(a.tokens, a.width);
+    const auto launch_in = [&](auto in_lds_too, auto aligned, auto x_is) {
+        constexpr bool kStaged = decltype(in_lds_too)::value;
+        constexpr auto kKernel = few_in_kernel<T, FOUR, kStaged, decltype(aligned)::value, decltype(x_is)::value>;
+        const size_t lds = in_lds + (kStaged ? staged : 0);
+        const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kInLds) : hipSuccess;
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kKernel, dim3((uint32_t)(items < kInGroups ? items : kInGroups)), dim3(kFewThreads), lds, stream, a, room.most, room.pitch, room.shares);
+        return hipGetLastError();
+    };
+    const auto launch_out = [&](auto aligned, auto tiles) {
+        constexpr int kTiles = decltype(tiles)::value;
+        constexpr auto kKernel = few_out_kernel<T, FOUR, decltype(aligned)::value, kTiles>;
+        const size_t lds = (size_t)kOutWaves<kTiles> * a.tokens * kTiles * kChannels * 4 + named_bytes(count, a.experts, room.most, false);
+        const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kOutLds) : hipSuccess;
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kKernel, dim3((a.width + kTiles * kChannels - 1) / (kTiles * kChannels), kTiles == 1 ? 1 : room.shares), dim3(64 * kOutWaves<kTiles>), lds, stream,
+                           a, room.most, room.pitch);
+        return hipGetLastError();
+    };
+    hipError_t e = hipSuccess;
+    if (FOUR && items >= 4 * kInGroups && in_lds + staged <= kInLds) {
+        if constexpr (FOUR) e = x_aligned ? launch_in(Bool<true>(), Bool<true>(), Bool<true>()) : launch_in(Bool<true>(), Bool<true>(), Bool<false>());
+    } else {
+        e = in_aligned && x_aligned ? launch_in(Bool<false>(), Bool<true>(), Bool<true>()) : launch_in(Bool<false>(), Bool<false>(), Bool<false>());
+    }
+    if (e != hipSuccess) return e;
+    const auto launch_shared = [&](auto aligned) {
+        return room.shares == 1 ? launch_out(aligned, std::integral_constant<int, 1>()) : launch_out(aligned, std::integral_constant<int, kShareTiles>());
+    };
+    return out_aligned ? launch_shared(Bool<true>()) : launch_shared(Bool<false>());
+}
+
+static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX, few_most(TPERM_FEW_TOKENS, TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX), true) <=
+                  kInLds - 2 * kFewWaves * kImages * 64 * 16, "LDS of two workgroups");
+static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX, few_most(TPERM_FEW_TOKENS, TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX), false) <=
+                  kOutLds - 8 * TPERM_FEW_TOKENS * kShareTiles * kChannels * 4, "LDS of a workgroup of the second kernel");
+
+}  // namespace
+
+template <typename T> hipError_t few_of(const FewArgs& a, int type, hipStream_t stream) { return a.in_scales != nullptr ? layer<T, true>(a, type, stream) : layer<T, false>(a, type, stream); }
+
+}  // namespace tperm

@@ -11,7 +11,7 @@ namespace {
 template <typename T, bool ALIGNED, int STEPS, typename S> __global__ __launch_bounds__(kFewThreads) void four_bit_product_kernel(const FourBitProductArgs a) {
     extern __shared__ f32x4 sums[];
     constexpr int R = S::R, M = S::M, kEach = S::kSums * M;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, first = blockIdx.x * R * 8, first_row = blockIdx.y * 64;
+    const uint32_t lane = threadIdx.x & 63u, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), first = blockIdx.x * R * 8, first_row = blockIdx.y * 64;
     const FourBits w = {a.codes, a.scales, (a.k + 31) / 32};
     uint32_t row[R];
     for (int r = 0; r < R; ++r) {
