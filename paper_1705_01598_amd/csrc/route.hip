@@ -1,8 +1,13 @@
 // The router's choice: the largest scores of every token, their softmax, and its gradient.
 //
-// A group of 16 or 64 lanes to a token, every lane some of its scores in registers as whole numbers that order as the scores
-// do.  A round finds the largest number of the group by DPP moves, then the lowest expert that has it, and strikes it out; the
-// lane whose turn it is keeps it for the softmax.  Scores are read once; the rounds are what there is to compute.
+// A group of lanes to a token, every lane some of its scores in registers as numbers that order as the scores do.  Up to 8 slots:
+// every lane sorts its scores eight (or four) at a time, two sorted lists become the best eight of both by one comparison
+// of each with the other in reverse and a bitonic merge, first in a lane, then between lanes by DPP moves.  A score's expert is part of
+// its number (the lower, the larger), so that no two are equal and a comparison is one instruction for the larger and one for
+// the smaller: whole numbers of 32 bits where scores have 16, doubles where they have 32.  More slots: a round for each finds the
+// largest number of the group and strikes it out.
+#include <type_traits>
+
 #include "decode.hpp"
 #include "expert_vector.hpp"
 #include "plan.hpp"
@@ -35,16 +40,170 @@ template <int LANES, typename F> __device__ __forceinline__ uint32_t over_group(
 }
 template <int LANES> __device__ __forceinline__ uint32_t largest(uint32_t v) { return over_group<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
 template <int LANES> __device__ __forceinline__ uint32_t least(uint32_t v) { return over_group<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
-// Sums in an order that is the same for every lane: pairs at a distance, and addition of two does not depend on which is first.
+// Sums, the same bits in every lane: who adds does not matter to a sum of two.
 template <int LANES> __device__ __forceinline__ float total(float v) {
-    for (int d = 1; d < LANES; d <<= 1) v += __shfl_xor(v, d);
+    const auto add = [&](uint32_t o) { v += __uint_as_float(o); };
+    add(moved<0xB1>(__float_as_uint(v)));           // 1 0 3 2
+    add(moved<0x4E>(__float_as_uint(v)));           // 2 3 0 1
+    if constexpr (LANES > 4) add(moved<0x141>(__float_as_uint(v)));     // mirrored in 8 lanes
+    if constexpr (LANES > 8) add(moved<0x140>(__float_as_uint(v)));     // and in 16
+    if constexpr (LANES > 16) v += __shfl_xor(v, 16);
+    if constexpr (LANES > 32) v += __shfl_xor(v, 32);
     return v;
 }
 
-// exp(score - most), 1 for the largest also where that is infinite.
-__device__ __forceinline__ float part_of(float v, float most) { return v == most ? 1.0f : expf(v - most); }
+// exp(score - most), 1 for the largest also where that is infinite; 2^x with what x * log2(e) rounds off put right, which leaves
+// 2^-23 for exp2 and 2^-24 |x| for the difference.
+__device__ __forceinline__ float part_of(float v, float most) {
+    constexpr float kLog = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f;     // log2(e) and what that rounds off
+    const float x = v - most, p = x * kLog, rest = __builtin_fmaf(x, kRest, __builtin_fmaf(x, kLog, -p));
+    float e = __builtin_amdgcn_exp2f(p);
+    e = __builtin_fmaf(e, rest * 0.6931472f, e);
+    e = x < -104.0f ? 0.0f : e;         // also where rest is no number
+    return v == most ? 1.0f : e;
+}
 
-// V scores a lane: expert v * LANES + lane.
+// Numbers that order as the scores of T do, equal ones by expert, none equal to another; without its expert 0 if barred.
+template <typename T> struct Ordered {
+    typedef uint32_t Key;
+    static __device__ __forceinline__ Key key(T v, uint32_t expert) {
+        constexpr uint32_t kInfinity = std::is_same_v<T, _Float16> ? 0x7C00u : 0x7F80u;
+        uint32_t b = __builtin_bit_cast(uint16_t, v);
+        const uint32_t size = b & 0x7FFFu;
+        b = size == 0 ? 0u : b;                     // one zero
+        const bool barred = size > kInfinity || b == (0x8000u | kInfinity);
+        return (barred ? 0u : (b & 0x8000u) ? b ^ 0xFFFFu : b | 0x8000u) << 16 | (TPERM_EXPERTS_MAX - 1 - expert);
+    }
+    static __device__ __forceinline__ uint32_t expert(Key k) { return TPERM_EXPERTS_MAX - 1 - (k & 0xFFFFu); }
+    static __device__ __forceinline__ bool barred(Key k) { return k >> 16 == 0; }
+    static __device__ __forceinline__ float score(Key k) {
+        const uint32_t b = k >> 16;
+        return (float)__builtin_bit_cast(T, (uint16_t)(b & 0x8000u ? b & 0x7FFFu : b ^ 0xFFFFu));
+    }
+    static __device__ __forceinline__ Key high(Key a, Key b) { return a > b ? a : b; }
+    static __device__ __forceinline__ Key low(Key a, Key b) { return a < b ? a : b; }
+};
+// The score's bits as the high word of a double, which orders as they do (only a NaN's would make one), and behind them the expert, complemented
+// under a negative sign; minus infinity is barred.
+template <> struct Ordered<float> {
+    typedef double Key;
+    static __device__ __forceinline__ Key key(float v, uint32_t expert) {
+        const uint32_t b = __float_as_uint(__builtin_fmaxf(v + 0.0f, -__builtin_inff()));      // one zero; NaN as minus infinity
+        return __builtin_bit_cast(double, (uint64_t)b << 32 | (uint32_t)((int32_t)b >> 31 ^ (int32_t)(TPERM_EXPERTS_MAX - 1 - expert)));
+    }
+    static __device__ __forceinline__ uint32_t bits(Key k) { return (uint32_t)(__builtin_bit_cast(uint64_t, k) >> 32); }
+    static __device__ __forceinline__ uint32_t expert(Key k) {
+        return TPERM_EXPERTS_MAX - 1 - ((uint32_t)__builtin_bit_cast(uint64_t, k) ^ (uint32_t)((int32_t)bits(k) >> 31));
+    }
+    static __device__ __forceinline__ bool barred(Key k) { return bits(k) == 0xFF800000u; }
+    static __device__ __forceinline__ float score(Key k) { return __uint_as_float(bits(k)); }
+    static __device__ __forceinline__ Key high(Key a, Key b) { return __builtin_fmax(a, b); }
+    static __device__ __forceinline__ Key low(Key a, Key b) { return __builtin_fmin(a, b); }
+};
+template <int CTRL> __device__ __forceinline__ uint32_t from_lane(uint32_t v) { return moved<CTRL>(v); }
+template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)moved<CTRL>((uint32_t)(b >> 32)) << 32 | moved<CTRL>((uint32_t)b));
+}
+__device__ __forceinline__ uint32_t across(uint32_t v, int lanes) { return (uint32_t)__shfl_xor((int)v, lanes); }
+__device__ __forceinline__ double across(double v, int lanes) { return __shfl_xor(v, lanes); }
+
+template <typename O, int I, int J, int P> __device__ __forceinline__ void exchange(typename O::Key (&k)[P]) {
+    const typename O::Key a = k[I], b = k[J];
+    k[I] = O::high(a, b), k[J] = O::low(a, b);
+}
+// Largest first; networks of 19 and 5 exchanges.
+template <typename O> __device__ __forceinline__ void sort(typename O::Key (&k)[8]) {
+    exchange<O, 0, 2>(k), exchange<O, 1, 3>(k), exchange<O, 4, 6>(k), exchange<O, 5, 7>(k);
+    exchange<O, 0, 4>(k), exchange<O, 1, 5>(k), exchange<O, 2, 6>(k), exchange<O, 3, 7>(k);
+    exchange<O, 0, 1>(k), exchange<O, 2, 3>(k), exchange<O, 4, 5>(k), exchange<O, 6, 7>(k);
+    exchange<O, 2, 4>(k), exchange<O, 3, 5>(k);
+    exchange<O, 1, 4>(k), exchange<O, 3, 6>(k);
+    exchange<O, 1, 2>(k), exchange<O, 3, 4>(k), exchange<O, 5, 6>(k);
+}
+template <typename O> __device__ __forceinline__ void sort(typename O::Key (&k)[4]) {
+    exchange<O, 0, 1>(k), exchange<O, 2, 3>(k), exchange<O, 0, 2>(k), exchange<O, 1, 3>(k), exchange<O, 1, 2>(k);
+}
+// The best P of a sorted list and another one, sorted.
+template <typename O, int P, typename F> __device__ __forceinline__ void merge(typename O::Key (&k)[P], F other) {
+    typename O::Key both[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) both[i] = O::high(k[i], other(P - 1 - i));
+#pragma unroll
+    for (int i = 0; i < P; ++i) k[i] = both[i];
+    if constexpr (P == 8) exchange<O, 0, 4>(k), exchange<O, 1, 5>(k), exchange<O, 2, 6>(k), exchange<O, 3, 7>(k);
+    if constexpr (P == 8) exchange<O, 4, 6>(k), exchange<O, 5, 7>(k);
+    exchange<O, 0, 2>(k), exchange<O, 1, 3>(k);
+    if constexpr (P == 8) exchange<O, 4, 5>(k), exchange<O, 6, 7>(k);
+    exchange<O, 0, 1>(k), exchange<O, 2, 3>(k);
+}
+
+// Up to P slots, V scores a lane.  ALIGNED: rows of whole 16 bytes, which a lane takes in turn with its neighbours.
+template <typename T, int LANES, int V, int P, bool ALIGNED> __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteArgs a, const bool over_all) {
+    typedef Ordered<T> O;
+    typedef typename O::Key Key;
+    constexpr int C = ALIGNED ? 16 / (int)sizeof(T) : 1;
+    static_assert(V % C == 0 && V % P == 0, "whole loads and lists");
+    const uint32_t lane = threadIdx.x % LANES;
+    const uint64_t t = long_block() * (kRouteThreads / LANES) + threadIdx.x / LANES;
+    const uint64_t token = t < a.tokens ? t : a.tokens - 1;
+    const T* const row = (const T*)a.scores + (int64_t)token * a.scores_stride;
+    const auto expert_of = [&](int v) { return (uint32_t)(v / C * LANES * C + lane * C + v % C); };
+    T score[V];
+#pragma unroll
+    for (int v = 0; v < V; v += C) {
+        const uint32_t e = expert_of(v);
+        const Vec<T, C> part = load_vec<T, C, ALIGNED>(row + (e < a.experts ? e : 0u));
+        for (int c = 0; c < C; ++c) score[v + c] = part[c];
+    }
+    Key list[V / P][P];
+#pragma unroll
+    for (int v = 0; v < V; ++v) list[v / P][v % P] = O::key(expert_of(v) < a.experts ? score[v] : (T)-__builtin_inff(), expert_of(v));
+#pragma unroll
+    for (int l = 0; l < V / P; ++l) sort<O>(list[l]);
+#pragma unroll
+    for (int l = 1; l < V / P; ++l) merge<O, P>(list[0], [&](int i) { return list[l][i]; });
+    Key(&best)[P] = list[0];
+    merge<O, P>(best, [&](int i) { return from_lane<0xB1>(best[i]); });                                    // 1 0 3 2
+    merge<O, P>(best, [&](int i) { return from_lane<0x4E>(best[i]); });                                    // 2 3 0 1
+    if constexpr (LANES > 4) merge<O, P>(best, [&](int i) { return from_lane<0x141>(best[i]); });          // mirrored in 8 lanes
+    if constexpr (LANES > 8) merge<O, P>(best, [&](int i) { return from_lane<0x140>(best[i]); });          // and in 16
+    if constexpr (LANES > 16) merge<O, P>(best, [&](int i) { return across(best[i], 16); });
+    if constexpr (LANES > 32) merge<O, P>(best, [&](int i) { return across(best[i], 32); });
+    const float most = O::score(best[0]);
+    // lane l holds slots l, l + LANES, ...
+    constexpr int kKept = LANES < P ? P / LANES : 1;
+    Key kept[kKept];
+    float part[kKept], sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) {
+        kept[k] = best[k * LANES];
+#pragma unroll
+        for (int l = 1; l < LANES && k * LANES + l < P; ++l) kept[k] = lane == (uint32_t)l ? best[k * LANES + l] : kept[k];
+        part[k] = k * LANES + lane < a.slots && !O::barred(kept[k]) ? part_of(O::score(kept[k]), most) : 0.0f;
+        sum += part[k];
+    }
+    if (over_all) {
+        sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float s = (float)score[v];
+            sum += expert_of(v) < a.experts && s > -__builtin_inff() ? part_of(s, most) : 0.0f;
+        }
+    }
+    sum = total<LANES>(sum);
+    if (t >= a.tokens) return;
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) {
+        const uint32_t s = k * LANES + lane;
+        if (s >= a.slots) continue;
+        const bool there = s < (uint32_t)P && !O::barred(kept[k]);
+        a.expert[token * a.slots + s] = there ? (int32_t)O::expert(kept[k]) : -1;
+        a.weights[token * a.slots + s] = there ? part[k] / sum : 0.0f;
+    }
+}
+
+// Any number of slots, V scores a lane: expert v * LANES + lane.
 template <typename T, int LANES, int V, bool OVER_ALL> __global__ __launch_bounds__(kRouteThreads) void route_kernel(const RouteArgs a) {
     const uint32_t lane = threadIdx.x % LANES;
     const uint64_t t = long_block() * (kRouteThreads / LANES) + threadIdx.x / LANES;
@@ -106,57 +265,74 @@ template <typename T, int LANES, int V, bool OVER_ALL> __global__ __launch_bound
     }
 }
 
-template <typename T, int LANES, int V, bool OVER_ALL> __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
+// KEPT: up to that many slots, which every lane loads, or 0: any number, each in a lane and handed round.
+template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
     const uint32_t lane = threadIdx.x % LANES;
     const uint64_t t = long_block() * (kRouteThreads / LANES) + threadIdx.x / LANES;
     const uint64_t token = t < a.tokens ? t : a.tokens - 1;
-    constexpr int kKept = TPERM_SLOTS_MAX / LANES;
-    int32_t number[kKept];
-    float weight[kKept], each[kKept], sum = 0.0f;
+    constexpr int kHere = KEPT != 0 ? KEPT : TPERM_SLOTS_MAX / LANES;
+    int32_t number[kHere];
+    float weight[kHere], each[kHere], mean = 0.0f;
 #pragma unroll
-    for (int k = 0; k < kKept; ++k) {
-        const uint32_t s = k * LANES + lane;
-        number[k] = s < a.slots ? a.expert[token * a.slots + s] : -1;
-        const bool there = (uint32_t)number[k] < a.experts;
-        weight[k] = there ? a.weights[token * a.slots + s] : 0.0f;
-        each[k] = there ? weight[k] * a.grad_weights[token * a.slots + s] : 0.0f;
-        sum += each[k];
+    for (int k = 0; k < kHere; ++k) {
+        const uint32_t s = KEPT != 0 ? k : k * LANES + lane, at = s < a.slots ? s : a.slots - 1;
+        number[k] = a.expert[token * a.slots + at], weight[k] = a.weights[token * a.slots + at], each[k] = a.grad_weights[token * a.slots + at];
     }
-    const float mean = total<LANES>(sum);
-    float grad[V];
+    T score[V];
     if constexpr (OVER_ALL) {
         const T* const row = (const T*)a.scores + (int64_t)token * a.scores_stride;
-        uint32_t key[V], best = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const uint32_t e = v * LANES + lane;
-            key[v] = key_of(e < a.experts ? (float)row[e] : -__builtin_inff());
-            best = key[v] > best ? key[v] : best;
+            score[v] = row[e < a.experts ? e : 0u];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kHere; ++k) {
+        const bool there = (uint32_t)(KEPT != 0 ? k : k * LANES + lane) < a.slots && (uint32_t)number[k] < a.experts;
+        weight[k] = there ? weight[k] : 0.0f, number[k] = there ? number[k] : -1;
+        each[k] = there ? weight[k] * each[k] : 0.0f;
+        mean += each[k];
+    }
+    if constexpr (KEPT == 0) mean = total<LANES>(mean);
+    float grad[V];
+    if constexpr (OVER_ALL) {
+        uint32_t best = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t key = key_of((uint32_t)(v * LANES) + lane < a.experts ? (float)score[v] : -__builtin_inff());
+            best = key > best ? key : best;
         }
         const float most = score_of(largest<LANES>(best));
         float all = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            grad[v] = key[v] != 0 ? part_of(score_of(key[v]), most) : 0.0f;
+            const float s = (float)score[v], part = part_of(s, most);
+            grad[v] = (uint32_t)(v * LANES) + lane < a.experts && s > -__builtin_inff() ? part : 0.0f;
             all += grad[v];
         }
         all = total<LANES>(all);
+        const float by = all > 0.0f ? -mean / all : 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) grad[v] = key[v] != 0 ? grad[v] / all * -mean : 0.0f;
+        for (int v = 0; v < V; ++v) grad[v] *= by;
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v) grad[v] = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kKept; ++k) each[k] -= weight[k] * mean;
+        for (int k = 0; k < kHere; ++k) each[k] -= weight[k] * mean;
     }
+    const auto give = [&](int32_t e, float d) {
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
-        for (uint32_t s = 0; s < LANES && k * LANES + s < a.slots; ++s) {
-            const int32_t e = __shfl(number[k], (int)s, LANES);
-            const float d = __shfl(each[k], (int)s, LANES);
+        for (int v = 0; v < V; ++v) grad[v] += e == (int32_t)(v * LANES + lane) ? d : 0.0f;
+    };
+    if constexpr (KEPT != 0) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) grad[v] += e == (int32_t)(v * LANES + lane) ? d : 0.0f;
-        }
+        for (int k = 0; k < KEPT; ++k) give(number[k], each[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kHere; ++k)
+            for (uint32_t s = 0; s < LANES && k * LANES + s < a.slots; ++s) give(__shfl(number[k], (int)s, LANES), __shfl(each[k], (int)s, LANES));
+    }
     if (t >= a.tokens) return;
     T* const out = (T*)a.grad_scores + (int64_t)token * a.grad_stride;
 #pragma unroll
@@ -171,14 +347,36 @@ template <int LANES, typename K> hipError_t go(K kernel, const RouteArgs& a, hip
     hipLaunchKernelGGL(kernel, long_grid((a.tokens + each - 1) / each), dim3(kRouteThreads), 0, stream, a);
     return hipGetLastError();
 }
-#define TPERM_BY_EXPERTS(KERNEL)                                                                                     \
-    (a.experts <= 32    ? go<16>(KERNEL<T, 16, 2, OVER_ALL>, a, stream)                                              \
-     : a.experts <= 64  ? go<16>(KERNEL<T, 16, 4, OVER_ALL>, a, stream)                                              \
-     : a.experts <= 128 ? go<16>(KERNEL<T, 16, 8, OVER_ALL>, a, stream)                                              \
-     : a.experts <= 256 ? go<64>(KERNEL<T, 64, 4, OVER_ALL>, a, stream)                                              \
-                        : go<64>(KERNEL<T, 64, 16, OVER_ALL>, a, stream))
-template <typename T, bool OVER_ALL> hipError_t route_of(const RouteArgs& a, hipStream_t stream) { return TPERM_BY_EXPERTS(route_kernel); }
-template <typename T, bool OVER_ALL> hipError_t backward_of(const RouteArgs& a, hipStream_t stream) { return TPERM_BY_EXPERTS(route_backward_kernel); }
+#define TPERM_BY_EXPERTS(KERNEL, ...)                                                                                \
+    (a.experts <= 32    ? go<16>(KERNEL<T, 16, 2, __VA_ARGS__>, a, stream)                                           \
+     : a.experts <= 64  ? go<16>(KERNEL<T, 16, 4, __VA_ARGS__>, a, stream)                                           \
+     : a.experts <= 128 ? go<16>(KERNEL<T, 16, 8, __VA_ARGS__>, a, stream)                                           \
+     : a.experts <= 256 ? go<64>(KERNEL<T, 64, 4, __VA_ARGS__>, a, stream)                                           \
+                        : go<64>(KERNEL<T, 64, 16, __VA_ARGS__>, a, stream))
+// Few lanes to a token do the fewest operations, more of them answer sooner where there are few tokens.
+template <typename T, int P, bool ALIGNED> hipError_t few_slots(const RouteArgs& a, bool over_all, hipStream_t stream) {
+    const auto with = [&](auto kernel, uint32_t lanes) {
+        const uint64_t each = kRouteThreads / lanes;
+        hipLaunchKernelGGL(kernel, long_grid((a.tokens + each - 1) / each), dim3(kRouteThreads), 0, stream, a, over_all);
+        return hipGetLastError();
+    };
+    const bool many = a.tokens >= 8192;
+    if (many && a.experts <= 32) return with(route_few_kernel<T, 4, 8, P, ALIGNED>, 4);
+    if (many && a.experts <= 64) return with(route_few_kernel<T, 4, 16, P, ALIGNED>, 4);
+    if (many && a.experts <= 128) return with(route_few_kernel<T, 4, 32, P, ALIGNED>, 4);
+    return a.experts <= 128 ? with(route_few_kernel<T, 16, 8, P, ALIGNED>, 16) : a.experts <= 256 ? with(route_few_kernel<T, 16, 16, P, ALIGNED>, 16)
+           : a.experts <= 512 ? with(route_few_kernel<T, 16, 32, P, ALIGNED>, 16) : with(route_few_kernel<T, 64, 16, P, ALIGNED>, 64);
+}
+template <typename T, bool OVER_ALL> hipError_t route_of(const RouteArgs& a, hipStream_t stream) {
+    const bool aligned = ((uintptr_t)a.scores | (uintptr_t)a.scores_stride * sizeof(T)) % 16 == 0 && a.experts * sizeof(T) % 16 == 0;
+    if (a.slots <= 4) return aligned ? few_slots<T, 4, true>(a, OVER_ALL, stream) : few_slots<T, 4, false>(a, OVER_ALL, stream);
+    if (a.slots <= 8) return aligned ? few_slots<T, 8, true>(a, OVER_ALL, stream) : few_slots<T, 8, false>(a, OVER_ALL, stream);
+    return TPERM_BY_EXPERTS(route_kernel, OVER_ALL);
+}
+template <typename T, bool OVER_ALL> hipError_t backward_of(const RouteArgs& a, hipStream_t stream) {
+    return a.slots <= 4 ? TPERM_BY_EXPERTS(route_backward_kernel, 4, OVER_ALL) : a.slots <= 8 ? TPERM_BY_EXPERTS(route_backward_kernel, 8, OVER_ALL)
+                                                                               : TPERM_BY_EXPERTS(route_backward_kernel, 0, OVER_ALL);
+}
 
 }  // namespace
 

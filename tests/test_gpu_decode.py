@@ -91,6 +91,29 @@ def test_route(t, kind, over_all):
 
 
 @pytest.mark.parametrize("over_all", [False, True])
+@pytest.mark.parametrize("tokens,experts,slots", [(8192, 32, 4), (8200, 30, 3), (9001, 64, 8), (8192, 61, 7), (10007, 128, 8), (8192, 101, 6), (8195, 200, 5)])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_route_of_many_tokens(t, tokens, experts, slots, over_all):
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    v = torch.randn(tokens, experts, generator=g, device="cuda") * 3
+    v[torch.rand(v.shape, generator=g, device="cuda") < 0.2] = -math.inf
+    v[::100] = -math.inf
+    v[1::100] = v[1::100].round()
+    scores = v.to(TYPES[t])
+    expert, weights = torch.empty(tokens, slots, dtype=torch.int32, device="cuda"), torch.empty(tokens, slots, device="cuda")
+    B.tperm_expert_route(scores.data_ptr(), experts, expert.data_ptr(), weights.data_ptr(), tokens, slots, experts, over_all, B.TYPES[t], stream())
+    v = scores.double()
+    top, at = torch.sort(v, dim=1, descending=True, stable=True)
+    top, at = top[:, :slots], at[:, :slots]
+    there = top > -math.inf
+    assert torch.equal(expert, torch.where(there, at, -1).to(torch.int32))
+    total = torch.logsumexp(v if over_all else top, 1, keepdim=True)
+    want = torch.where(there, torch.exp(top - total), 0.0)
+    far = torch.where(there, top[:, :1] - top, 0.0)
+    near(weights, want.cpu(), ((4 + far + experts) * SUM * want).cpu())
+
+
+@pytest.mark.parametrize("over_all", [False, True])
 @pytest.mark.parametrize("kind", ["plain", "barred", "wide"])
 @pytest.mark.parametrize("t", list(TYPES))
 def test_route_backward(t, kind, over_all):
