@@ -34,25 +34,25 @@ __device__ __forceinline__ f32x4 multiply(f32x4 w, f32x4 x, f32x4 sum) {
 
 // A number as the sum of bfloat16 parts, each what the one before it left: 8 bits to a part, so that two hold a
 // binary16 number and three a binary32 one (below 2^-110 what 2^-133 leaves off).  Infinities and NaN are the first part alone.
-__device__ __forceinline__ uint32_t first_part(float v, float* rest) {
-    uint32_t b = __float_as_uint(v);
-    const uint32_t size = b & 0x7FFFFFFFu;
-    b |= size > 0x7F800000u ? 0x400000u : 0u;      // a NaN stays one
-    b &= 0xFFFF0000u;
-    *rest = size < 0x7F800000u ? v - __uint_as_float(b) : 0.0f;
-    return b;
-}
 // P parts of 8 numbers.
 template <int P> __device__ __forceinline__ void parts_of(Vec<float, 8> v, bf16x8 (&part)[P]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_canonicalizef(v[i]);      // a NaN with a bit among the upper 16
+#pragma unroll
     for (int p = 0; p < P; ++p) {
         u32x4 words;
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float rest[2];
-            const uint32_t low = first_part(v[2 * i], &rest[0]), high = first_part(v[2 * i + 1], &rest[1]);
-            words[i] = low >> 16 | high;
-            v[2 * i] = rest[0], v[2 * i + 1] = rest[1];
+            const uint32_t low = __float_as_uint(v[2 * i]), high = __float_as_uint(v[2 * i + 1]);
+            words[i] = __builtin_amdgcn_perm(high, low, 0x07060302u);
         }
         part[p] = __builtin_bit_cast(bf16x8, words);
+        if (p + 1 < P)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float rest = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+                v[i] = __builtin_isfinite(v[i]) ? rest : 0.0f;
+            }
     }
 }
 
