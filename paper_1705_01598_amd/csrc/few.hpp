@@ -208,10 +208,13 @@ __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], c
     constexpr int R = S::R, M = S::M, kTurns = S::kPaired ? 2 : 1;      // paired: first the even pieces of both tiles, then the odd ones
     const auto there = [&](int t) { return REACH == Reach::kAll || i + t * W::kDepth < depth; };
     typename W::Step s[STEPS][R];
+    const auto request = [&] {
 #pragma unroll
-    for (int t = 0; t < STEPS; ++t)
+        for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[t][r] = w.template load<REACH, ALIGNED>(row[r], i + t * W::kDepth + S::piece() * W::kEach, depth);
+            for (int r = 0; r < R; ++r) s[t][r] = w.template load<REACH, ALIGNED>(row[r], i + t * W::kDepth + S::piece() * W::kEach, depth);
+        __builtin_amdgcn_sched_barrier(0);
+    };
     const auto columns_of = [&](int t, int turn, int j, int m) {
         const uint32_t at = i + t * W::kDepth + (S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece()) * W::kEach;
         return cols.template load<REACH, ALIGNED>(x[m], at, depth, j);
@@ -234,48 +237,26 @@ __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], c
 #pragma unroll
             for (int r = 0; r < R; r += 2) W::pair(s[t][r], s[t][r + 1]);
     };
-    // Columns are requested in front of the products, all of them where they fit 32 registers, else what half of a turn needs, or less.  The
-    // fence is for the compiler, which would move the requests down to the products, until a few are under way at a time.
-    constexpr int kWords = M * (int)sizeof(typename X::Raw) / 4;
-    if constexpr (STEPS * kTurns * W::kSub * kWords <= 32) {
-        typename X::Raw raw[STEPS][kTurns][W::kSub][M];
+    // Loads come back in their order, so the columns, which are near, are requested in front of the matrix, all of them where they fit 32
+    // registers, else as many as do.  The fences are for the compiler, which would move the requests down to the products, until a few are
+    // under way at a time.
+    constexpr int kWords = M * (int)sizeof(typename X::Raw) / 4, kTurnSubs = kTurns * W::kSub;
+    constexpr int kHeld = 32 / kWords, kAhead = kHeld >= STEPS * kTurnSubs ? STEPS * kTurnSubs : kHeld >= kTurnSubs ? kTurnSubs : kHeld >= W::kSub ? W::kSub : kHeld >= 2 && W::kSub % 2 == 0 ? 2 : 1;
 #pragma unroll
-        for (int t = 0; t < STEPS; ++t)
+    for (int first = 0; first < STEPS * kTurnSubs; first += kAhead) {
+        if (first != 0 && first % kTurnSubs == 0 && !there(first / kTurnSubs)) break;
+        typename X::Raw raw[kAhead][M];
 #pragma unroll
-            for (int turn = 0; turn < kTurns; ++turn)
+        for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-                for (int j = 0; j < W::kSub; ++j)
+            for (int m = 0; m < M; ++m) raw[u][m] = columns_of((first + u) / kTurnSubs, (first + u) / W::kSub % kTurns, (first + u) % W::kSub, m);
+        if (first == 0) request();
 #pragma unroll
-                    for (int m = 0; m < M; ++m) raw[t][turn][j][m] = columns_of(t, turn, j, m);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            if (!there(t)) break;
-            paired(t);
-#pragma unroll
-            for (int turn = 0; turn < kTurns; ++turn)
-#pragma unroll
-                for (int j = 0; j < W::kSub; ++j) products(t, turn, j, raw[t][turn][j]);
-        }
-    } else {
-        constexpr int kHeld = 32 / kWords, kAhead = kHeld < 2 ? 1 : kHeld < W::kSub ? 2 : W::kSub;
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int t = 0; t < STEPS; ++t) {
-            if (!there(t)) break;
-#pragma unroll
-            for (int turn = 0; turn < kTurns; ++turn)
-#pragma unroll
-                for (int j0 = 0; j0 < W::kSub; j0 += kAhead) {
-                    typename X::Raw raw[kAhead][M];
-#pragma unroll
-                    for (int j = 0; j < kAhead; ++j)
-#pragma unroll
-                        for (int m = 0; m < M; ++m) raw[j][m] = columns_of(t, turn, j0 + j, m);
-                    if (turn == 0 && j0 == 0) paired(t);
-#pragma unroll
-                    for (int j = 0; j < kAhead; ++j) products(t, turn, j0 + j, raw[j]);
-                }
+        for (int u = 0; u < kAhead; ++u) {
+            const int t = (first + u) / kTurnSubs, turn = (first + u) / W::kSub % kTurns, j = (first + u) % W::kSub;
+            if (u != 0 && (first + u) % kTurnSubs == 0 && !there(t)) break;
+            if (turn == 0 && j == 0) paired(t);
+            products(t, turn, j, raw[u]);
         }
     }
 }
