@@ -8,18 +8,29 @@ and the token's result is the weighted sum over its experts.  One forward pass i
 expert, the two products with the gated activation between them and the combination of the rows; the first product
 reads tokens through the sorted order, so rows are never gathered into a buffer.  For the backward pass the layer
 keeps the input and the gates in 8 bits (``tperm_checkpoint_store``, ``tperm_gated_forward``); the input's rows
-are multiplied out of their codes.  Everything here is argument bookkeeping around the calls of
-``include/tperm_experts.h``; tensors are dense and contiguous, on the layer's GPU, and work is enqueued on
+are multiplied out of their codes.  A program that only asks for answers calls ``answer``, which keeps nothing and takes few tokens through
+two kernels, with matrices as they are or held in 4 bits (``hold``); ``route`` chooses the experts and their weights from a
+router's scores, ``route_backward`` takes the weights' gradient back to them.  Everything here is argument bookkeeping around the calls of
+``include/tperm_experts.h`` and ``include/tperm_decode.h``; tensors are dense and contiguous, on the layer's GPU, and work is enqueued on
 that GPU's current stream, whichever GPU is the current one (a layer is used on one stream at a time).
 """
 from __future__ import annotations
 
 import contextlib
 import itertools
-from typing import Dict, Tuple
+from typing import Dict, NamedTuple, Tuple
 
 _HERE = contextlib.nullcontext()
 _NAMES = {"torch.float32": "f32", "torch.float16": "f16", "torch.bfloat16": "bf16"}
+
+
+class HeldMatrices(NamedTuple):
+    """A layer's matrices in 4 bits, as tperm_four_bit_store writes them: for w_in and w_out codes [experts, rows, 16 * groups] and
+    scales [experts, rows, groups], a group to every 32 elements of a row."""
+    w_in: "torch.Tensor"        # noqa: F821
+    in_scales: "torch.Tensor"   # noqa: F821
+    w_out: "torch.Tensor"       # noqa: F821
+    out_scales: "torch.Tensor"  # noqa: F821
 
 
 class ExpertLayer:
@@ -78,6 +89,115 @@ class ExpertLayer:
             raise ValueError("the layer computes on a GPU: no host tensors")
         return _HERE if self._torch.cuda.current_device() == self._device.index else self._torch.cuda.device(self._device)
 
+    def _device_of(self, t):
+        return t.device if self._device.index is None and t.device.type == self._device.type else self._device
+
+    def route(self, scores, over_all: bool = False):
+        """The experts of every token and their weights from scores [tokens, experts] (float32, float16 or bfloat16): those with the
+        largest scores, and the softmax over these, or with over_all their part of the softmax over all.  Scores of minus infinity
+        or NaN bar an expert; a slot that finds none holds -1 and the weight 0."""
+        torch, B = self._torch, self._B
+        if str(scores.dtype) not in _NAMES:
+            raise ValueError("scores: float32, float16 or bfloat16 only")
+        tokens, device = scores.shape[0], self._device_of(scores)
+        self._check("scores", scores, (tokens, self.experts), scores.dtype, device)
+        self._device = device
+        expert = torch.empty(tokens, self.slots, dtype=torch.int32, device=device)
+        weights = torch.empty(tokens, self.slots, dtype=torch.float32, device=device)
+        with self._gpu():
+            B.tperm_expert_route(scores.data_ptr(), self.experts, expert.data_ptr(), weights.data_ptr(), tokens, self.slots, self.experts, over_all,
+                                 B.TYPES[_NAMES[str(scores.dtype)]], torch.cuda.current_stream().cuda_stream)
+        return expert, weights
+
+    def route_backward(self, grad_weights, scores, expert, weights, over_all: bool = False):
+        """The gradient of the scores from that of the weights (float32), which backward() returns; the other arguments as route() took
+        and gave them."""
+        torch, B = self._torch, self._B
+        if str(scores.dtype) not in _NAMES:
+            raise ValueError("scores: float32, float16 or bfloat16 only")
+        tokens, device = scores.shape[0], self._device_of(scores)
+        self._check("scores", scores, (tokens, self.experts), scores.dtype, device)
+        self._check("expert", expert, (tokens, self.slots), torch.int32, device)
+        self._check("weights", weights, (tokens, self.slots), torch.float32, device)
+        self._check("grad_weights", grad_weights, (tokens, self.slots), torch.float32, device)
+        self._device = device
+        grad = torch.empty_like(scores)
+        with self._gpu():
+            B.tperm_expert_route_backward(grad_weights.data_ptr(), scores.data_ptr(), self.experts, expert.data_ptr(), weights.data_ptr(), grad.data_ptr(),
+                                          self.experts, tokens, self.slots, self.experts, over_all, B.TYPES[_NAMES[str(scores.dtype)]],
+                                          torch.cuda.current_stream().cuda_stream)
+        return grad
+
+    def hold(self, w_in, w_out) -> HeldMatrices:
+        """The matrices in 4 bits, for answer(): 17 bytes for 32 elements."""
+        torch, B = self._torch, self._B
+        e, w, h = self.experts, self.width, self.hidden
+        device = self._device_of(w_in)
+        self._check("w_in", w_in, (e, 2 * h, w), self.dtype, device)
+        self._check("w_out", w_out, (e, w, h), self.dtype, device)
+        self._device = device
+        held = []
+        with self._gpu():
+            for m in (w_in, w_out):
+                rows, width = m.shape[1:]
+                groups = B.four_bit_groups(width)
+                codes = torch.empty(e, rows, 16 * groups, dtype=torch.uint8, device=device)
+                scales = torch.empty(e, rows, groups, dtype=torch.uint8, device=device)
+                B.tperm_four_bit_store(m.data_ptr(), width, codes.data_ptr(), scales.data_ptr(), e * rows, width, self._type, torch.cuda.current_stream().cuda_stream)
+                held += [codes, scales]
+        return HeldMatrices(*held)
+
+    def answer(self, x, expert, weights, w_in, w_out=None):
+        """The layer's result as forward() gives it, with nothing kept for a backward pass and what a forward pass kept left as it is.  w_in and
+        w_out are matrices, or w_in alone is what hold() gave.  Up to FEW_TOKENS tokens take two kernels that read the experts'
+        matrices once; more take the passes of forward(), with matrices in 4 bits brought back to the layer's type first."""
+        torch, B = self._torch, self._B
+        e, k, w, h, t = self.experts, self.slots, self.width, self.hidden, self._type
+        held = w_in if isinstance(w_in, HeldMatrices) else None
+        if (held is None) == (w_out is None):
+            raise ValueError("w_in and w_out, or held matrices alone")
+        tokens = x.shape[0]
+        rows = tokens * k
+        device = self._device_of(x)
+        self._check("x", x, (tokens, w), self.dtype, device)
+        self._check("expert", expert, (tokens, k), torch.int32, device)
+        self._check("weights", weights, (tokens, k), torch.float32, device)
+        if held is not None:
+            for name, m, shape in zip(HeldMatrices._fields, held, ((e, 2 * h, 16 * B.four_bit_groups(w)), (e, 2 * h, B.four_bit_groups(w)),
+                                                                   (e, w, 16 * B.four_bit_groups(h)), (e, w, B.four_bit_groups(h)))):
+                self._check(name, m, shape, torch.uint8, device)
+        else:
+            self._check("w_in", w_in, (e, 2 * h, w), self.dtype, device)
+            self._check("w_out", w_out, (e, w, h), self.dtype, device)
+        self._device = device
+        out = torch.empty_like(x)
+        if tokens == 0:
+            return out
+        with self._gpu():
+            s = torch.cuda.current_stream().cuda_stream
+            if tokens <= B.FEW_TOKENS:
+                matrices = (w_in.data_ptr(), None, w_out.data_ptr(), None) if held is None else tuple(m.data_ptr() for m in held)
+                need = B.expert_few_workspace_bytes(tokens, k, e, w, h, t, held is not None)
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                B.tperm_expert_few(x.data_ptr(), w, expert.data_ptr(), weights.data_ptr(), *matrices, out.data_ptr(), w, workspace.data_ptr(), need,
+                                   tokens, k, e, w, h, t, s)
+                return out
+            size, need = self._size, B.expert_sort_workspace_bytes(rows, e)
+            restored = (e * 2 * h * w * size, e * w * h * size) if held is not None else (0, 0)
+            scratch, gates, hidden, back, sort, offsets, source, place, in_matrices, out_matrices = self._scratch(
+                rows * 2 * h * size, rows * h * size, rows * w * size, need, 4 * (e + 1), 4 * rows, 4 * rows, *restored)
+            if held is not None:
+                B.tperm_four_bit_load(held.w_in.data_ptr(), held.in_scales.data_ptr(), in_matrices, w, e * 2 * h, w, t, s)
+                B.tperm_four_bit_load(held.w_out.data_ptr(), held.out_scales.data_ptr(), out_matrices, h, e * w, h, t, s)
+            else:
+                in_matrices, out_matrices = w_in.data_ptr(), w_out.data_ptr()
+            B.tperm_expert_sort(expert.data_ptr(), tokens, k, e, offsets, source, place, sort, need, s)
+            B.tperm_expert_product(x.data_ptr(), w, tokens, source, k, offsets, in_matrices, True, gates, 2 * h, rows, e, w, 2 * h, t, s)
+            B.tperm_gated_forward(gates, 2 * h, hidden, h, None, None, rows, h, t, s)
+            B.tperm_expert_product(hidden, h, rows, None, 1, offsets, out_matrices, True, back, w, rows, e, h, w, t, s)
+            B.tperm_expert_combine(back, w, place, offsets, weights.data_ptr(), out.data_ptr(), w, tokens, k, e, w, t, s)
+        return out
+
     def forward(self, x, expert, weights, w_in, w_out):
         """The layer's result for x [tokens, width]; expert [tokens, slots] int32 (a number outside 0 .. experts-1 names
         none), weights [tokens, slots] float32, w_in [experts, 2 * hidden, width], w_out [experts, width, hidden]."""
@@ -85,7 +205,7 @@ class ExpertLayer:
         e, k, w, h, t = self.experts, self.slots, self.width, self.hidden, self._type
         tokens = x.shape[0]
         rows = tokens * k
-        device = x.device if self._device.index is None and x.device.type == self._device.type else self._device
+        device = self._device_of(x)
         self._check("x", x, (tokens, w), self.dtype, device)
         self._check("expert", expert, (tokens, k), torch.int32, device)
         self._check("weights", weights, (tokens, k), torch.float32, device)
@@ -168,7 +288,7 @@ class ExpertLayer:
 
 
 def _bench(argv=None):
-    """Times a layer's forward and backward pass (synthetic tokens, random routing)."""
+    """Times a layer's forward and backward pass, or with --answer its answers (synthetic tokens, random routing)."""
     import argparse
     import json
 
@@ -181,17 +301,21 @@ def _bench(argv=None):
     ap.add_argument("--hidden", type=int, default=1024)
     ap.add_argument("--dtype", choices=["f32", "f16", "bf16"], default="bf16")
     ap.add_argument("--reps", type=int, default=10)
+    ap.add_argument("--answer", action="store_true", help="router and answer, nothing kept")
+    ap.add_argument("--bits", type=int, choices=[4, 16, 32], help="with --answer: 4 holds the matrices in 4 bits")
     a = ap.parse_args(argv)
     dtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[a.dtype]
     g = torch.Generator(device="cuda").manual_seed(1705)
     randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
     layer = ExpertLayer(a.experts, a.slots, a.width, a.hidden, dtype)
+    if a.bits not in (None, 4, 8 * dtype.itemsize) or (a.bits == 4 and not a.answer):
+        ap.error("--bits: 4 with --answer, or those of the type")
     x, grad = randn(a.tokens, a.width).to(dtype), randn(a.tokens, a.width).to(dtype)
     w_in = (randn(a.experts, 2 * a.hidden, a.width) / a.width ** 0.5).to(dtype)
     w_out = (randn(a.experts, a.width, a.hidden) / a.hidden ** 0.5).to(dtype)
     grad_w_in, grad_w_out = torch.zeros(w_in.shape, device="cuda"), torch.zeros(w_out.shape, device="cuda")
-    top, expert = randn(a.tokens, a.experts).topk(a.slots, dim=1)
-    expert, weights = expert.to(torch.int32), torch.softmax(top, dim=1)
+    scores = randn(a.tokens, a.experts)
+    expert, weights = layer.route(scores)
 
     def timed(f):
         f()
@@ -207,6 +331,15 @@ def _bench(argv=None):
         layer.forward(x, expert, weights, w_in, w_out)
         layer.backward(grad, grad_w_in, grad_w_out)
 
+    if a.answer:
+        matrices = layer.hold(w_in, w_out) if a.bits == 4 else (w_in, w_out)
+        named = int(expert.unique().numel())
+        size = 3 * a.hidden * a.width * (17 / 32 if a.bits == 4 else dtype.itemsize)
+        each = timed(lambda: layer.answer(x, *layer.route(scores), *([matrices] if a.bits == 4 else matrices)))
+        print(json.dumps({"metric": "mixture-of-experts layer, router and answer", "tokens": a.tokens, "experts": a.experts, "slots": a.slots, "width": a.width,
+                          "hidden": a.hidden, "dtype": a.dtype, "bits": a.bits or 8 * dtype.itemsize, "answer_ms": round(each, 4), "experts_named": named,
+                          "matrices_tb_per_s": round(named * size / each / 1e9, 3)}), flush=True)
+        return
     forward = timed(lambda: layer.forward(x, expert, weights, w_in, w_out))
     total = timed(both)
     flops = 2 * a.tokens * a.slots * 3 * a.hidden * a.width
