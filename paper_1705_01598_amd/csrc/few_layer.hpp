@@ -25,7 +25,6 @@ constexpr int kShareTiles = kFewShareTiles;
 constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit
 constexpr size_t kInLds = 80 * 1024, kOutLds = 112 * 1024;
 constexpr uint32_t kColumns = 32;       // tokens of an entry at most
-constexpr uint32_t kImages = 2;         // 16 x 16 products of an item of the first kernel at most
 
 // What the second product's columns are: how a hidden row is held between the kernels.
 template <typename T, bool FOUR> struct Hidden {
@@ -188,7 +187,8 @@ template <uint32_t THREADS, bool WEIGHTS> __device__ __forceinline__ Named find_
     return n;
 }
 
-// An item of the first kernel: an entry and 8 hidden channels, of which wavefront `wave` of `waves` adds up its piece.
+// An item of the first kernel: an entry and R / 2 times 8 hidden channels, of which wavefront `wave` of `waves` adds up its piece.  Tiles 2 b and 2 b + 1 are
+// the g and u rows of its b-th 8 channels.
 struct Item {
     uint32_t expert, named, first, channel, wave, waves;
 };
@@ -196,8 +196,11 @@ template <typename T, bool FOUR, bool STAGED, typename S, int STEPS, bool ALIGNE
 __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, const Item& item, f32x4* sums, const typename Tokens<T, FOUR, true>::E* staged) {
     typedef Matrix<T, FOUR> W;
     const W w = matrix_of<W>(a.w_in, a.in_scales, item.expert, 2 * a.hidden, a.width);
-    const uint32_t g = item.channel + S::row() < a.hidden ? item.channel + S::row() : a.hidden - 1;
-    const uint32_t row[2] = {g, g + a.hidden};
+    uint32_t row[S::R];
+    for (int b = 0; b < S::R / 2; ++b) {
+        const uint32_t g = item.channel + b * kChannels + S::row();
+        row[2 * b] = g < a.hidden ? g : a.hidden - 1, row[2 * b + 1] = row[2 * b] + a.hidden;
+    }
     const typename Tokens<T, FOUR, STAGED>::E* x[S::M];
     typename Tokens<T, FOUR, STAGED>::Columns cols = {};
     for (int m = 0; m < S::M; ++m) {
@@ -208,19 +211,19 @@ __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, co
     if constexpr (STAGED) cols.apart = a.tokens * staged_pitch<T, FOUR>(a.width);
     f32x4 sum[S::kSums][S::M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, item.wave, item.waves, sum);
-    static_assert(S::kSums * S::M <= (int)kImages, "a wavefront's place");
+    static_assert(S::kSums * S::M <= S::R, "a wavefront's place");
     for (int r = 0; r < S::kSums; ++r)
-        for (int m = 0; m < S::M; ++m) sums[(item.wave * kImages + r * S::M + m) * 64 + threadIdx.x % 64] = sum[r][m];
+        for (int m = 0; m < S::M; ++m) sums[(item.wave * S::R + r * S::M + m) * 64 + threadIdx.x % 64] = sum[r][m];
 }
 // The sums of all wavefronts of an item, the activation, and the hidden rows in parts: four channels of one column to a lane.
 template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, uint32_t pitch, const Named& n, const Item& item, const f32x4* sums) {
     typedef Hidden<T, FOUR> H;
-    for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < S::M * 2 * S::kColumns; i += item.waves * 64) {
-        const uint32_t m = i / (2 * S::kColumns), half = i / S::kColumns % 2, c = i % S::kColumns, column = m * S::kColumns + c;
-        if (column >= item.named) continue;
+    for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < S::M * S::R * S::kColumns; i += item.waves * 64) {
+        const uint32_t half = i % 2, b = i / 2 % (S::R / 2), column = i / S::R, m = column / S::kColumns, c = column % S::kColumns, channel = item.channel + b * kChannels + half * 4;
+        if (column >= item.named || channel >= pitch) continue;
         f32x4 gu[2] = {};
         for (uint32_t v = 0; v < item.waves; ++v)
-            for (int r = 0; r < 2; ++r) gu[r] += sums_at<S>(sums + v * kImages * 64, r, m, half, c);
+            for (int r = 0; r < 2; ++r) gu[r] += sums_at<S>(sums + v * S::R * 64, 2 * b + r, m, half, c);
         const float weight = n.weight[item.first + column];
         f32x4 h;
         for (int k = 0; k < 4; ++k) {
@@ -228,7 +231,7 @@ template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hid
             h[k] = gu[0][k] * s.p * gu[1][k] * s.last * weight;
         }
         const int64_t rows = (int64_t)a.tokens * a.slots;
-        typename H::E* const out = (typename H::E*)a.rows + (int64_t)(item.first + column) * pitch + item.channel + half * 4;
+        typename H::E* const out = (typename H::E*)a.rows + (int64_t)(item.first + column) * pitch + channel;
         for (int p = 0; p < H::kParts; ++p) {
             const Vec<typename H::E, 4> part = narrow<typename H::E, 4>(h);
             store_vec<typename H::E, 4, true>(out + p * rows * pitch, part);
@@ -238,45 +241,52 @@ template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hid
     }
 }
 
-template <typename T, bool FOUR, bool STAGED, bool ALIGNED, bool X_ALIGNED>
-__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch, const uint32_t shares) {
-    extern __shared__ f32x4 dynamic[];
+// All items of a workgroup, with R tiles.
+template <typename T, bool FOUR, bool STAGED, bool ALIGNED, int R>
+__device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, const Named& n, f32x4* places, const typename Tokens<T, FOUR, true>::E* staged) {
     typedef Matrix<T, FOUR> W;
-    typedef Shape<2, 1, false> Few;
-    typedef Shape<2, 1, true> Some;
-    typedef Shape<2, 2, true> Many;
-    constexpr uint32_t kPlace = kFewWaves * kImages * 64;      // of all wavefronts' sums; two of them, used in turn
-    typedef typename Tokens<T, FOUR, true>::E E;
-    E* const staged = (E*)(dynamic + 2 * kPlace);
-    if constexpr (STAGED) stage<T, FOUR, X_ALIGNED>(a, staged);
-    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T, FOUR>(a.tokens, a.width) : 0), most);
-    if (blockIdx.x == 0 && shares != 1)     // counters of the second kernel
-        for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
-    const uint32_t channels = (a.hidden + kChannels - 1) / kChannels, items = n.total * channels, steps = (a.width + W::kDepth - 1) / W::kDepth;
-    // Eight loads in flight a wavefront where there are more than four for each, else one step to each; a workgroup's wavefronts
-    // share as many items as that leaves them.
-    constexpr int kSteps = FOUR ? 2 : 4;
-    const bool long_steps = items * steps * 2 > 4 * 2 * kInGroups * kFewWaves;
+    typedef Shape<R, 1, false> Few;
+    typedef Shape<R, 1, true> Some;
+    typedef Shape<R, 2, true> Many;
+    constexpr uint32_t kPlace = kFewWaves * R * 64;            // of all wavefronts' sums; two of them, used in turn
+    constexpr uint32_t kItem = R / 2 * kChannels;
+    // Eight loads in flight a wavefront (four where two conversions follow each) where there are more than four for each, else one step to each;
+    // a workgroup's wavefronts share as many items as that leaves them.
+    constexpr int kSteps = (FOUR ? 4 : 8) / R;
+    const uint32_t channels = (a.hidden + kItem - 1) / kItem, items = n.total * channels, steps = (a.width + W::kDepth - 1) / W::kDepth;
+    const bool long_steps = items * steps * R > 4 * kInGroups * kFewWaves;
     const uint32_t pieces = long_steps ? (steps + kSteps - 1) / kSteps : steps, waves = pieces > 4 ? 8 : pieces > 2 ? 4 : pieces, at_once = kFewWaves / waves;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave / waves;
-    f32x4* place = dynamic + group * waves * kImages * 64;
+    f32x4* place = places + group * waves * R * 64;
     for (uint32_t base = blockIdx.x * at_once; base < items; base += gridDim.x * at_once) {
         Item item = {};
         if (base + group < items) {
             const uint32_t rank = (base + group) / channels, entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]);
-            item = {entry & 0xFFFFu, entry >> 16, (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]), (base + group - rank * channels) * kChannels, wave % waves, waves};
+            item = {entry & 0xFFFFu, entry >> 16, (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]), (base + group - rank * channels) * kItem, wave % waves, waves};
             if (item.named <= 8 && long_steps) hidden_sums<T, FOUR, STAGED, Few, kSteps, ALIGNED>(a, n, item, place, staged);
             else if (item.named <= 8) hidden_sums<T, FOUR, STAGED, Few, 1, ALIGNED>(a, n, item, place, staged);
-            else if (item.named <= 16) hidden_sums<T, FOUR, STAGED, Some, FOUR ? 1 : 4, ALIGNED>(a, n, item, place, staged);
-            else hidden_sums<T, FOUR, STAGED, Many, FOUR ? 1 : 2, ALIGNED>(a, n, item, place, staged);
+            else if (item.named <= 16) hidden_sums<T, FOUR, STAGED, Some, FOUR ? 1 : kSteps, ALIGNED>(a, n, item, place, staged);
+            else hidden_sums<T, FOUR, STAGED, Many, FOUR ? 1 : kSteps / 2, ALIGNED>(a, n, item, place, staged);
         }
         __syncthreads();
         if (item.named == 0) {
         } else if (item.named <= 8) hidden_rows<T, FOUR, Few>(a, pitch, n, item, place);
         else if (item.named <= 16) hidden_rows<T, FOUR, Some>(a, pitch, n, item, place);
         else hidden_rows<T, FOUR, Many>(a, pitch, n, item, place);
-        place = place < dynamic + kPlace ? place + kPlace : place - kPlace;
+        place = place < places + kPlace ? place + kPlace : place - kPlace;
     }
+}
+
+template <typename T, bool FOUR, bool STAGED, bool ALIGNED, bool X_ALIGNED, int R>
+__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch, const uint32_t shares) {
+    extern __shared__ f32x4 dynamic[];
+    typedef typename Tokens<T, FOUR, true>::E E;
+    E* const staged = (E*)(dynamic + 2 * kFewWaves * R * 64);
+    if constexpr (STAGED) stage<T, FOUR, X_ALIGNED>(a, staged);
+    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T, FOUR>(a.tokens, a.width) : 0), most);
+    if (blockIdx.x == 0 && shares != 1)     // counters of the second kernel
+        for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
+    hidden_items<T, FOUR, STAGED, ALIGNED, R>(a, pitch, n, dynamic, staged);
 }
 
 // What lane l + 40 holds, for the lanes l of the first half whose l % 16 is below 8.
@@ -378,6 +388,7 @@ __global__ __launch_bounds__(64 * kOutWaves<R>, 4) void few_out_kernel(const Few
 }
 
 template <bool B> using Bool = std::integral_constant<bool, B>;
+template <int N> using Int = std::integral_constant<int, N>;
 
 template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream_t stream) {
     const FewRoom room = few_room(a.tokens, a.slots, a.experts, a.width, a.hidden, type, FOUR);
@@ -387,12 +398,14 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
     const bool x_aligned = on_eights(a.x, a.x_stride, a.width);
     const bool in_aligned = FOUR || on_eights(a.w_in, a.width, a.width), out_aligned = FOUR ? a.hidden % 8 == 0 : on_eights(a.w_out, a.hidden, a.hidden);
     a.by_slots = make_fastdiv(a.slots);
-    const uint64_t items = (uint64_t)room.most * ((a.hidden + kChannels - 1) / kChannels);
-    const size_t in_lds = (size_t)2 * kFewWaves * kImages * 64 * 16 + named_bytes(count, a.experts, room.most, true), staged = staged_bytes<T, FOUR>(a.tokens, a.width);
-    const auto launch_in = [&](auto in_lds_too, auto aligned, auto x_is) {
-        constexpr bool kStaged = decltype(in_lds_too)::value;
-        constexpr auto kKernel = few_in_kernel<T, FOUR, kStaged, decltype(aligned)::value, decltype(x_is)::value>;
-        const size_t lds = in_lds + (kStaged ? staged : 0);
+    const size_t named = named_bytes(count, a.experts, room.most, true), staged = staged_bytes<T, FOUR>(a.tokens, a.width);
+    const auto sums_bytes = [](int tiles) { return (size_t)2 * kFewWaves * tiles * 64 * 16; };
+    const auto launch_in = [&](auto from_lds, auto aligned, auto x_is, auto tiles) {
+        constexpr bool kStaged = decltype(from_lds)::value;
+        constexpr int kTiles = decltype(tiles)::value;
+        constexpr auto kKernel = few_in_kernel<T, FOUR, kStaged, decltype(aligned)::value, decltype(x_is)::value, kTiles>;
+        const uint64_t items = (uint64_t)room.most * ((a.hidden + kTiles / 2 * kChannels - 1) / (kTiles / 2 * kChannels));
+        const size_t lds = sums_bytes(kTiles) + named + (kStaged ? staged : 0);
         const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kInLds) : hipSuccess;
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL(kKernel, dim3((uint32_t)(items < kInGroups ? items : kInGroups)), dim3(kFewThreads), lds, stream, a, room.most, room.pitch, room.shares);
@@ -409,20 +422,23 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
         return hipGetLastError();
     };
     hipError_t e = hipSuccess;
-    if (FOUR && items >= 4 * kInGroups && in_lds + staged <= kInLds) {
-        if constexpr (FOUR) e = x_aligned ? launch_in(Bool<true>(), Bool<true>(), Bool<true>()) : launch_in(Bool<true>(), Bool<true>(), Bool<false>());
+    const bool many_items = (uint64_t)room.most * over(a.hidden, kChannels) >= 4 * kInGroups;
+    if (FOUR && many_items && sums_bytes(2) + named + staged <= kInLds) {
+        if constexpr (FOUR) e = x_aligned ? launch_in(Bool<true>(), Bool<true>(), Bool<true>(), Int<2>()) : launch_in(Bool<true>(), Bool<true>(), Bool<false>(), Int<2>());
     } else {
-        e = in_aligned && x_aligned ? launch_in(Bool<false>(), Bool<true>(), Bool<true>()) : launch_in(Bool<false>(), Bool<false>(), Bool<false>());
+        const bool four_tiles = many_items && count >= (FOUR ? 2 : 3) * room.most && sums_bytes(4) + named <= kInLds, aligned = in_aligned && x_aligned;
+        e = four_tiles ? (aligned ? launch_in(Bool<false>(), Bool<true>(), Bool<true>(), Int<4>()) : launch_in(Bool<false>(), Bool<false>(), Bool<false>(), Int<4>()))
+                       : (aligned ? launch_in(Bool<false>(), Bool<true>(), Bool<true>(), Int<2>()) : launch_in(Bool<false>(), Bool<false>(), Bool<false>(), Int<2>()));
     }
     if (e != hipSuccess) return e;
     const auto launch_shared = [&](auto aligned) {
-        return room.shares == 1 ? launch_out(aligned, std::integral_constant<int, 1>()) : launch_out(aligned, std::integral_constant<int, kShareTiles>());
+        return room.shares == 1 ? launch_out(aligned, Int<1>()) : launch_out(aligned, Int<kShareTiles>());
     };
     return out_aligned ? launch_shared(Bool<true>()) : launch_shared(Bool<false>());
 }
 
 static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX, few_most(TPERM_FEW_TOKENS, TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX), true) <=
-                  kInLds - 2 * kFewWaves * kImages * 64 * 16, "LDS of two workgroups");
+                  kInLds - 2 * kFewWaves * 2 * 64 * 16, "LDS of two workgroups");
 static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX, few_most(TPERM_FEW_TOKENS, TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX), false) <=
                   kOutLds - 8 * TPERM_FEW_TOKENS * kShareTiles * kChannels * 4, "LDS of a workgroup of the second kernel");
 

@@ -3,6 +3,7 @@
 
 #include "decode.hpp"
 #include "few.hpp"
+#include "launch.hpp"
 
 namespace tperm {
 
@@ -41,7 +42,12 @@ template <typename T, bool ALIGNED, int STEPS, typename S> __global__ __launch_b
 }
 
 template <typename T, bool ALIGNED, int STEPS, typename S> hipError_t go(const FourBitProductArgs& a, hipStream_t stream) {
-    static_assert(S::kSums * S::M <= 8, "LDS that needs no leave");
+    constexpr auto kKernel = four_bit_product_kernel<T, ALIGNED, STEPS, S>;
+    constexpr size_t kLds = (size_t)kFewWaves * S::kSums * S::M * 64 * 16;
+    if constexpr (kLds > 64 * 1024) {
+        const hipError_t e = allow_lds<kKernel>(kLds);
+        if (e != hipSuccess) return e;
+    }
     const uint32_t chunks = (a.rows + 63) / 64;
     // a launch has at most 65535 workgroups along the second dimension of its grid here
     FourBitProductArgs part = a;
@@ -49,8 +55,7 @@ template <typename T, bool ALIGNED, int STEPS, typename S> hipError_t go(const F
         const uint32_t now = chunks - done < 65535 ? chunks - done : 65535;
         part.x = (const T*)a.x + (int64_t)done * 64 * a.x_stride, part.out = (T*)a.out + (int64_t)done * 64 * a.out_stride;
         part.rows = a.rows - done * 64 < now * 64 ? a.rows - done * 64 : now * 64;
-        hipLaunchKernelGGL((four_bit_product_kernel<T, ALIGNED, STEPS, S>), dim3((a.n + S::R * 8 - 1) / (S::R * 8), now), dim3(kFewThreads),
-                           (size_t)kFewWaves * S::kSums * S::M * 64 * 16, stream, part);
+        hipLaunchKernelGGL(kKernel, dim3((a.n + S::R * 8 - 1) / (S::R * 8), now), dim3(kFewThreads), kLds, stream, part);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -65,10 +70,16 @@ template <typename T, bool ALIGNED> hipError_t product_of(const FourBitProductAr
                            : tiles < 4096 ? go<T, ALIGNED, 1, Shape<8, 1, true>>(a, stream) : go<T, ALIGNED, 1, Shape<16, 1, true>>(a, stream);
     if (a.rows <= 32) {
         if constexpr (sizeof(T) == 2)
-            if (tiles >= 2048) return go<T, ALIGNED, 1, Shape<8, 2, true>>(a, stream);
+            if (tiles >= 1024) return go<T, ALIGNED, 1, Shape<8, 2, true>>(a, stream);
         return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 2, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 2, true>>(a, stream);
     }
-    if (a.rows <= 48) return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 3, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 3, true>>(a, stream);
+    if (a.rows <= 48) {
+        if constexpr (sizeof(T) == 2)
+            if (tiles >= 1024) return go<T, ALIGNED, 1, Shape<8, 3, true>>(a, stream);
+        return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 3, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 3, true>>(a, stream);
+    }
+    if constexpr (sizeof(T) == 2)
+        if (tiles >= 1024) return go<T, ALIGNED, 1, Shape<8, 4, true>>(a, stream);
     return tiles < 1024 ? go<T, ALIGNED, 1, Shape<2, 4, true>>(a, stream) : go<T, ALIGNED, 1, Shape<4, 4, true>>(a, stream);
 }
 

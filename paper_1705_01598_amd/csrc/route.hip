@@ -26,12 +26,12 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 __device__ __forceinline__ float score_of(uint32_t key) { return __uint_as_float((int32_t)key < 0 ? key & 0x7FFFFFFFu : ~key); }
 
 template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true); }
-// f over the lanes of a group, in all of them: rotations of a row of 16, then across the rows.
+// f over the lanes of a group, in all of them: lanes 1 and 2 apart, mirrored in 8 and in 16, then across the rows.
 template <int LANES, typename F> __device__ __forceinline__ uint32_t over_group(uint32_t v, F f) {
-    v = f(v, moved<0x121>(v));
-    v = f(v, moved<0x122>(v));
-    v = f(v, moved<0x124>(v));
-    v = f(v, moved<0x128>(v));
+    v = f(v, moved<0xB1>(v));
+    v = f(v, moved<0x4E>(v));
+    if constexpr (LANES > 4) v = f(v, moved<0x141>(v));
+    if constexpr (LANES > 8) v = f(v, moved<0x140>(v));
     if constexpr (LANES == 64) {
         v = f(v, (uint32_t)__shfl_xor((int)v, 16));
         v = f(v, (uint32_t)__shfl_xor((int)v, 32));
@@ -63,23 +63,27 @@ __device__ __forceinline__ float part_of(float v, float most) {
     return v == most ? 1.0f : e;
 }
 
-// Numbers that order as the scores of T do, equal ones by expert, none equal to another; without its expert 0 if barred.
+// The same for a sum over all scores, where what the product rounds off, 2^-24 |x| exp(-|x|) at most, is less than what the sum does.
+__device__ __forceinline__ float rough_part_of(float v, float most) {
+    const float e = __builtin_amdgcn_exp2f((v - most) * 0x1.715476p+0f);
+    return v == most ? 1.0f : e;
+}
+
+// Numbers that order as the scores of T do, equal ones by expert, none equal to another; minus infinity is barred.  The bits of a score of 16
+// as binary32, all but the sign of negative ones complemented: 13 low bits are free for the expert.
 template <typename T> struct Ordered {
-    typedef uint32_t Key;
+    typedef int32_t Key;
+    static constexpr uint32_t kFree = 0x1FFFu;
     static __device__ __forceinline__ Key key(T v, uint32_t expert) {
-        constexpr uint32_t kInfinity = std::is_same_v<T, _Float16> ? 0x7C00u : 0x7F80u;
-        uint32_t b = __builtin_bit_cast(uint16_t, v);
-        const uint32_t size = b & 0x7FFFu;
-        b = size == 0 ? 0u : b;                     // one zero
-        const bool barred = size > kInfinity || b == (0x8000u | kInfinity);
-        return (barred ? 0u : (b & 0x8000u) ? b ^ 0xFFFFu : b | 0x8000u) << 16 | (TPERM_EXPERTS_MAX - 1 - expert);
+        const uint32_t b = __float_as_uint(__builtin_fmaxf((float)v + 0.0f, -__builtin_inff()));      // one zero; NaN as minus infinity
+        return (Key)((b ^ ((uint32_t)((int32_t)b >> 31) & (0x7FFFFFFFu & ~kFree))) | (TPERM_EXPERTS_MAX - 1 - expert));
     }
-    static __device__ __forceinline__ uint32_t expert(Key k) { return TPERM_EXPERTS_MAX - 1 - (k & 0xFFFFu); }
-    static __device__ __forceinline__ bool barred(Key k) { return k >> 16 == 0; }
+    static __device__ __forceinline__ uint32_t expert(Key k) { return TPERM_EXPERTS_MAX - 1 - ((uint32_t)k & kFree); }
     static __device__ __forceinline__ float score(Key k) {
-        const uint32_t b = k >> 16;
-        return (float)__builtin_bit_cast(T, (uint16_t)(b & 0x8000u ? b & 0x7FFFu : b ^ 0xFFFFu));
+        const uint32_t b = (uint32_t)k & ~kFree;
+        return __uint_as_float(b ^ ((uint32_t)(k >> 31) & (0x7FFFFFFFu & ~kFree)));
     }
+    static __device__ __forceinline__ bool barred(Key k) { return score(k) == -__builtin_inff(); }
     static __device__ __forceinline__ Key high(Key a, Key b) { return a > b ? a : b; }
     static __device__ __forceinline__ Key low(Key a, Key b) { return a < b ? a : b; }
 };
@@ -100,12 +104,12 @@ template <> struct Ordered<float> {
     static __device__ __forceinline__ Key high(Key a, Key b) { return __builtin_fmax(a, b); }
     static __device__ __forceinline__ Key low(Key a, Key b) { return __builtin_fmin(a, b); }
 };
-template <int CTRL> __device__ __forceinline__ uint32_t from_lane(uint32_t v) { return moved<CTRL>(v); }
+template <int CTRL> __device__ __forceinline__ int32_t from_lane(int32_t v) { return (int32_t)moved<CTRL>((uint32_t)v); }
 template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
     return __builtin_bit_cast(double, (uint64_t)moved<CTRL>((uint32_t)(b >> 32)) << 32 | moved<CTRL>((uint32_t)b));
 }
-__device__ __forceinline__ uint32_t across(uint32_t v, int lanes) { return (uint32_t)__shfl_xor((int)v, lanes); }
+__device__ __forceinline__ int32_t across(int32_t v, int lanes) { return __shfl_xor(v, lanes); }
 __device__ __forceinline__ double across(double v, int lanes) { return __shfl_xor(v, lanes); }
 
 template <typename O, int I, int J, int P> __device__ __forceinline__ void exchange(typename O::Key (&k)[P]) {
@@ -188,7 +192,8 @@ template <typename T, int LANES, int V, int P, bool ALIGNED> __global__ __launch
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float s = (float)score[v];
-            sum += expert_of(v) < a.experts && s > -__builtin_inff() ? part_of(s, most) : 0.0f;
+            const float part = rough_part_of(s, most);
+            sum += expert_of(v) < a.experts && s > -__builtin_inff() ? part : 0.0f;
         }
     }
     sum = total<LANES>(sum);
@@ -228,7 +233,7 @@ template <typename T, int LANES, int V, bool OVER_ALL> __global__ __launch_bound
     float all = 0.0f;
     if constexpr (OVER_ALL) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) all += key[v] != 0 ? part_of(score_of(key[v]), most) : 0.0f;
+        for (int v = 0; v < V; ++v) all += key[v] != 0 ? rough_part_of(score_of(key[v]), most) : 0.0f;
         all = total<LANES>(all);
     }
     constexpr int kKept = TPERM_SLOTS_MAX / LANES;
@@ -266,10 +271,14 @@ template <typename T, int LANES, int V, bool OVER_ALL> __global__ __launch_bound
 }
 
 // KEPT: up to that many slots, which every lane loads, or 0: any number, each in a lane and handed round.
-template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
+// ALIGNED: rows of whole 16 bytes, which a lane takes in turn with its neighbours.
+template <typename T, int LANES, int V, int KEPT, bool OVER_ALL, bool ALIGNED> __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
+    constexpr int C = ALIGNED ? 16 / (int)sizeof(T) : 1;
+    static_assert(V % C == 0, "whole loads");
     const uint32_t lane = threadIdx.x % LANES;
     const uint64_t t = long_block() * (kRouteThreads / LANES) + threadIdx.x / LANES;
     const uint64_t token = t < a.tokens ? t : a.tokens - 1;
+    const auto expert_of = [&](int v) { return (uint32_t)(v / C * LANES * C + lane * C + v % C); };
     constexpr int kHere = KEPT != 0 ? KEPT : TPERM_SLOTS_MAX / LANES;
     int32_t number[kHere];
     float weight[kHere], each[kHere], mean = 0.0f;
@@ -282,9 +291,10 @@ template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __la
     if constexpr (OVER_ALL) {
         const T* const row = (const T*)a.scores + (int64_t)token * a.scores_stride;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t e = v * LANES + lane;
-            score[v] = row[e < a.experts ? e : 0u];
+        for (int v = 0; v < V; v += C) {
+            const uint32_t e = expert_of(v);
+            const Vec<T, C> part = load_vec<T, C, ALIGNED>(row + (e < a.experts ? e : 0u));
+            for (int c = 0; c < C; ++c) score[v + c] = part[c];
         }
     }
 #pragma unroll
@@ -300,7 +310,7 @@ template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __la
         uint32_t best = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t key = key_of((uint32_t)(v * LANES) + lane < a.experts ? (float)score[v] : -__builtin_inff());
+            const uint32_t key = key_of(expert_of(v) < a.experts ? (float)score[v] : -__builtin_inff());
             best = key > best ? key : best;
         }
         const float most = score_of(largest<LANES>(best));
@@ -308,7 +318,7 @@ template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __la
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float s = (float)score[v], part = part_of(s, most);
-            grad[v] = (uint32_t)(v * LANES) + lane < a.experts && s > -__builtin_inff() ? part : 0.0f;
+            grad[v] = expert_of(v) < a.experts && s > -__builtin_inff() ? part : 0.0f;
             all += grad[v];
         }
         all = total<LANES>(all);
@@ -323,7 +333,7 @@ template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __la
     }
     const auto give = [&](int32_t e, float d) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) grad[v] += e == (int32_t)(v * LANES + lane) ? d : 0.0f;
+        for (int v = 0; v < V; ++v) grad[v] += e == (int32_t)expert_of(v) ? d : 0.0f;
     };
     if constexpr (KEPT != 0) {
 #pragma unroll
@@ -336,9 +346,10 @@ template <typename T, int LANES, int V, int KEPT, bool OVER_ALL> __global__ __la
     if (t >= a.tokens) return;
     T* const out = (T*)a.grad_scores + (int64_t)token * a.grad_stride;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const uint32_t e = v * LANES + lane;
-        if (e < a.experts) out[e] = (T)grad[v];
+    for (int v = 0; v < V; v += C) {
+        Vec<T, C> part;
+        for (int c = 0; c < C; ++c) part[c] = (T)grad[v + c];
+        if (expert_of(v) < a.experts) store_vec<T, C, ALIGNED>(out + expert_of(v), part);
     }
 }
 
@@ -373,9 +384,22 @@ template <typename T, bool OVER_ALL> hipError_t route_of(const RouteArgs& a, hip
     if (a.slots <= 8) return aligned ? few_slots<T, 8, true>(a, OVER_ALL, stream) : few_slots<T, 8, false>(a, OVER_ALL, stream);
     return TPERM_BY_EXPERTS(route_kernel, OVER_ALL);
 }
+#define TPERM_BACKWARD(LANES, V) go<LANES>(route_backward_kernel<T, LANES, V, KEPT, OVER_ALL, ALIGNED>, a, stream)
+template <typename T, bool OVER_ALL, int KEPT, bool ALIGNED> hipError_t backward_by_experts(const RouteArgs& a, hipStream_t stream) {
+    if constexpr (KEPT != 0) {
+        if (a.experts <= 32) return TPERM_BACKWARD(4, 8);
+        if (a.experts <= 64) return TPERM_BACKWARD(8, 8);
+    }
+    return a.experts <= 128 ? TPERM_BACKWARD(16, 8) : a.experts <= 512 ? TPERM_BACKWARD(64, 8) : TPERM_BACKWARD(64, 16);
+}
+template <typename T, bool OVER_ALL, bool ALIGNED> hipError_t backward_of(const RouteArgs& a, hipStream_t stream) {
+    return a.slots <= 4 ? backward_by_experts<T, OVER_ALL, 4, ALIGNED>(a, stream) : a.slots <= 8 ? backward_by_experts<T, OVER_ALL, 8, ALIGNED>(a, stream)
+                                                                                                 : backward_by_experts<T, OVER_ALL, 0, ALIGNED>(a, stream);
+}
 template <typename T, bool OVER_ALL> hipError_t backward_of(const RouteArgs& a, hipStream_t stream) {
-    return a.slots <= 4 ? TPERM_BY_EXPERTS(route_backward_kernel, 4, OVER_ALL) : a.slots <= 8 ? TPERM_BY_EXPERTS(route_backward_kernel, 8, OVER_ALL)
-                                                                               : TPERM_BY_EXPERTS(route_backward_kernel, 0, OVER_ALL);
+    const auto on_16 = [](const void* p, int64_t stride) { return ((uintptr_t)p | (uintptr_t)stride * sizeof(T)) % 16 == 0; };
+    const bool aligned = a.experts * sizeof(T) % 16 == 0 && on_16(a.grad_scores, a.grad_stride) && (!OVER_ALL || on_16(a.scores, a.scores_stride));
+    return aligned ? backward_of<T, OVER_ALL, true>(a, stream) : backward_of<T, OVER_ALL, false>(a, stream);
 }
 
 }  // namespace
