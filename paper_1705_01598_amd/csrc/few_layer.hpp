@@ -254,7 +254,7 @@ __device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, c
     // a workgroup's wavefronts share as many items as that leaves them.
     constexpr int kSteps = (FOUR ? 4 : 8) / R;
     const uint32_t channels = (a.hidden + kItem - 1) / kItem, items = n.total * channels, steps = (a.width + W::kDepth - 1) / W::kDepth;
-    const bool long_steps = items * steps * R > 4 * kInGroups * kFewWaves;
+    const bool long_steps = (uint64_t)items * steps * R > 4 * kInGroups * kFewWaves;
     const uint32_t pieces = long_steps ? (steps + kSteps - 1) / kSteps : steps, waves = pieces > 4 ? 8 : pieces > 2 ? 4 : pieces, at_once = kFewWaves / waves;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave / waves;
     f32x4* place = places + group * waves * R * 64;

@@ -509,6 +509,75 @@ def test_tokens_do_not_touch_each_other(t, four):
             assert not bool(out.view()[i].isfinite().all())
 
 
+def few_on_the_gpu(x, expert, weights, w_in, w_out, t, four):
+    """plain_few, by expert; matrices are what the call takes, or what their codes stand for."""
+    tokens, width = x.shape
+    hidden = w_out.shape[2]
+    want, off, size = (torch.zeros(tokens, width, dtype=torch.float64, device="cuda") for _ in range(3))
+    keep = (2.0 ** -16 if t != "f32" else 0.0) if four else HELD[t]
+    for e in range(w_in.shape[0]):
+        token, slot = (expert == e).nonzero(as_tuple=True)
+        a, w, b, c = x[token], weights[token, slot, None].double(), w_in[e].double(), w_out[e].double()
+        both, both_size = a @ b.t(), a.abs() @ b.abs().t()
+        g, u, off_g, off_u = both[:, :hidden], both[:, hidden:], width * SUM * both_size[:, :hidden], width * SUM * both_size[:, hidden:]
+        silu = g * torch.special.expit(g)
+        h = silu * u
+        off_h = 1.1 * off_g * (u.abs() + off_u) + silu.abs() * off_u + (keep + 12 * SUM) * h.abs()
+        off_h = w.abs() * off_h + (2.0 ** -25 if t == "f16" and not four else 2.0 ** -120)
+        want.index_add_(0, token, w * (h @ c.t()))
+        size.index_add_(0, token, (w.abs() * h.abs()) @ c.abs().t())
+        off.index_add_(0, token, off_h @ c.abs().t())
+    return want, off + (hidden + expert.shape[1]) * SUM * size + rounding(t, want)
+
+
+# Sizes that take four tiles to an item, shares of results, tokens from LDS, entries of more than 8, 16 and 32 tokens.
+WIDE = [(64, 2, 24, 72, 1024), (64, 2, 24, 75, 1027), (64, 2, 4, 1208, 4104), (64, 2, 4, 1203, 4101), (8, 4, 40, 520, 1024), (7, 4, 40, 523, 1021),
+        (16, 4, 64, 1536, 1544), (40, 3, 64, 1541, 1537), (1, 8, 64, 1536, 4096)]
+
+
+@pytest.mark.parametrize("tokens,slots,experts,width,hidden", WIDE)
+@pytest.mark.parametrize("four", [False, True], ids=["own", "four"])
+@pytest.mark.parametrize("t", list(TYPES))
+def test_few_of_wide_layers(t, four, tokens, slots, experts, width, hidden):
+    g = torch.Generator(device="cuda").manual_seed(width)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    x, w_in, w_out = randn(tokens, width).to(TYPES[t]), (randn(experts, 2 * hidden, width) / width ** 0.5).to(TYPES[t]), (randn(experts, width, hidden) / hidden ** 0.5).to(TYPES[t])
+    expert = torch.argsort(randn(tokens, experts), dim=1)[:, :slots].to(torch.int32)
+    expert = torch.where(torch.rand(tokens, slots, generator=g, device="cuda") < 0.05, -1, expert)
+    weights = torch.rand(tokens, slots, generator=g, device="cuda")
+    matrices, stands, keep = [], [], []
+    for w in (w_in, w_out):
+        rows, k = w.shape[0] * w.shape[1], w.shape[2]
+        if four:
+            codes, scales = (torch.empty(rows * B.four_bit_groups(k) * n, dtype=torch.uint8, device="cuda") for n in (16, 1))
+            B.tperm_four_bit_store(w.data_ptr(), k, codes.data_ptr(), scales.data_ptr(), rows, k, B.TYPES[t], stream())
+            v = torch.empty(w.shape, device="cuda")
+            B.tperm_four_bit_load(codes.data_ptr(), scales.data_ptr(), v.data_ptr(), k, rows, k, B.TYPE_F32, stream())
+            matrices += [codes.data_ptr(), scales.data_ptr()]
+            keep += [codes, scales]
+            stands.append(v)
+        else:
+            matrices += [w.data_ptr(), None]
+            stands.append(w)
+    out = Matrix(tokens, width, TYPES[t], pad=1)
+    need = B.expert_few_workspace_bytes(tokens, slots, experts, width, hidden, B.TYPES[t], four)
+    room = Matrix(1, need, torch.uint8)
+
+    def few():
+        B.tperm_expert_few(x.data_ptr(), width, expert.data_ptr(), weights.data_ptr(), *matrices, out.ptr, out.stride, room.ptr, need, tokens, slots, experts, width,
+                           hidden, B.TYPES[t], stream())
+        torch.cuda.synchronize()
+        return out.view().clone()
+
+    got = few()
+    want, off = few_on_the_gpu(x.double(), expert, weights, *stands, t, four)
+    near(got, want.cpu(), off.cpu())
+    assert torch.equal(few(), got) and out.outside_untouched()
+    room.before[room.lead:room.lead + need] = 0
+    room.buf[room.lead:room.lead + need] = 0
+    assert torch.equal(room.buf, room.before)
+
+
 def test_large_matrices():
     """An expert's matrix behind 4 GiB: the same bits as from the first place (how a sum is split goes by the sizes, number of experts among them)."""
     experts, width, hidden, tokens, slots = 5, 16384, 16384, 3, 2
