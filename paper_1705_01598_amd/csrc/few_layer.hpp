@@ -295,10 +295,6 @@ __device__ __forceinline__ float forty_on(float v) {
     return __uint_as_float(__builtin_amdgcn_permlane32_swap(w, w, false, false)[1]);
 }
 
-// Workgroups of the second kernel.  With one tile of 8 channels: 16 wavefronts, all entries.  With four: 8 wavefronts and a share of
-// the entries, the shares of the same channels added by the workgroup that comes to its end last.
-template <int R> constexpr uint32_t kOutWaves = R == 1 ? 16 : 8;
-
 template <typename T, bool FOUR, typename S, int STEPS, bool ALIGNED>
 __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
                                             uint32_t to, float* sums) {
@@ -327,10 +323,12 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
     }
 }
 
+// With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the
+// workgroup that comes to its end last.
 template <typename T, bool FOUR, bool ALIGNED, int R>
-__global__ __launch_bounds__(64 * kOutWaves<R>, 4) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
+__global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
     extern __shared__ f32x4 dynamic[];
-    constexpr uint32_t kWaves = kOutWaves<R>, kThreads = 64 * kWaves, kSteps = R == 1 ? (FOUR ? 2 : 8) : (FOUR ? 1 : 2), kBlock = kSteps * Matrix<T, FOUR>::kDepth;
+    constexpr uint32_t kWaves = kFewWaves, kThreads = kFewThreads, kSteps = R == 1 ? (FOUR ? 2 : 4) : (FOUR ? 1 : 2), kBlock = kSteps * Matrix<T, FOUR>::kDepth;
     constexpr uint32_t kRows = R * kChannels;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     float* const sums = (float*)dynamic;
@@ -414,10 +412,10 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
     const auto launch_out = [&](auto aligned, auto tiles) {
         constexpr int kTiles = decltype(tiles)::value;
         constexpr auto kKernel = few_out_kernel<T, FOUR, decltype(aligned)::value, kTiles>;
-        const size_t lds = (size_t)kOutWaves<kTiles> * a.tokens * kTiles * kChannels * 4 + named_bytes(count, a.experts, room.most, false);
+        const size_t lds = (size_t)kFewWaves * a.tokens * kTiles * kChannels * 4 + named_bytes(count, a.experts, room.most, false);
         const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kOutLds) : hipSuccess;
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kKernel, dim3((a.width + kTiles * kChannels - 1) / (kTiles * kChannels), kTiles == 1 ? 1 : room.shares), dim3(64 * kOutWaves<kTiles>), lds, stream,
+        hipLaunchKernelGGL(kKernel, dim3((a.width + kTiles * kChannels - 1) / (kTiles * kChannels), kTiles == 1 ? 1 : room.shares), dim3(kFewThreads), lds, stream,
                            a, room.most, room.pitch);
         return hipGetLastError();
     };
