@@ -6,7 +6,12 @@
 // experts and pieces of their sums, and add up by token in LDS, one array for each wavefront, joined in their order: no
 // atomics on numbers that round, and no rows of the experts in memory.
 // Every workgroup of both finds the named experts and their tokens from the numbers themselves (at most 64 x 64 of
-// them), so no order has to be made first.
+// them; 1.6 us), so no order has to be made first.
+//
+// The matrices are what bounds it: a compute unit takes in 26 GB/s at most, so both kernels want 256 of them busy.  bfloat16, 2048 -> 2 x 1024 -> 2048,
+// kernel times: 64 tokens x 8 of 128 experts 144 + 87 us, 7.4 and 6.1 TB/s; one token x 4 9.8 + 6.1 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
+// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 14.5 + 13.8 us for 56 + 28 MB: 2.1 times what
+// comes in are columns, 64 bytes a lane beside 17 of the matrix.
 #pragma once
 #include <type_traits>
 
@@ -22,7 +27,8 @@ namespace {
 
 constexpr uint32_t kChannels = kFewChannels;
 constexpr int kShareTiles = kFewShareTiles;
-constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit
+constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit, each with many items, so that the tables are made once
+                                        // (64 tokens x 8 of 128, a workgroup to every item of 8 channels 212 us, now 144)
 constexpr size_t kInLds = 80 * 1024, kOutLds = 112 * 1024;
 constexpr uint32_t kColumns = 32;       // tokens of an entry at most
 
@@ -323,6 +329,8 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
     }
 }
 
+// R tiles of 8 channels to a workgroup: columns are read once for them.  64 tokens x 8 of 128 experts, bfloat16: one tile 129 us, as many bytes of hidden rows as of
+// the matrix to each workgroup; four, and eight workgroups to share the entries 86, of which 6 is the joining.
 // With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the
 // workgroup that comes to its end last.
 template <typename T, bool FOUR, bool ALIGNED, int R>
@@ -420,6 +428,8 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
         return hipGetLastError();
     };
     hipError_t e = hipSuccess;
+    // Tokens come from LDS where every workgroup meets them more than four times (8 x 4 of 64 in 4 bits 18.8 -> 15.1 us, while one token's
+    // matrices of 16 bits take 11.8 for 10.5).  Four tiles where an expert has several tokens: 64 x 8 of 128 in 4 bits 92 -> 70, bfloat16 154 -> 144.
     const bool many_items = (uint64_t)room.most * over(a.hidden, kChannels) >= 4 * kInGroups;
     if (FOUR && many_items && sums_bytes(2) + named + staged <= kInLds) {
         if constexpr (FOUR) e = x_aligned ? launch_in(Bool<true>(), Bool<true>(), Bool<true>(), Int<2>()) : launch_in(Bool<true>(), Bool<true>(), Bool<false>(), Int<2>());

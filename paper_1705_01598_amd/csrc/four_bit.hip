@@ -3,6 +3,9 @@
 // HBM is the bound: every element is read once and every code written once.  A thread takes 8 neighbours, four
 // threads side by side a group of 32, whose largest magnitude goes between them by DPP moves.  Scales are powers
 // of two, so the division is exact and the only rounding is that of the code, two of which take one conversion.
+//
+// 65536 x 2048 bfloat16: 61 us to 4 bits, 5.6 TB/s, and 47 back, 7.2 TB/s, as the codes are still in the memory-side cache; 16384 x 8192 binary32
+// 103 and 105 us, 5.9 TB/s.
 #include <type_traits>
 
 #include "decode.hpp"
@@ -82,7 +85,7 @@ template <> struct Largest<__bf16> { static constexpr float k = 0x1.fep127f; };
 template <> struct Largest<_Float16> { static constexpr float k = 65504.0f; };
 
 // 16 bytes of results to a thread: stores past the caches that are whole lines (with 32 bytes of binary32, two stores of every other
-// 16 bytes, 199 us for 536 MB).
+// 16 bytes, 199 us for 536 MB, now 105).
 template <typename T> constexpr int kLoaded = 16 / (int)sizeof(T);
 template <typename T, bool ALIGNED> __global__ __launch_bounds__(kFourBitThreads) void four_bit_load_kernel(const FourBitArgs a) {
     constexpr int V = kLoaded<T>;

@@ -1,4 +1,9 @@
 // Products of few rows with a matrix held in 4 bits.
+//
+// The matrix is read once for 64 rows, the rows once for every workgroup, whose tiles are as many as leave 256 compute units one each: the rows are
+// 4 times the bytes of the matrix for an element, and a compute unit takes in 26 GB/s at most of both together.  bfloat16: one row 2048 x 2048
+// 3.3 us (an empty launch takes 1.6); 16 rows 4096 x 32768 20 us, 3.6 TB/s, with tiles of 32 rows of the matrix 34, of 64 21.2;
+// one row 8192 x 16384 15.8 us, 4.5 TB/s; 64 rows 4096 x 16384 39 us (tiles of 32 65).
 #include <type_traits>
 
 #include "decode.hpp"
