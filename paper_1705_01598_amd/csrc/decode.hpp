@@ -66,10 +66,14 @@ constexpr uint32_t few_most(int64_t tokens, int64_t slots, int64_t experts) {
     const int64_t count = tokens * slots;
     return (uint32_t)((experts < count ? experts : count) + count / 33);
 }
-// Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of matrices on.
-inline uint32_t few_shares(uint64_t blocks, uint32_t most, uint64_t matrix_bytes) {
-    const uint64_t want = over(512, blocks);
-    return most * matrix_bytes < 64 << 20 ? 1 : (uint32_t)(want < most ? want : most);
+// Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of matrices on, and only where columns are
+// much beside the matrix (4 bits, or two tokens to an expert) or 8 channels to a workgroup leave compute units idle.  bfloat16, second kernel, without shares and
+// with: 64 tokens x 8 of 128 129 and 86 us, 16 x 4 of 64, 1024 -> 2 x 512, 16.6 and 14.1, but 4 x 4 of 64 14.6 and 18.7 and 16 x 4 of 32, 2001 -> 2 x 1003, 37 and
+// 44; one x 8 of 128 in 4 bits, 4096 -> 2 x 4096, 34 and 24.
+inline uint32_t few_shares(uint64_t width, uint64_t count, uint32_t most, bool four_bits, uint64_t matrix_bytes) {
+    if (most * matrix_bytes < 64 << 20 || !(four_bits || count >= 2 * (uint64_t)most || width < 1600)) return 1;
+    const uint64_t want = over(512, over(width, kFewShareTiles * kFewChannels));
+    return (uint32_t)(want < most ? want : most);
 }
 struct FewRoom {
     uint32_t most;          // entries at most: one for every 32 tokens that name the same expert
@@ -85,7 +89,7 @@ inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t 
     // one part of 4 bytes an element, two of 2, or three of 2
     r.rows = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
     const uint64_t blocks = over(width, kFewShareTiles * kFewChannels);
-    r.shares = few_shares(blocks, r.most, (uint64_t)width * hidden * (four_bits ? 1 : 2 * type_bytes(type)) / 2);
+    r.shares = few_shares(width, count, r.most, four_bits, (uint64_t)width * hidden * (four_bits ? 1 : 2 * type_bytes(type)) / 2);
     r.partial = r.shares == 1 ? 0 : (size_t)r.shares * blocks * tokens * kFewShareTiles * kFewChannels * 4;
     r.bytes = r.rows + r.partial + (r.shares == 1 ? 0 : blocks * 4);
     return r;
