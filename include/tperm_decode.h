@@ -57,7 +57,8 @@ tperm_status_t tperm_four_bit_load(const uint8_t *codes, const uint8_t *scales, 
                                    int64_t rows, int64_t width, int type, void *hip_stream);
 
 /* Products with a matrix held in 4 bits:  out[r, j] = sum over i of x[r, i] * w[j, i],  w the n rows of k elements that
- * codes and scales stand for.  Values are multiplied as they stand, neither they nor x are rounded first.  Made for few rows, when
+ * codes and scales stand for.  Values are multiplied as they stand, neither they nor x are rounded first (of binary32 numbers below
+ * 2^-102 not all bits may count).  Made for few rows, when
  * the matrix is what there is to read: it is read once for every 64 of them.  Any number of rows is right.
  * TOO_LARGE: codes of more than 2^32 - 256 bytes. */
 tperm_status_t tperm_four_bit_product(const void *x, int64_t x_stride, const uint8_t *codes, const uint8_t *scales,
@@ -70,9 +71,9 @@ tperm_status_t tperm_four_bit_product(const void *x, int64_t x_stride, const uin
  * at).  x, out: tokens rows of width elements, tokens <= TPERM_FEW_TOKENS; w_in: experts matrices of 2 * hidden rows of width
  * elements; w_out: of width rows of hidden elements, dense.  w_in_scales and w_out_scales both NULL: the matrices are of `type`.
  * Both given: w_in and w_out are the codes of tperm_four_bit_store of all rows of all experts.  weights NULL: ones.
- * What lies between the two products is not rounded to `type`: 16 bits of precision at least are kept (22 in binary16, all in
- * binary32); in binary16 weights * g * sigmoid(g) * u beyond its range becomes infinite.  Every expert that is named is read
- * once, others not at all.  A token that names an expert twice gives it the sum of both weights.
+ * What lies between the two products, weights * g * sigmoid(g) * u, is not rounded to `type`: 16 bits of precision at least are kept, all
+ * in binary32, 22 in binary16 with matrices of that type, where it becomes infinite beyond the type's range.  Every expert that is
+ * named is read once for every 32 tokens that name it, others not at all.  A token that names an expert twice gives it the sum of both weights.
  * workspace: tperm_expert_few_workspace(...) bytes on 16 bytes, apart from the other arrays; overwritten; two calls that use
  * the same one at the same time race.  TOO_LARGE: too small a workspace, or one expert's matrix (its codes) of more than 2^32 - 256
  * bytes. */

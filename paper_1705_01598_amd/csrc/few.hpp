@@ -32,9 +32,8 @@ __device__ __forceinline__ f32x4 multiply(f32x4 w, f32x4 x, f32x4 sum) {
     return sum;
 }
 
-// A number as the sum of bfloat16 parts, each what the one before it left: 8 bits to a part, so that two hold a
-// binary16 number and three a binary32 one (below 2^-110 what 2^-133 leaves off).  Infinities and NaN are the first part alone.
-// P parts of 8 numbers.
+// 8 numbers as sums of P bfloat16 parts, each the upper 8 bits of what the one before it left, so that two hold a binary16 number
+// and three a binary32 one (below 2^-102 the last of them is no normal number).  Infinities and NaN are the first part alone.
 template <int P> __device__ __forceinline__ void parts_of(Vec<float, 8> v, bf16x8 (&part)[P]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __builtin_canonicalizef(v[i]);      // a NaN with a bit among the upper 16

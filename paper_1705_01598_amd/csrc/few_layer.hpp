@@ -39,42 +39,30 @@ template <typename T, bool FOUR> struct Hidden {
     typedef Ready<E, kParts> Columns;
 };
 template <typename T, bool FOUR> using Matrix = std::conditional_t<FOUR, FourBits, Elements<T>>;
-// The first product's columns: the tokens as they lie, or, where all of them fit it, from LDS, with rows that are filled up with zeros and
-// in the parts that a matrix in 4 bits takes.
+// The first product's columns: the tokens as they lie, or, for matrices in 4 bits where all tokens fit it, from LDS, in the parts that such a
+// matrix takes and with rows that are filled up with zeros.
 template <typename T, bool FOUR, bool STAGED> struct Tokens {
     typedef std::conditional_t<FOUR, Split<T>, Ready<T, 1>> Columns;
     typedef T E;
 };
-template <typename T, bool FOUR> struct Tokens<T, FOUR, true> {
-    typedef std::conditional_t<FOUR, __bf16, T> E;
-    static constexpr int kParts = FOUR ? Split<T>::kParts : 1;
-    typedef Ready<E, kParts, true> Columns;
+template <typename T> struct Tokens<T, true, true> {
+    typedef Ready<__bf16, Split<T>::kParts, true> Columns;
+    typedef __bf16 E;
 };
 // Elements of a staged row: whole steps, and 16 bytes more so that rows start at different banks.
-template <typename T, bool FOUR> constexpr uint32_t staged_pitch(uint32_t width) {
-    typedef Matrix<T, FOUR> W;
-    return (width + W::kDepth - 1) / W::kDepth * W::kDepth + 16 / sizeof(typename Tokens<T, FOUR, true>::E);
-}
-template <typename T, bool FOUR> constexpr size_t staged_bytes(uint32_t tokens, uint32_t width) {
-    return (size_t)tokens * staged_pitch<T, FOUR>(width) * sizeof(typename Tokens<T, FOUR, true>::E) * Tokens<T, FOUR, true>::kParts;
-}
-template <typename T, bool FOUR, bool ALIGNED> __device__ __forceinline__ void stage(const FewArgs& a, typename Tokens<T, FOUR, true>::E* rows) {
-    typedef typename Tokens<T, FOUR, true>::E E;
-    constexpr int kParts = Tokens<T, FOUR, true>::kParts;
-    const uint32_t pitch = staged_pitch<T, FOUR>(a.width), eights = pitch / 8;     // the 16 bytes more are left as they are
+constexpr uint32_t staged_pitch(uint32_t width) { return (width + FourBits::kDepth - 1) / FourBits::kDepth * FourBits::kDepth + 8; }
+template <typename T> constexpr size_t staged_bytes(uint32_t tokens, uint32_t width) { return (size_t)tokens * staged_pitch(width) * 2 * Split<T>::kParts; }
+template <typename T, bool ALIGNED> __device__ __forceinline__ void stage(const FewArgs& a, __bf16* rows) {
+    constexpr int kParts = Split<T>::kParts;
+    const uint32_t pitch = staged_pitch(a.width), eights = pitch / 8 - 1;      // the 16 bytes more are left as they are
     for (uint32_t i = threadIdx.x; i < a.tokens * eights; i += kFewThreads) {
         const uint32_t t = i / eights, at = (i - t * eights) * 8;
         Vec<T, 8> v = {};
         if (at < a.width) v = load_some<T, 8, ALIGNED>((const T*)a.x + (int64_t)t * a.x_stride + at, (int)(a.width - at));
-        E* const row = rows + t * pitch + at;
-        if constexpr (!FOUR) {
-            store_vec<T, 8, true>(row, v);
-        } else {
-            bf16x8 part[kParts];
-            if constexpr (kParts == 1) part[0] = v;
-            else parts_of<kParts>(widen<T, 8>(v), part);
-            for (int p = 0; p < kParts; ++p) store_vec<__bf16, 8, true>(row + p * a.tokens * pitch, part[p]);
-        }
+        bf16x8 part[kParts];
+        if constexpr (kParts == 1) part[0] = v;
+        else parts_of<kParts>(widen<T, 8>(v), part);
+        for (int p = 0; p < kParts; ++p) store_vec<__bf16, 8, true>(rows + (p * a.tokens + t) * pitch + at, part[p]);
     }
 }
 
@@ -199,7 +187,7 @@ struct Item {
     uint32_t expert, named, first, channel, wave, waves;
 };
 template <typename T, bool FOUR, bool STAGED, typename S, int STEPS, bool ALIGNED>
-__device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, const Item& item, f32x4* sums, const typename Tokens<T, FOUR, true>::E* staged) {
+__device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, const Item& item, f32x4* sums, const __bf16* staged) {
     typedef Matrix<T, FOUR> W;
     const W w = matrix_of<W>(a.w_in, a.in_scales, item.expert, 2 * a.hidden, a.width);
     uint32_t row[S::R];
@@ -211,10 +199,10 @@ __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, co
     typename Tokens<T, FOUR, STAGED>::Columns cols = {};
     for (int m = 0; m < S::M; ++m) {
         const uint32_t t = n.token[item.first + (S::column(m) < item.named ? S::column(m) : 0)];
-        if constexpr (STAGED) x[m] = staged + t * staged_pitch<T, FOUR>(a.width);
+        if constexpr (STAGED) x[m] = staged + t * staged_pitch(a.width);
         else x[m] = (const T*)a.x + (int64_t)t * a.x_stride;
     }
-    if constexpr (STAGED) cols.apart = a.tokens * staged_pitch<T, FOUR>(a.width);
+    if constexpr (STAGED) cols.apart = a.tokens * staged_pitch(a.width);
     f32x4 sum[S::kSums][S::M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, item.wave, item.waves, sum);
     static_assert(S::kSums * S::M <= S::R, "a wavefront's place");
@@ -249,7 +237,7 @@ template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hid
 
 // All items of a workgroup, with R tiles.
 template <typename T, bool FOUR, bool STAGED, bool ALIGNED, int R>
-__device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, const Named& n, f32x4* places, const typename Tokens<T, FOUR, true>::E* staged) {
+__device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, const Named& n, f32x4* places, const __bf16* staged) {
     typedef Matrix<T, FOUR> W;
     typedef Shape<R, 1, false> Few;
     typedef Shape<R, 1, true> Some;
@@ -286,10 +274,10 @@ __device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, c
 template <typename T, bool FOUR, bool STAGED, bool ALIGNED, bool X_ALIGNED, int R>
 __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch, const uint32_t shares) {
     extern __shared__ f32x4 dynamic[];
-    typedef typename Tokens<T, FOUR, true>::E E;
-    E* const staged = (E*)(dynamic + 2 * kFewWaves * R * 64);
-    if constexpr (STAGED) stage<T, FOUR, X_ALIGNED>(a, staged);
-    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T, FOUR>(a.tokens, a.width) : 0), most);
+    static_assert(FOUR || !STAGED, "tokens of matrices in 4 bits");
+    __bf16* const staged = (__bf16*)(dynamic + 2 * kFewWaves * R * 64);
+    if constexpr (STAGED) stage<T, X_ALIGNED>(a, staged);
+    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T>(a.tokens, a.width) : 0), most);
     if (blockIdx.x == 0 && shares != 1)     // counters of the second kernel
         for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
     hidden_items<T, FOUR, STAGED, ALIGNED, R>(a, pitch, n, dynamic, staged);
@@ -404,7 +392,7 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
     const bool x_aligned = on_eights(a.x, a.x_stride, a.width);
     const bool in_aligned = FOUR || on_eights(a.w_in, a.width, a.width), out_aligned = FOUR ? a.hidden % 8 == 0 : on_eights(a.w_out, a.hidden, a.hidden);
     a.by_slots = make_fastdiv(a.slots);
-    const size_t named = named_bytes(count, a.experts, room.most, true), staged = staged_bytes<T, FOUR>(a.tokens, a.width);
+    const size_t named = named_bytes(count, a.experts, room.most, true), staged = staged_bytes<T>(a.tokens, a.width);
     const auto sums_bytes = [](int tiles) { return (size_t)2 * kFewWaves * tiles * 64 * 16; };
     const auto launch_in = [&](auto from_lds, auto aligned, auto x_is, auto tiles) {
         constexpr bool kStaged = decltype(from_lds)::value;
