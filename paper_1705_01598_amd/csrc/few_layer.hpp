@@ -74,7 +74,7 @@ template <typename M> __device__ __forceinline__ M matrix_of(const void* p, cons
         const uint64_t before = (uint64_t)e * rows * m.groups;
         m.rows = (const uint8_t*)p + before * 16, m.scales = scales + before;
     } else {
-        m.stride = depth * (uint32_t)sizeof(*m.rows);
+        m.stride = depth * (uint32_t)sizeof(*m.rows), m.odd = odd_of(p);
         m.rows = (decltype(m.rows))((const char*)p + (uint64_t)e * rows * m.stride);
     }
     return m;
@@ -203,6 +203,7 @@ __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, co
         else x[m] = (const T*)a.x + (int64_t)t * a.x_stride;
     }
     if constexpr (STAGED) cols.apart = a.tokens * staged_pitch(a.width);
+    else cols.odd = odd_of(a.x);
     f32x4 sum[S::kSums][S::M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.width, item.wave, item.waves, sum);
     static_assert(S::kSums * S::M <= S::R, "a wavefront's place");
@@ -304,7 +305,7 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
     }
     const typename H::E* x[M];
     for (int m = 0; m < M; ++m) x[m] = (const typename H::E*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
-    const typename H::Columns cols = {(int64_t)a.tokens * a.slots * pitch};
+    const typename H::Columns cols = {(int64_t)a.tokens * a.slots * pitch, 0};     // rows on 16 bytes
     f32x4 sum[S::kSums][M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, from, to, 0u, 1u, sum);
     for (int m = 0; m < M; ++m) {

@@ -29,7 +29,7 @@ template <typename T, bool ALIGNED, int STEPS, typename S> __global__ __launch_b
         const uint32_t c = first_row + S::column(m);
         x[m] = (const T*)a.x + (int64_t)(c < a.rows ? c : a.rows - 1) * a.x_stride;
     }
-    const Split<T> cols = {};
+    const Split<T> cols = {odd_of(a.x)};
     f32x4 sum[S::kSums][M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, 0u, a.k, wave, (uint32_t)kFewWaves, sum);
     for (int r = 0; r < S::kSums; ++r)
