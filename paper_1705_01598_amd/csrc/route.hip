@@ -7,8 +7,8 @@
 // the smaller: whole numbers of 32 bits where scores have 16, doubles where they have 32.  More slots: a round for each finds the
 // largest number of the group and strikes it out.
 //
-// 65536 tokens x 8 of 128 experts: binary32 9.5 us for 38 MB, of which 1.6 is an empty launch, 5.6 the bytes, and the rest the comparisons, which stand behind the
-// loads of the one round of workgroups (rounds that strike out, for any number of slots, 19.9); bfloat16 through all 128 9.8.  33 x 4 of 64: 2.2 us.
+// 65536 tokens x 8 of 128 experts: binary32 9.5 us for 38 MB, of which 1.6 is an empty launch, 5.6 the bytes, and the comparisons of doubles, which run at half the
+// rate, the longest part (two tokens a lane, the second's scores requested first, 10.4; rounds that strike out, for any number of slots, 19.9); bfloat16 through all 128 9.8.  33 x 4 of 64: 2.2 us.
 // Gradient of 16384 x 6 of 101, binary32, through all: 6.6 us for 14 MB; 65536 x 8 of 128 bfloat16 11 us.
 #include <type_traits>
 
