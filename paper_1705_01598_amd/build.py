@@ -22,7 +22,7 @@ SOURCES = ["plan.cpp", "model.cpp", "product_plan.cpp", "api.cpp", "cache.cpp", 
            "experts_api.cpp", "expert_sort.hip", "expert_rows.hip", "checkpoint.hip",
            "expert_product_f32.hip", "expert_product_f16.hip", "expert_product_bf16.hip"]
 HEADERS = ["fastcall.cpp", "pattern_probe.hip", "latency_probe.hip", "plan.hpp", "kernels.hpp", "verify.hpp", "product.hpp", "tperm_desc.h", "tile_kernel.hpp",
-           "checks.hpp", "decode.hpp", "few.hpp", "few_layer.hpp", "gated.hpp", "launch.hpp", os.path.join("..", "..", "include", "tperm_decode.h"),
+           "checks.hpp", "decode.hpp", "few.hpp", "few_layer.hpp", "few_places.hpp", "gated.hpp", "launch.hpp", os.path.join("..", "..", "include", "tperm_decode.h"),
            "experts.hpp", "expert_vector.hpp", "expert_product.hpp", "expert_product_inst.hpp", os.path.join("..", "..", "include", "tperm_experts.h"), os.path.join("..", "..", "include", "tperm.h"),
            os.path.join("..", "..", "include", "tperm_tuning.h")]
 

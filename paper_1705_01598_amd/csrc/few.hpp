@@ -16,6 +16,7 @@
 #include <stdint.h>
 
 #include "expert_vector.hpp"
+#include "few_places.hpp"
 
 namespace tperm {
 
@@ -101,7 +102,7 @@ template <Reach REACH, typename T, int N, bool ALIGNED> __device__ __forceinline
     } else if constexpr (REACH == Reach::kShort) {
         return load_some<T, N, false>(i < depth ? row + i : row, (int)depth - (int)i);
     } else if constexpr (ALIGNED) {
-        const Vec<T, N> v = load_vec<T, N, true>(row + (i < depth ? i : 0u));
+        const Vec<T, N> v = load_vec<T, N, true>(row + start_in(i, depth));
         u32x4 w = __builtin_bit_cast(u32x4, v);
         for (int k = 0; k < 4; ++k) w[k] = i < depth ? w[k] : 0u;
         return __builtin_bit_cast(Vec<T, N>, w);
@@ -139,7 +140,7 @@ template <typename T> struct Elements {
 // A matrix in 4 bits: a group of 32 codes and its scale to a lane and step.  A code times its power of two is exact in bfloat16, and two
 // of them take one conversion.
 struct FourBits {
-    static constexpr int kEach = 32, kDepth = 256, kSub = 4;
+    static constexpr int kEach = 32, kDepth = kFourBitDepth, kSub = 4;
     typedef bf16x8 Part;
     const uint8_t *rows, *scales;
     uint32_t groups;                    // of a row
@@ -166,8 +167,8 @@ struct FourBits {
     static __device__ __forceinline__ float scale_value(uint32_t biased) { return __uint_as_float(biased == 255u ? 0x7FC00000u : biased << 23); }
 };
 
-// Columns that are there as the products take them: kParts arrays of E, `apart` elements from each other.  FILLED: they are zeros up to a whole step,
-// and start on 16 bytes.
+// Columns that are there as the products take them: kParts arrays of E, `apart` elements from each other.  FILLED: rows start on 16 bytes and are zeros up to
+// the end of the step that their last element is in; steps behind that are not looked at, though they may be requested.
 template <typename E, int P, bool FILLED = false> struct Ready {
     static constexpr int kParts = P, N = 16 / sizeof(E);
     int64_t apart;
@@ -177,7 +178,8 @@ template <typename E, int P, bool FILLED = false> struct Ready {
     // sub-product j of a lane's elements from i on
     template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const E* x, uint32_t i, uint32_t depth, int j) const {
         Raw r;
-        for (int p = 0; p < P; ++p) r.part[p] = load_reach<FILLED ? Reach::kAll : REACH, E, N, ALIGNED || FILLED>(x + p * apart, i + j * N, depth, odd);
+        constexpr Reach kReach = FILLED && REACH != Reach::kAll ? Reach::kEnd : REACH;
+        for (int p = 0; p < P; ++p) r.part[p] = load_reach<kReach, E, N, ALIGNED || FILLED>(x + p * apart, i + j * N, depth, odd);
         return r;
     }
     static __device__ __forceinline__ void open(const Raw& r, Part (&part)[P]) {

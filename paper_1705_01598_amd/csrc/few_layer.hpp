@@ -49,8 +49,6 @@ template <typename T> struct Tokens<T, true, true> {
     typedef Ready<__bf16, Split<T>::kParts, true> Columns;
     typedef __bf16 E;
 };
-// Elements of a staged row: whole steps, and 16 bytes more so that rows start at different banks.
-constexpr uint32_t staged_pitch(uint32_t width) { return (width + FourBits::kDepth - 1) / FourBits::kDepth * FourBits::kDepth + 8; }
 template <typename T> constexpr size_t staged_bytes(uint32_t tokens, uint32_t width) { return (size_t)tokens * staged_pitch(width) * 2 * Split<T>::kParts; }
 template <typename T, bool ALIGNED> __device__ __forceinline__ void stage(const FewArgs& a, __bf16* rows) {
     constexpr int kParts = Split<T>::kParts;
