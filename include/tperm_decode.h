@@ -71,8 +71,8 @@ tperm_status_t tperm_four_bit_product(const void *x, int64_t x_stride, const uin
  * at).  x, out: tokens rows of width elements, tokens <= TPERM_FEW_TOKENS; w_in: experts matrices of 2 * hidden rows of width
  * elements; w_out: of width rows of hidden elements, dense.  w_in_scales and w_out_scales both NULL: the matrices are of `type`.
  * Both given: w_in and w_out are the codes of tperm_four_bit_store of all rows of all experts.  weights NULL: ones.
- * What lies between the two products, weights * g * sigmoid(g) * u, is not rounded to `type`: 16 bits of precision at least are kept, all
- * in binary32, 22 in binary16 with matrices of that type, where it becomes infinite beyond the type's range.  Every expert that is
+ * What lies between the two products, weights * g * sigmoid(g) * u, is held in binary32 whatever `type` is, with its bits and its range (beside matrices of
+ * bfloat16 or 4 bits not all bits of numbers below 2^-102 may count).  Every expert that is
  * named is read once for every 32 tokens that name it, others not at all.  A token that names an expert twice gives it the sum of both weights.
  * workspace: tperm_expert_few_workspace(...) bytes on 16 bytes, apart from the other arrays; overwritten; two calls that use
  * the same one at the same time race.  TOO_LARGE: too small a workspace, or one expert's matrix (its codes) of more than 2^32 - 256

@@ -6,6 +6,7 @@
 
 #include "../../include/tperm_decode.h"
 #include "experts.hpp"
+#include "few_places.hpp"
 
 namespace tperm {
 
@@ -66,12 +67,14 @@ constexpr uint32_t few_most(int64_t tokens, int64_t slots, int64_t experts) {
     const int64_t count = tokens * slots;
     return (uint32_t)((experts < count ? experts : count) + count / 33);
 }
-// Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of matrices on, and only where columns are
-// much beside the matrix (4 bits, or two tokens to an expert) or 8 channels to a workgroup leave compute units idle.  bfloat16, second kernel, without shares and
-// with: 64 tokens x 8 of 128 129 and 86 us, 16 x 4 of 64, 1024 -> 2 x 512, 16.6 and 14.1, but 4 x 4 of 64 14.6 and 18.7 and 16 x 4 of 32, 2001 -> 2 x 1003, 37 and
-// 44; one x 8 of 128 in 4 bits, 4096 -> 2 x 4096, 34 and 24.
+// Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of second matrices on (of those of all entries that there
+// could be; which experts are named is not known here), and only where columns are much beside the matrix (two tokens to an entry) or 8 channels to a workgroup
+// leave compute units idle; in 4 bits, where columns are always much, from 20 MiB on.  Second kernel, without shares and with, in us.  bfloat16: 64 tokens x 8 of 128,
+// 2048 -> 2 x 1024, 135 and 92, 64 x 4 of 32 56 and 44, 16 x 4 of 64, 1024 -> 2 x 512, 16.8 and 15.0, but 4 x 4 of 64 16.1 and 18.5 and 16 x 4 of 32,
+// 2001 -> 2 x 1003, 32 and 50.  4 bits: one x 8 of 128, 4096 -> 2 x 4096, 39 and 28, 8 x 4 of 64, 2048 -> 2 x 1024 (32 MiB), 17.0 and 14.4, 16 x 4 of 32 (32 MiB)
+// 20.7 and 15.8, binary32 64 x 2 of 8, 2048 -> 2 x 2048 (22 MiB), 44.6 and 29.7, but 4 x 4 of 32 (16 MiB) 11.3 and 11.8, one x 4 (4 MiB) 6.4 and 8.4.
 inline uint32_t few_shares(uint64_t width, uint64_t count, uint32_t most, bool four_bits, uint64_t matrix_bytes) {
-    if (most * matrix_bytes < 64 << 20 || !(four_bits || count >= 2 * (uint64_t)most || width < 1600)) return 1;
+    if (most * matrix_bytes < (four_bits ? 20 << 20 : 64 << 20) || !(four_bits || count >= 2 * (uint64_t)most || width < 1600)) return 1;
     const uint64_t want = over(512, over(width, kFewShareTiles * kFewChannels));
     return (uint32_t)(want < most ? want : most);
 }
@@ -85,9 +88,8 @@ inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t 
     FewRoom r;
     const int64_t count = tokens * slots;
     r.most = few_most(tokens, slots, experts);
-    r.pitch = (uint32_t)((hidden + 31) / 32 * 32);
-    // one part of 4 bytes an element, two of 2, or three of 2
-    r.rows = (size_t)count * r.pitch * (four_bits && type == TPERM_TYPE_F32 ? 6 : 4);
+    r.pitch = hidden_pitch((uint32_t)hidden, four_bits ? 32 : 16 / (uint32_t)type_bytes(type));
+    r.rows = (size_t)count * r.pitch * 4;
     const uint64_t blocks = over(width, kFewShareTiles * kFewChannels);
     r.shares = few_shares(width, count, r.most, four_bits, (uint64_t)width * hidden * (four_bits ? 1 : 2 * type_bytes(type)) / 2);
     r.partial = r.shares == 1 ? 0 : (size_t)r.shares * blocks * tokens * kFewShareTiles * kFewChannels * 4;

@@ -32,10 +32,18 @@ __device__ __forceinline__ f32x4 multiply(f32x4 w, f32x4 x, f32x4 sum) {
     for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[i], sum, 0, 0, 0);
     return sum;
 }
+// Binary32 columns beside a matrix of binary16, which holds neither their range nor their bits: its elements are exact in binary32, whose products take the
+// matrix cores 16 times as long.
+__device__ __forceinline__ f32x4 multiply(f16x8 w, Vec<float, 8> x, f32x4 sum) {
+    for (int i = 0; i < 8; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32((float)w[i], x[i], sum, 0, 0, 0);
+    return sum;
+}
 
 // 8 numbers as sums of P bfloat16 parts, each the upper 8 bits of what the one before it left, so that two hold a binary16 number
-// and three a binary32 one (below 2^-102 the last of them is no normal number).  Infinities and NaN are the first part alone.
-template <int P> __device__ __forceinline__ void parts_of(Vec<float, 8> v, bf16x8 (&part)[P]) {
+// and three a binary32 one (below 2^-102 the last of them is no normal number).  Infinities and NaN are the first part alone; with FINITE, which is 44
+// instructions for three parts instead of 68, they make the second one NaN.
+template <int P, bool FINITE = false> __device__ __forceinline__ void parts_of(Vec<float, 8> v, bf16x8 (&part)[P]) {
+    if constexpr (!FINITE)
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __builtin_canonicalizef(v[i]);      // a NaN with a bit among the upper 16
 #pragma unroll
@@ -51,7 +59,7 @@ template <int P> __device__ __forceinline__ void parts_of(Vec<float, 8> v, bf16x
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float rest = v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
-                v[i] = __builtin_isfinite(v[i]) ? rest : 0.0f;
+                v[i] = FINITE || p > 0 || __builtin_isfinite(v[i]) ? rest : 0.0f;
             }
     }
 }
@@ -175,11 +183,11 @@ template <typename E, int P, bool FILLED = false> struct Ready {
     uint32_t odd;
     typedef Vec<E, N> Part;
     struct Raw { Part part[P]; };
-    // sub-product j of a lane's elements from i on
-    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const E* x, uint32_t i, uint32_t depth, int j) const {
+    // sub-product j of the elements that piece `piece` of a step from i on has
+    template <typename W, Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const E* x, uint32_t i, uint32_t piece, uint32_t depth, int j) const {
         Raw r;
         constexpr Reach kReach = FILLED && REACH != Reach::kAll ? Reach::kEnd : REACH;
-        for (int p = 0; p < P; ++p) r.part[p] = load_reach<kReach, E, N, ALIGNED || FILLED>(x + p * apart, i + j * N, depth, odd);
+        for (int p = 0; p < P; ++p) r.part[p] = load_reach<kReach, E, N, ALIGNED || FILLED>(x + p * apart, i + piece * W::kEach + j * N, depth, odd);
         return r;
     }
     static __device__ __forceinline__ void open(const Raw& r, Part (&part)[P]) {
@@ -194,14 +202,33 @@ template <typename T> struct Split {
     static constexpr int kLoads = sizeof(T) / 2, N = 16 / sizeof(T);
     struct Raw { Vec<T, N> v[kLoads]; };
     uint32_t odd;
-    template <Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const T* x, uint32_t i, uint32_t depth, int j) const {
+    template <typename W, Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const T* x, uint32_t i, uint32_t piece, uint32_t depth, int j) const {
         Raw r;
-        for (int k = 0; k < kLoads; ++k) r.v[k] = load_reach<REACH, T, N, ALIGNED>(x, i + j * 8 + k * N, depth, odd);
+        for (int k = 0; k < kLoads; ++k) r.v[k] = load_reach<REACH, T, N, ALIGNED>(x, i + piece * W::kEach + j * 8 + k * N, depth, odd);
         return r;
     }
     static __device__ __forceinline__ void open(const Raw& r, Part (&part)[kParts]) {
         if constexpr (kParts == 1) part[0] = __builtin_bit_cast(bf16x8, r.v[0]);
         else parts_of<kParts>(widen<T, 8>(__builtin_bit_cast(Eight, r.v)), part);
+    }
+};
+// Columns in binary32, laid out as hidden_place says and zeros to the end of their last step: as bfloat16 parts (FINITE: see there), or as they are beside a
+// matrix of PART.
+template <typename PART, bool FINITE> struct Held {
+    static constexpr bool kSplit = std::is_same_v<PART, bf16x8>;
+    static constexpr int kParts = kSplit ? 3 : 1, kNumbers = std::is_same_v<PART, f32x4> ? 4 : 8, kLoads = kNumbers / 4;
+    typedef Vec<float, kNumbers> Numbers;
+    typedef std::conditional_t<kSplit, bf16x8, Numbers> Part;
+    struct Raw { f32x4 v[kLoads]; };
+    template <typename W, Reach REACH, bool ALIGNED> __device__ __forceinline__ Raw load(const float* x, uint32_t i, uint32_t piece, uint32_t depth, int j) const {
+        const float* const step = x + (REACH == Reach::kAll ? i : start_in(i, depth)) + hidden_piece(piece);
+        Raw r;
+        for (int k = 0; k < kLoads; ++k) r.v[k] = load_vec<float, 4, true>(step + hidden_quad(j * kLoads + k));
+        return r;
+    }
+    static __device__ __forceinline__ void open(const Raw& r, Part (&part)[kParts]) {
+        if constexpr (kSplit) parts_of<kParts, FINITE>(__builtin_bit_cast(Numbers, r.v), part);
+        else part[0] = __builtin_bit_cast(Part, r.v);
     }
 };
 
@@ -240,8 +267,8 @@ __device__ __forceinline__ void steps(const W& w, const uint32_t (&row)[S::R], c
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto columns_of = [&](int t, int turn, int j, int m) {
-        const uint32_t at = i + t * W::kDepth + (S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece()) * W::kEach;
-        return cols.template load<REACH, ALIGNED>(x[m], at, depth, j);
+        const uint32_t piece = S::kPaired ? (threadIdx.x & 63u) / 16 * 2 + turn : S::piece();
+        return cols.template load<W, REACH, ALIGNED>(x[m], i + t * W::kDepth, piece, depth, j);
     };
     const auto products = [&](int t, int turn, int j, const typename X::Raw (&raw)[M]) {
         typename X::Part c[M][X::kParts];

@@ -1,7 +1,7 @@
 // A whole mixture-of-experts layer for a few tokens, in two kernels.
 //
 // The first multiplies the g and u rows of 8 hidden channels of a named expert (an item) with the tokens that name it, applies the gated
-// activation and the token's weight, and stores the hidden rows in parts; a workgroup goes through every so-many-th
+// activation and the token's weight, and stores the hidden rows in binary32; a workgroup goes through every so-many-th
 // item.  The second: a workgroup to 8 channels of the result goes through all named experts, its wavefronts share
 // experts and pieces of their sums, and add up by token in LDS, one array for each wavefront, joined in their order: no
 // atomics on numbers that round, and no rows of the experts in memory.
@@ -9,9 +9,9 @@
 // them; 1.6 us), so no order has to be made first.
 //
 // The matrices are what bounds it: a compute unit takes in 26 GB/s at most, so both kernels want 256 of them busy.  bfloat16, 2048 -> 2 x 1024 -> 2048,
-// kernel times: 64 tokens x 8 of 128 experts 144 + 87 us, 7.4 and 6.1 TB/s; one token x 4 9.8 + 6.1 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
-// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 14.5 + 13.8 us for 56 + 28 MB: 2.1 times what
-// comes in are columns, 64 bytes a lane beside 17 of the matrix.
+// kernel times: 64 tokens x 8 of 128 experts 142 + 91 us, 7.5 and 5.9 TB/s; one token x 4 9.9 + 7.2 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
+// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 14.9 + 14.6 us for 56 + 28 MB: most of what
+// comes in are columns, 64 bytes a lane of tokens and 128 of hidden rows beside 17 of the matrix.
 #pragma once
 #include <type_traits>
 
@@ -28,17 +28,16 @@ namespace {
 constexpr uint32_t kChannels = kFewChannels;
 constexpr int kShareTiles = kFewShareTiles;
 constexpr uint32_t kInGroups = 512;     // workgroups of the first kernel: two to a compute unit, each with many items, so that the tables are made once
-                                        // (64 tokens x 8 of 128, a workgroup to every item of 8 channels 212 us, now 144)
+                                        // (64 tokens x 8 of 128, a workgroup to every item of 8 channels 212 us, now 142)
 constexpr size_t kInLds = 80 * 1024, kOutLds = 112 * 1024;
 constexpr uint32_t kColumns = 32;       // tokens of an entry at most
 
-// What the second product's columns are: how a hidden row is held between the kernels.
-template <typename T, bool FOUR> struct Hidden {
-    typedef std::conditional_t<FOUR, __bf16, T> E;
-    static constexpr int kParts = !FOUR && sizeof(T) == 4 ? 1 : FOUR && sizeof(T) == 4 ? 3 : 2;
-    typedef Ready<E, kParts> Columns;
-};
 template <typename T, bool FOUR> using Matrix = std::conditional_t<FOUR, FourBits, Elements<T>>;
+// What the second product's columns are: hidden rows are held in binary32 between the kernels, and become what the matrix takes on their way.
+// Held in two bfloat16 parts, 16 bits, the second kernel takes 85 us for 64 x 8 of 128 instead of 91, and 14.0 for one of 8 x 4 of 64 in 4 bits instead of 14.6;
+// in three parts stored by the first kernel 97 and 17.6 (without shares, for 17.0).  In binary16 (64 x 8 of 128: 102) the matrix in two bfloat16
+// parts, which meet all three of a hidden value, was no faster than products of binary32.
+template <typename T, bool FOUR, bool FINITE = true> using Hidden = Held<typename Matrix<T, FOUR>::Part, FINITE>;
 // The first product's columns: the tokens as they lie, or, for matrices in 4 bits where all tokens fit it, from LDS, in the parts that such a
 // matrix takes and with rows that are filled up with zeros.
 template <typename T, bool FOUR, bool STAGED> struct Tokens {
@@ -208,12 +207,11 @@ __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, co
     for (int r = 0; r < S::kSums; ++r)
         for (int m = 0; m < S::M; ++m) sums[(item.wave * S::R + r * S::M + m) * 64 + threadIdx.x % 64] = sum[r][m];
 }
-// The sums of all wavefronts of an item, the activation, and the hidden rows in parts: four channels of one column to a lane.
-template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, uint32_t pitch, const Named& n, const Item& item, const f32x4* sums) {
-    typedef Hidden<T, FOUR> H;
+// The sums of all wavefronts of an item, the activation, and the hidden rows: four channels of one column to a lane.
+template <uint32_t EACH, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, uint32_t pitch, const Named& n, const Item& item, const f32x4* sums) {
     for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < S::M * S::R * S::kColumns; i += item.waves * 64) {
         const uint32_t half = i % 2, b = i / 2 % (S::R / 2), column = i / S::R, m = column / S::kColumns, c = column % S::kColumns, channel = item.channel + b * kChannels + half * 4;
-        if (column >= item.named || channel >= pitch) continue;
+        if (column >= item.named) continue;
         f32x4 gu[2] = {};
         for (uint32_t v = 0; v < item.waves; ++v)
             for (int r = 0; r < 2; ++r) gu[r] += sums_at<S>(sums + v * S::R * 64, 2 * b + r, m, half, c);
@@ -221,17 +219,15 @@ template <typename T, bool FOUR, typename S> __device__ __forceinline__ void hid
         f32x4 h;
         for (int k = 0; k < 4; ++k) {
             const Sigmoid s = sigmoid<float>(gu[0][k]);
-            h[k] = gu[0][k] * s.p * gu[1][k] * s.last * weight;
+            h[k] = channel + k < a.hidden ? gu[0][k] * s.p * gu[1][k] * s.last * weight : 0.0f;
         }
-        const int64_t rows = (int64_t)a.tokens * a.slots;
-        typename H::E* const out = (typename H::E*)a.rows + (int64_t)(item.first + column) * pitch + channel;
-        for (int p = 0; p < H::kParts; ++p) {
-            const Vec<typename H::E, 4> part = narrow<typename H::E, 4>(h);
-            store_vec<typename H::E, 4, true>(out + p * rows * pitch, part);
-            const f32x4 back = widen<typename H::E, 4>(part);
-            for (int k = 0; k < 4; ++k) h[k] = __builtin_isfinite(back[k]) ? h[k] - back[k] : 0.0f;
-        }
+        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + column) * pitch + hidden_place(channel, EACH), h);
     }
+    // behind the last channels zeros to the row's end, which whole items reach at most
+    const uint32_t end = item.channel + S::R / 2 * kChannels, quads = (pitch - end) / 4;
+    if (end < a.hidden || quads == 0) return;
+    for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < quads * item.named; i += item.waves * 64)
+        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + i / quads) * pitch + hidden_place(end + i % quads * 4, EACH), f32x4{});
 }
 
 // All items of a workgroup, with R tiles.
@@ -263,9 +259,9 @@ __device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, c
         }
         __syncthreads();
         if (item.named == 0) {
-        } else if (item.named <= 8) hidden_rows<T, FOUR, Few>(a, pitch, n, item, place);
-        else if (item.named <= 16) hidden_rows<T, FOUR, Some>(a, pitch, n, item, place);
-        else hidden_rows<T, FOUR, Many>(a, pitch, n, item, place);
+        } else if (item.named <= 8) hidden_rows<W::kEach, Few>(a, pitch, n, item, place);
+        else if (item.named <= 16) hidden_rows<W::kEach, Some>(a, pitch, n, item, place);
+        else hidden_rows<W::kEach, Many>(a, pitch, n, item, place);
         place = place < places + kPlace ? place + kPlace : place - kPlace;
     }
 }
@@ -292,7 +288,6 @@ template <typename T, bool FOUR, typename S, int STEPS, bool ALIGNED>
 __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
                                             uint32_t to, float* sums) {
     typedef Matrix<T, FOUR> W;
-    typedef Hidden<T, FOUR> H;
     constexpr int R = S::R, M = S::M;
     const uint32_t lane = threadIdx.x & 63u, channel = blockIdx.x * (R * kChannels);
     const W w = matrix_of<W>(a.w_out, a.out_scales, e, a.width, a.hidden);
@@ -301,11 +296,23 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
         const uint32_t j = channel + r * kChannels + S::row();
         row[r] = j < a.width ? j : a.width - 1;
     }
-    const typename H::E* x[M];
-    for (int m = 0; m < M; ++m) x[m] = (const typename H::E*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
-    const typename H::Columns cols = {(int64_t)a.tokens * a.slots * pitch, 0};     // rows on 16 bytes
+    const float* x[M];
+    for (int m = 0; m < M; ++m) x[m] = (const float*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
     f32x4 sum[S::kSums][M] = {};
-    rows_by_columns<S, STEPS, ALIGNED>(w, row, cols, x, from, to, 0u, 1u, sum);
+    rows_by_columns<S, STEPS, ALIGNED>(w, row, Hidden<T, FOUR>{}, x, from, to, 0u, 1u, sum);
+    if constexpr (Hidden<T, FOUR>::kSplit) {
+        // An infinity in a column has made all its sums NaN: those are formed again, in the same order, with parts that hold infinities.
+        bool none = false;
+        for (int r = 0; r < S::kSums; ++r)
+            for (int m = 0; m < M; ++m) none = none || __builtin_isunordered(sum[r][m][0], sum[r][m][1]) || __builtin_isunordered(sum[r][m][2], sum[r][m][3]);
+        if (__builtin_amdgcn_ballot_w64(none) != 0) {
+            f32x4 again[S::kSums][M] = {};
+            rows_by_columns<S, 1, ALIGNED>(w, row, Hidden<T, FOUR, false>{}, x, from, to, 0u, 1u, again);
+            for (int r = 0; r < S::kSums; ++r)
+                for (int m = 0; m < M; ++m)
+                    for (int i = 0; i < 4; ++i) sum[r][m][i] = sum[r][m][i] == sum[r][m][i] ? sum[r][m][i] : again[r][m][i];
+        }
+    }
     for (int m = 0; m < M; ++m) {
         if constexpr (!S::kPaired)
             for (int r = 0; r < R; ++r)
@@ -316,8 +323,8 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
     }
 }
 
-// R tiles of 8 channels to a workgroup: columns are read once for them.  64 tokens x 8 of 128 experts, bfloat16: one tile 129 us, as many bytes of hidden rows as of
-// the matrix to each workgroup; four, and eight workgroups to share the entries 86, of which 6 is the joining.
+// R tiles of 8 channels to a workgroup: columns are read once for them.  64 tokens x 8 of 128 experts, bfloat16: one tile 135 us, as many bytes of hidden rows as of
+// the matrix to each workgroup; four, and eight workgroups to share the entries 91, of which 6 is the joining.
 // With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the
 // workgroup that comes to its end last.
 template <typename T, bool FOUR, bool ALIGNED, int R>
@@ -363,7 +370,7 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a
     // The share goes out, the workgroup counts itself, and the one that finds all others counted adds up the shares in their order.  Shares are stored
     // and loaded at agent scope, past every cache that not all compute units see, and a wavefront waits until its stores are complete before
     // the barrier behind which one thread counts; so who sees the count sees the shares.  A release at agent scope would also write back
-    // the L2 with all that is in it, for each workgroup: 64 tokens x 8 of 128 experts 86 -> 102 us.
+    // the L2 with all that is in it, for each workgroup: 64 tokens x 8 of 128 experts 91 -> 109 us.
     float* const shares = a.shares + (int64_t)blockIdx.x * gridDim.y * a.tokens * kRows;
     for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads)
         __hip_atomic_store(shares + (int64_t)blockIdx.y * a.tokens * kRows + i, joined(i / kRows, i % kRows), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
