@@ -42,22 +42,6 @@ struct FourBitProductArgs {
 };
 hipError_t launch_four_bit_product(const FourBitProductArgs& a, int type, hipStream_t stream);
 
-struct FewArgs {
-    const void* x;
-    const int32_t* expert;
-    const float* weights;           // or NULL
-    const void *w_in, *w_out;       // elements or codes
-    const uint8_t *in_scales, *out_scales;
-    void* out;
-    int64_t x_stride, out_stride;
-    uint32_t tokens, slots, experts, width, hidden;
-    void* rows;                     // the workspace: the hidden rows, and behind them (set by the launcher) shares of results and counters
-    float* shares;
-    uint32_t* ended;
-    FastDiv by_slots;               // set by the launcher
-};
-hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
-
 constexpr uint32_t kFewChannels = 8;        // of a tile
 constexpr uint32_t kFewShareTiles = 4;      // of a workgroup of the second kernel where workgroups share the entries of their channels
 
@@ -96,5 +80,22 @@ inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t 
     r.bytes = r.rows + r.partial + (r.shares == 1 ? 0 : blocks * 4);
     return r;
 }
+
+struct FewArgs {
+    const void* x;
+    const int32_t* expert;
+    const float* weights;           // or NULL
+    const void *w_in, *w_out;       // elements or codes
+    const uint8_t *in_scales, *out_scales;
+    void* out;
+    int64_t x_stride, out_stride;
+    uint32_t tokens, slots, experts, width, hidden;
+    FewRoom room;                   // the workspace's layout, by which its size was checked
+    void* rows;                     // the workspace: the hidden rows, and behind them (set by the launcher) shares of results and counters
+    float* shares;
+    uint32_t* ended;
+    FastDiv by_slots;               // set by the launcher
+};
+hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);
 
 }  // namespace tperm

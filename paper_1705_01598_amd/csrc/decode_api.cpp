@@ -5,9 +5,9 @@
 #include "decode.hpp"
 
 namespace tperm {
-template <typename T> hipError_t few_of(const FewArgs& a, int type, hipStream_t stream);
+template <typename T> hipError_t few_of(const FewArgs& a, hipStream_t stream);
 hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream) {
-    return type == TPERM_TYPE_F32 ? few_of<float>(a, type, stream) : type == TPERM_TYPE_F16 ? few_of<_Float16>(a, type, stream) : few_of<__bf16>(a, type, stream);
+    return type == TPERM_TYPE_F32 ? few_of<float>(a, stream) : type == TPERM_TYPE_F16 ? few_of<_Float16>(a, stream) : few_of<__bf16>(a, stream);
 }
 }  // namespace tperm
 
@@ -131,7 +131,7 @@ tperm_status_t tperm_expert_few(const void* x, int64_t x_stride, const int32_t* 
     const int64_t in_bytes = four ? in_groups * 16 : 2 * hidden * width * (int64_t)elem, out_bytes = four ? out_groups * 16 : hidden * width * (int64_t)elem;
     if (in_bytes > kOperandBytes || out_bytes > kOperandBytes) return TPERM_ERR_TOO_LARGE;
     if (tokens == 0) return TPERM_OK;
-    const size_t need = few_room(tokens, slots, experts, width, hidden, type, four).bytes;
+    const FewRoom room = few_room(tokens, slots, experts, width, hidden, type, four);
     const Array arrays[] = {{x, matrix_bytes(tokens, x_stride, width, elem), elem, false},
                             {expert, tokens * slots * 4, 4, false},
                             {weights, weights ? tokens * slots * 4 : 0, 4, false},
@@ -140,15 +140,15 @@ tperm_status_t tperm_expert_few(const void* x, int64_t x_stride, const int32_t* 
                             {w_out, experts * out_bytes, w_align, false},
                             {w_out_scales, four ? experts * out_groups : 0, 1, false},
                             {out, matrix_bytes(tokens, out_stride, width, elem), elem, true},
-                            {workspace, (int64_t)need, 16, true}};
+                            {workspace, (int64_t)room.bytes, 16, true}};
     const tperm_status_t bad = check(arrays);
     if (bad != TPERM_OK) return bad;
-    if (workspace_bytes < need) return TPERM_ERR_TOO_LARGE;
+    if (workspace_bytes < room.bytes) return TPERM_ERR_TOO_LARGE;
     FewArgs a = {};
     a.x = x, a.expert = expert, a.weights = weights, a.w_in = w_in, a.w_out = w_out, a.in_scales = w_in_scales, a.out_scales = w_out_scales, a.out = out;
     a.x_stride = x_stride, a.out_stride = out_stride;
     a.tokens = (uint32_t)tokens, a.slots = (uint32_t)slots, a.experts = (uint32_t)experts, a.width = (uint32_t)width, a.hidden = (uint32_t)hidden;
-    a.rows = workspace;
+    a.room = room, a.rows = workspace;
     return launched(launch_few(a, type, (hipStream_t)hip_stream));
 }
 

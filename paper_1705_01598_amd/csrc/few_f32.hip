@@ -2,6 +2,6 @@
 
 namespace tperm {
 
-template hipError_t few_of<float>(const FewArgs&, int, hipStream_t);
+template hipError_t few_of<float>(const FewArgs&, hipStream_t);
 
 }  // namespace tperm

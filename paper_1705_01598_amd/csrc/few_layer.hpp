@@ -102,13 +102,13 @@ __device__ __forceinline__ uint32_t upto(uint32_t v) {
     return v;
 }
 
-template <uint32_t THREADS, bool WEIGHTS> __device__ __forceinline__ Named find_named(const FewArgs& a, void* lds, uint32_t most) {
+template <uint32_t THREADS, bool WEIGHTS> __device__ __forceinline__ Named find_named(const FewArgs& a, void* lds) {
     static_assert(2 * THREADS >= TPERM_EXPERTS_MAX, "two experts to a thread");
     __shared__ uint32_t wave_total[THREADS / 64], twice;
     const uint32_t count = a.tokens * a.slots, wave = threadIdx.x >> 6;
     Named n;
-    n.mask = (uint32_t*)lds, n.entry = n.mask + 2 * a.experts, n.weight = (float*)(n.entry + most), n.first = (uint16_t*)(n.weight + (WEIGHTS ? count : 0));
-    n.number = n.first + most, n.start = n.number + count, n.token = (uint8_t*)(n.start + a.experts);
+    n.mask = (uint32_t*)lds, n.entry = n.mask + 2 * a.experts, n.weight = (float*)(n.entry + a.room.most), n.first = (uint16_t*)(n.weight + (WEIGHTS ? count : 0));
+    n.number = n.first + a.room.most, n.start = n.number + count, n.token = (uint8_t*)(n.start + a.experts);
     int32_t own = -1;
     float own_weight = 1.0f;
     if (threadIdx.x < count) {
@@ -208,7 +208,7 @@ __device__ __forceinline__ void hidden_sums(const FewArgs& a, const Named& n, co
         for (int m = 0; m < S::M; ++m) sums[(item.wave * S::R + r * S::M + m) * 64 + threadIdx.x % 64] = sum[r][m];
 }
 // The sums of all wavefronts of an item, the activation, and the hidden rows: four channels of one column to a lane.
-template <uint32_t EACH, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, uint32_t pitch, const Named& n, const Item& item, const f32x4* sums) {
+template <uint32_t EACH, typename S> __device__ __forceinline__ void hidden_rows(const FewArgs& a, const Named& n, const Item& item, const f32x4* sums) {
     for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < S::M * S::R * S::kColumns; i += item.waves * 64) {
         const uint32_t half = i % 2, b = i / 2 % (S::R / 2), column = i / S::R, m = column / S::kColumns, c = column % S::kColumns, channel = item.channel + b * kChannels + half * 4;
         if (column >= item.named) continue;
@@ -221,18 +221,18 @@ template <uint32_t EACH, typename S> __device__ __forceinline__ void hidden_rows
             const Sigmoid s = sigmoid<float>(gu[0][k]);
             h[k] = channel + k < a.hidden ? gu[0][k] * s.p * gu[1][k] * s.last * weight : 0.0f;
         }
-        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + column) * pitch + hidden_place(channel, EACH), h);
+        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + column) * a.room.pitch + hidden_place(channel, EACH), h);
     }
     // behind the last channels zeros to the row's end, which whole items reach at most
-    const uint32_t end = item.channel + S::R / 2 * kChannels, quads = (pitch - end) / 4;
+    const uint32_t end = item.channel + S::R / 2 * kChannels, quads = (a.room.pitch - end) / 4;
     if (end < a.hidden || quads == 0) return;
     for (uint32_t i = item.wave * 64 + threadIdx.x % 64; i < quads * item.named; i += item.waves * 64)
-        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + i / quads) * pitch + hidden_place(end + i % quads * 4, EACH), f32x4{});
+        store_vec<float, 4, true>((float*)a.rows + (int64_t)(item.first + i / quads) * a.room.pitch + hidden_place(end + i % quads * 4, EACH), f32x4{});
 }
 
 // All items of a workgroup, with R tiles.
 template <typename T, bool FOUR, bool STAGED, bool ALIGNED, int R>
-__device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, const Named& n, f32x4* places, const __bf16* staged) {
+__device__ __forceinline__ void hidden_items(const FewArgs& a, const Named& n, f32x4* places, const __bf16* staged) {
     typedef Matrix<T, FOUR> W;
     typedef Shape<R, 1, false> Few;
     typedef Shape<R, 1, true> Some;
@@ -259,23 +259,23 @@ __device__ __forceinline__ void hidden_items(const FewArgs& a, uint32_t pitch, c
         }
         __syncthreads();
         if (item.named == 0) {
-        } else if (item.named <= 8) hidden_rows<W::kEach, Few>(a, pitch, n, item, place);
-        else if (item.named <= 16) hidden_rows<W::kEach, Some>(a, pitch, n, item, place);
-        else hidden_rows<W::kEach, Many>(a, pitch, n, item, place);
+        } else if (item.named <= 8) hidden_rows<W::kEach, Few>(a, n, item, place);
+        else if (item.named <= 16) hidden_rows<W::kEach, Some>(a, n, item, place);
+        else hidden_rows<W::kEach, Many>(a, n, item, place);
         place = place < places + kPlace ? place + kPlace : place - kPlace;
     }
 }
 
 template <typename T, bool FOUR, bool STAGED, bool ALIGNED, bool X_ALIGNED, int R>
-__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch, const uint32_t shares) {
+__global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a) {
     extern __shared__ f32x4 dynamic[];
     static_assert(FOUR || !STAGED, "tokens of matrices in 4 bits");
     __bf16* const staged = (__bf16*)(dynamic + 2 * kFewWaves * R * 64);
     if constexpr (STAGED) stage<T, X_ALIGNED>(a, staged);
-    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T>(a.tokens, a.width) : 0), most);
-    if (blockIdx.x == 0 && shares != 1)     // counters of the second kernel
+    const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T>(a.tokens, a.width) : 0));
+    if (blockIdx.x == 0 && a.room.shares != 1)     // counters of the second kernel
         for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
-    hidden_items<T, FOUR, STAGED, ALIGNED, R>(a, pitch, n, dynamic, staged);
+    hidden_items<T, FOUR, STAGED, ALIGNED, R>(a, n, dynamic, staged);
 }
 
 // What lane l + 40 holds, for the lanes l of the first half whose l % 16 is below 8.
@@ -285,7 +285,7 @@ __device__ __forceinline__ float forty_on(float v) {
 }
 
 template <typename T, bool FOUR, typename S, int STEPS, bool ALIGNED>
-__device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
+__device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t e, uint32_t named, const uint8_t* token, uint32_t first_row, uint32_t from,
                                             uint32_t to, float* sums) {
     typedef Matrix<T, FOUR> W;
     constexpr int R = S::R, M = S::M;
@@ -297,7 +297,7 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
         row[r] = j < a.width ? j : a.width - 1;
     }
     const float* x[M];
-    for (int m = 0; m < M; ++m) x[m] = (const float*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * pitch;
+    for (int m = 0; m < M; ++m) x[m] = (const float*)a.rows + (int64_t)(first_row + (S::column(m) < named ? S::column(m) : 0)) * a.room.pitch;
     f32x4 sum[S::kSums][M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, Hidden<T, FOUR>{}, x, from, to, 0u, 1u, sum);
     if constexpr (Hidden<T, FOUR>::kSplit) {
@@ -328,14 +328,14 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t pitch, ui
 // With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the
 // workgroup that comes to its end last.
 template <typename T, bool FOUR, bool ALIGNED, int R>
-__global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a, const uint32_t most, const uint32_t pitch) {
+__global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a) {
     extern __shared__ f32x4 dynamic[];
     constexpr uint32_t kWaves = kFewWaves, kThreads = kFewThreads, kSteps = R == 1 ? (FOUR ? 2 : 4) : (FOUR ? 1 : 2), kBlock = kSteps * Matrix<T, FOUR>::kDepth;
     constexpr uint32_t kRows = R * kChannels;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     float* const sums = (float*)dynamic;
     for (uint32_t i = threadIdx.x; i < kWaves * a.tokens * kRows; i += kThreads) sums[i] = 0.0f;
-    const Named n = find_named<kThreads, false>(a, sums + kWaves * a.tokens * kRows, most);
+    const Named n = find_named<kThreads, false>(a, sums + kWaves * a.tokens * kRows);
     float* const mine = sums + wave * a.tokens * kRows;
     const uint32_t begin = n.total * blockIdx.y / gridDim.y, entries = n.total * (blockIdx.y + 1) / gridDim.y - begin;
     if (entries != 0) {
@@ -345,13 +345,13 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a
             const uint32_t rank = begin + item / pieces, from = item % pieces * per * kBlock, end = from + per * kBlock;
             const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.entry[rank]), first_row = (uint32_t)__builtin_amdgcn_readfirstlane((int)n.first[rank]);
             const uint32_t e = entry & 0xFFFFu, named = entry >> 16, to = end < a.hidden ? end : a.hidden;
-            if (named <= 8) result_sums<T, FOUR, Shape<R, 1, false>, kSteps, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+            if (named <= 8) result_sums<T, FOUR, Shape<R, 1, false>, kSteps, ALIGNED>(a, e, named, n.token, first_row, from, to, mine);
             else if constexpr (R == 1) {
-                if (named <= 16) result_sums<T, FOUR, Shape<R, 2, false>, FOUR ? 1 : 4, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
-                else result_sums<T, FOUR, Shape<R, 4, false>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+                if (named <= 16) result_sums<T, FOUR, Shape<R, 2, false>, FOUR ? 1 : 4, ALIGNED>(a, e, named, n.token, first_row, from, to, mine);
+                else result_sums<T, FOUR, Shape<R, 4, false>, FOUR ? 1 : 2, ALIGNED>(a, e, named, n.token, first_row, from, to, mine);
             } else {
-                if (named <= 16) result_sums<T, FOUR, Shape<R, 1, true>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
-                else result_sums<T, FOUR, Shape<R, 2, true>, FOUR ? 1 : 2, ALIGNED>(a, pitch, e, named, n.token, first_row, from, to, mine);
+                if (named <= 16) result_sums<T, FOUR, Shape<R, 1, true>, FOUR ? 1 : 2, ALIGNED>(a, e, named, n.token, first_row, from, to, mine);
+                else result_sums<T, FOUR, Shape<R, 2, true>, FOUR ? 1 : 2, ALIGNED>(a, e, named, n.token, first_row, from, to, mine);
             }
         }
     }
@@ -390,8 +390,8 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a
 template <bool B> using Bool = std::integral_constant<bool, B>;
 template <int N> using Int = std::integral_constant<int, N>;
 
-template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream_t stream) {
-    const FewRoom room = few_room(a.tokens, a.slots, a.experts, a.width, a.hidden, type, FOUR);
+template <typename T, bool FOUR> hipError_t layer(FewArgs a, hipStream_t stream) {
+    const FewRoom room = a.room;
     a.shares = (float*)((char*)a.rows + room.rows), a.ended = (uint32_t*)((char*)a.shares + room.partial);
     const uint32_t count = a.tokens * a.slots;
     const auto on_eights = [](const void* p, uint64_t stride, uint32_t width) { return ((uintptr_t)p | stride * sizeof(T)) % 16 == 0 && width % 8 == 0; };
@@ -408,7 +408,7 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
         const size_t lds = sums_bytes(kTiles) + named + (kStaged ? staged : 0);
         const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kInLds) : hipSuccess;
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kKernel, dim3((uint32_t)(items < kInGroups ? items : kInGroups)), dim3(kFewThreads), lds, stream, a, room.most, room.pitch, room.shares);
+        hipLaunchKernelGGL(kKernel, dim3((uint32_t)(items < kInGroups ? items : kInGroups)), dim3(kFewThreads), lds, stream, a);
         return hipGetLastError();
     };
     const auto launch_out = [&](auto aligned, auto tiles) {
@@ -417,8 +417,7 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, int type, hipStream
         const size_t lds = (size_t)kFewWaves * a.tokens * kTiles * kChannels * 4 + named_bytes(count, a.experts, room.most, false);
         const hipError_t e = lds > 64 * 1024 ? allow_lds<kKernel>(kOutLds) : hipSuccess;
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kKernel, dim3((a.width + kTiles * kChannels - 1) / (kTiles * kChannels), kTiles == 1 ? 1 : room.shares), dim3(kFewThreads), lds, stream,
-                           a, room.most, room.pitch);
+        hipLaunchKernelGGL(kKernel, dim3((a.width + kTiles * kChannels - 1) / (kTiles * kChannels), kTiles == 1 ? 1 : room.shares), dim3(kFewThreads), lds, stream, a);
         return hipGetLastError();
     };
     hipError_t e = hipSuccess;
@@ -446,6 +445,6 @@ static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX,
 
 }  // namespace
 
-template <typename T> hipError_t few_of(const FewArgs& a, int type, hipStream_t stream) { return a.in_scales != nullptr ? layer<T, true>(a, type, stream) : layer<T, false>(a, type, stream); }
+template <typename T> hipError_t few_of(const FewArgs& a, hipStream_t stream) { return a.in_scales != nullptr ? layer<T, true>(a, stream) : layer<T, false>(a, stream); }
 
 }  // namespace tperm
