@@ -53,10 +53,10 @@ constexpr uint32_t few_most(int64_t tokens, int64_t slots, int64_t experts) {
 }
 // Workgroups that share the entries of the same channels, so that there are 512 of them: from 64 MiB of second matrices on (of those of all entries that there
 // could be; which experts are named is not known here), and only where columns are much beside the matrix (two tokens to an entry) or 8 channels to a workgroup
-// leave compute units idle; in 4 bits, where columns are always much, from 20 MiB on.  Second kernel, without shares and with, in us.  bfloat16: 64 tokens x 8 of 128,
-// 2048 -> 2 x 1024, 135 and 92, 64 x 4 of 32 56 and 44, 16 x 4 of 64, 1024 -> 2 x 512, 16.8 and 15.0, but 4 x 4 of 64 16.1 and 18.5 and 16 x 4 of 32,
-// 2001 -> 2 x 1003, 32 and 50.  4 bits: one x 8 of 128, 4096 -> 2 x 4096, 39 and 28, 8 x 4 of 64, 2048 -> 2 x 1024 (32 MiB), 17.0 and 14.4, 16 x 4 of 32 (32 MiB)
-// 20.7 and 15.8, binary32 64 x 2 of 8, 2048 -> 2 x 2048 (22 MiB), 44.6 and 29.7, but 4 x 4 of 32 (16 MiB) 11.3 and 11.8, one x 4 (4 MiB) 6.4 and 8.4.
+// leave compute units idle; in 4 bits, where columns are always much, from 20 MiB on.  Whole calls, without shares and with, in us.  bfloat16: 64 tokens x 8 of 128,
+// 2048 -> 2 x 1024, 264 and 227, 64 x 4 of 32 114 and 99, 2 x 1024 from 1024 81 and 56, but 4 x 4 of 64 38 and 43 and 16 x 4 of 32, 2001 -> 2 x 1003, 86 and
+// 110.  4 bits: one x 8 of 128, 4096 -> 2 x 4096, 72 and 63, 16 x 4 of 32, 2048 -> 2 x 1024 (32 MiB), 37.9 and 35.4, 8 x 4 of 64 (32 MiB) 30.3 and 29.5,
+// 64 x 2 of 8, 2048 -> 2 x 2048 (22 MiB), 66 and 49, but 4 x 4 of 32 (16 MiB) 20.3 and 22.7.
 inline uint32_t few_shares(uint64_t width, uint64_t count, uint32_t most, bool four_bits, uint64_t matrix_bytes) {
     if (most * matrix_bytes < (four_bits ? 20 << 20 : 64 << 20) || !(four_bits || count >= 2 * (uint64_t)most || width < 1600)) return 1;
     const uint64_t want = over(512, over(width, kFewShareTiles * kFewChannels));
@@ -66,7 +66,7 @@ struct FewRoom {
     uint32_t most;          // entries at most: one for every 32 tokens that name the same expert
     uint32_t pitch;         // elements of a hidden row
     uint32_t shares;        // workgroups that share the entries of the same channels
-    size_t rows, partial, bytes;
+    size_t rows, bytes;     // of the hidden rows, and of all
 };
 inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t width, int64_t hidden, int type, bool four_bits) {
     FewRoom r;
@@ -76,8 +76,7 @@ inline FewRoom few_room(int64_t tokens, int64_t slots, int64_t experts, int64_t 
     r.rows = (size_t)count * r.pitch * 4;
     const uint64_t blocks = over(width, kFewShareTiles * kFewChannels);
     r.shares = few_shares(width, count, r.most, four_bits, (uint64_t)width * hidden * (four_bits ? 1 : 2 * type_bytes(type)) / 2);
-    r.partial = r.shares == 1 ? 0 : (size_t)r.shares * blocks * tokens * kFewShareTiles * kFewChannels * 4;
-    r.bytes = r.rows + r.partial + (r.shares == 1 ? 0 : blocks * 4);
+    r.bytes = r.rows + (r.shares == 1 ? 0 : (size_t)r.shares * blocks * tokens * kFewShareTiles * kFewChannels * 4);
     return r;
 }
 
@@ -91,9 +90,8 @@ struct FewArgs {
     int64_t x_stride, out_stride;
     uint32_t tokens, slots, experts, width, hidden;
     FewRoom room;                   // the workspace's layout, by which its size was checked
-    void* rows;                     // the workspace: the hidden rows, and behind them (set by the launcher) shares of results and counters
+    void* rows;                     // the workspace: the hidden rows, and behind them (set by the launcher) shares of results
     float* shares;
-    uint32_t* ended;
     FastDiv by_slots;               // set by the launcher
 };
 hipError_t launch_few(const FewArgs& a, int type, hipStream_t stream);

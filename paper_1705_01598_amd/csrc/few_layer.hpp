@@ -1,16 +1,17 @@
-// A whole mixture-of-experts layer for a few tokens, in two kernels.
+// A whole mixture-of-experts layer for a few tokens, in two kernels or three.
 //
 // The first multiplies the g and u rows of 8 hidden channels of a named expert (an item) with the tokens that name it, applies the gated
 // activation and the token's weight, and stores the hidden rows in binary32; a workgroup goes through every so-many-th
 // item.  The second: a workgroup to 8 channels of the result goes through all named experts, its wavefronts share
 // experts and pieces of their sums, and add up by token in LDS, one array for each wavefront, joined in their order: no
-// atomics on numbers that round, and no rows of the experts in memory.
+// atomics on numbers that round, and no rows of the experts in memory.  Where there is much to read, several workgroups share the experts of
+// their channels, and a third kernel adds up their shares.
 // Every workgroup of both finds the named experts and their tokens from the numbers themselves (at most 64 x 64 of
 // them; 1.6 us), so no order has to be made first.
 //
 // The matrices are what bounds it: a compute unit takes in 26 GB/s at most, so both kernels want 256 of them busy.  bfloat16, 2048 -> 2 x 1024 -> 2048,
-// kernel times: 64 tokens x 8 of 128 experts 142 + 91 us, 7.5 and 5.9 TB/s; one token x 4 9.9 + 7.2 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
-// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 14.9 + 14.6 us for 56 + 28 MB: most of what
+// kernel times: 64 tokens x 8 of 128 experts 142 + 83 + 5 us, 7.5 and 6.3 TB/s; one token x 4 9.9 + 7.2 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
+// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 15 + 12 + 4 us for 56 + 28 MB: most of what
 // comes in are columns, 64 bytes a lane of tokens and 128 of hidden rows beside 17 of the matrix.
 #pragma once
 #include <type_traits>
@@ -273,8 +274,6 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_in_kernel(const FewArgs a)
     __bf16* const staged = (__bf16*)(dynamic + 2 * kFewWaves * R * 64);
     if constexpr (STAGED) stage<T, X_ALIGNED>(a, staged);
     const Named n = find_named<kFewThreads, true>(a, (char*)staged + (STAGED ? staged_bytes<T>(a.tokens, a.width) : 0));
-    if (blockIdx.x == 0 && a.room.shares != 1)     // counters of the second kernel
-        for (uint32_t i = threadIdx.x; i < (a.width + kShareTiles * kChannels - 1) / (kShareTiles * kChannels); i += kFewThreads) a.ended[i] = 0;
     hidden_items<T, FOUR, STAGED, ALIGNED, R>(a, n, dynamic, staged);
 }
 
@@ -324,9 +323,11 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t e, uint32
 }
 
 // R tiles of 8 channels to a workgroup: columns are read once for them.  64 tokens x 8 of 128 experts, bfloat16: one tile 135 us, as many bytes of hidden rows as of
-// the matrix to each workgroup; four, and eight workgroups to share the entries 91, of which 6 is the joining.
-// With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the
-// workgroup that comes to its end last.
+// the matrix to each workgroup; four, and eight workgroups to share the entries 84.
+// With one tile of 8 channels a workgroup goes through all entries, with four through a share of them, and the shares of the same channels are added by the next kernel
+// (4.8 us, 1.6 of them the launch).  Adding them in the workgroup that comes to its end last saves a launch, but the others' stores have to be seen across the chip's L2 caches:
+// with a release by each workgroup the kernel took 109 us, and with stores past the caches and a wait for them, which no language
+// model covers, 91.
 template <typename T, bool FOUR, bool ALIGNED, int R>
 __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a) {
     extern __shared__ f32x4 dynamic[];
@@ -367,24 +368,27 @@ __global__ __launch_bounds__(kFewThreads, 4) void few_out_kernel(const FewArgs a
             if (i % kRows < channels) ((T*)a.out)[(int64_t)(i / kRows) * a.out_stride + first + i % kRows] = (T)joined(i / kRows, i % kRows);
         return;
     }
-    // The share goes out, the workgroup counts itself, and the one that finds all others counted adds up the shares in their order.  Shares are stored
-    // and loaded at agent scope, past every cache that not all compute units see, and a wavefront waits until its stores are complete before
-    // the barrier behind which one thread counts; so who sees the count sees the shares.  A release at agent scope would also write back
-    // the L2 with all that is in it, for each workgroup: 64 tokens x 8 of 128 experts 91 -> 109 us.
-    float* const shares = a.shares + (int64_t)blockIdx.x * gridDim.y * a.tokens * kRows;
-    for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads)
-        __hip_atomic_store(shares + (int64_t)blockIdx.y * a.tokens * kRows + i, joined(i / kRows, i % kRows), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __shared__ uint32_t before;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0) before = __hip_atomic_fetch_add(a.ended + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    if (before + 1 != gridDim.y) return;
-    for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads) {
-        float y = 0.0f;
-        for (uint32_t v = 0; v < gridDim.y; ++v) y += __hip_atomic_load(shares + (int64_t)v * a.tokens * kRows + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (i % kRows < channels) ((T*)a.out)[(int64_t)(i / kRows) * a.out_stride + first + i % kRows] = (T)y;
+    float* const share = a.shares + ((int64_t)blockIdx.x * gridDim.y + blockIdx.y) * a.tokens * kRows;
+    for (uint32_t i = threadIdx.x; i < a.tokens * kRows; i += kThreads) share[i] = joined(i / kRows, i % kRows);
+}
+
+// Adds up the shares of 4 channels of a token to a thread, in their order, eight of them requested at once.
+constexpr uint32_t kJoinThreads = 64;
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void few_join_kernel(const FewArgs a) {
+    constexpr uint32_t kRows = kShareTiles * kChannels;
+    const uint32_t quad = blockIdx.y * kJoinThreads + threadIdx.x, channel = blockIdx.x * kRows + quad % (kRows / 4) * 4;
+    if (quad >= a.tokens * (kRows / 4) || channel >= a.width) return;
+    const float* const shares = a.shares + (int64_t)blockIdx.x * a.room.shares * a.tokens * kRows + quad * 4;
+    f32x4 y = {};
+    for (uint32_t first = 0; first < a.room.shares; first += 8) {
+        f32x4 part[8];
+#pragma unroll
+        for (uint32_t v = 0; v < 8; ++v) part[v] = load_vec<float, 4, true>(shares + (int64_t)(first + v < a.room.shares ? first + v : first) * a.tokens * kRows);
+#pragma unroll
+        for (uint32_t v = 0; v < 8; ++v)
+            if (first + v < a.room.shares) y += part[v];
     }
+    store_some<T, 4, false>((T*)a.out + (int64_t)(quad / (kRows / 4)) * a.out_stride + channel, narrow<T, 4>(y), (int)(a.width - channel));
 }
 
 template <bool B> using Bool = std::integral_constant<bool, B>;
@@ -392,7 +396,7 @@ template <int N> using Int = std::integral_constant<int, N>;
 
 template <typename T, bool FOUR> hipError_t layer(FewArgs a, hipStream_t stream) {
     const FewRoom room = a.room;
-    a.shares = (float*)((char*)a.rows + room.rows), a.ended = (uint32_t*)((char*)a.shares + room.partial);
+    a.shares = (float*)((char*)a.rows + room.rows);
     const uint32_t count = a.tokens * a.slots;
     const auto on_eights = [](const void* p, uint64_t stride, uint32_t width) { return ((uintptr_t)p | stride * sizeof(T)) % 16 == 0 && width % 8 == 0; };
     const bool x_aligned = on_eights(a.x, a.x_stride, a.width);
@@ -435,7 +439,11 @@ template <typename T, bool FOUR> hipError_t layer(FewArgs a, hipStream_t stream)
     const auto launch_shared = [&](auto aligned) {
         return room.shares == 1 ? launch_out(aligned, Int<1>()) : launch_out(aligned, Int<kShareTiles>());
     };
-    return out_aligned ? launch_shared(Bool<true>()) : launch_shared(Bool<false>());
+    e = out_aligned ? launch_shared(Bool<true>()) : launch_shared(Bool<false>());
+    if (e != hipSuccess || room.shares == 1) return e;
+    constexpr uint32_t kRows = kShareTiles * kChannels;
+    hipLaunchKernelGGL(few_join_kernel<T>, dim3((a.width + kRows - 1) / kRows, (a.tokens * (kRows / 4) + kJoinThreads - 1) / kJoinThreads), dim3(kJoinThreads), 0, stream, a);
+    return hipGetLastError();
 }
 
 static_assert(named_bytes(TPERM_FEW_TOKENS * TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX, few_most(TPERM_FEW_TOKENS, TPERM_SLOTS_MAX, TPERM_EXPERTS_MAX), true) <=
