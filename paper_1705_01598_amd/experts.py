@@ -305,11 +305,11 @@ def _bench(argv=None):
     ap.add_argument("--bits", type=int, choices=[4, 16, 32], help="with --answer: 4 holds the matrices in 4 bits")
     a = ap.parse_args(argv)
     dtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[a.dtype]
+    if a.bits not in (None, 4, 8 * dtype.itemsize) or (a.bits == 4 and not a.answer):
+        ap.error("--bits: 4 with --answer, or those of the type")
     g = torch.Generator(device="cuda").manual_seed(1705)
     randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
     layer = ExpertLayer(a.experts, a.slots, a.width, a.hidden, dtype)
-    if a.bits not in (None, 4, 8 * dtype.itemsize) or (a.bits == 4 and not a.answer):
-        ap.error("--bits: 4 with --answer, or those of the type")
     x, grad = randn(a.tokens, a.width).to(dtype), randn(a.tokens, a.width).to(dtype)
     w_in = (randn(a.experts, 2 * a.hidden, a.width) / a.width ** 0.5).to(dtype)
     w_out = (randn(a.experts, a.width, a.hidden) / a.hidden ** 0.5).to(dtype)
