@@ -10,8 +10,8 @@
 // them; 1.6 us), so no order has to be made first.
 //
 // The matrices are what bounds it: a compute unit takes in 26 GB/s at most, so both kernels want 256 of them busy.  bfloat16, 2048 -> 2 x 1024 -> 2048,
-// kernel times: 64 tokens x 8 of 128 experts 142 + 83 + 5 us, 7.5 and 6.3 TB/s; one token x 4 9.9 + 7.2 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
-// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits: 15 + 12 + 4 us for 56 + 28 MB: most of what
+// kernel times: 64 tokens x 8 of 128 experts, 88 of them named, 142 + 83 + 5 us for 738 + 369 MB, 5.2 and 4.4 TB/s; one token x 4 9.9 + 7.2 us for 33.5 + 16.8 MB, of which 1.6 each is an empty
+// launch; a read of so many bytes that does nothing else takes 7.2 and 4.8 us.  8 x 4 of 64 in 4 bits, 20 of them named: 15.6 + 11.6 + 3.8 us for 45 + 22 MB: most of what
 // comes in are columns, 64 bytes a lane of tokens and 128 of hidden rows beside 17 of the matrix.
 #pragma once
 #include <type_traits>

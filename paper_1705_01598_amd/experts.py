@@ -9,7 +9,7 @@ expert, the two products with the gated activation between them and the combinat
 reads tokens through the sorted order, so rows are never gathered into a buffer.  For the backward pass the layer
 keeps the input and the gates in 8 bits (``tperm_checkpoint_store``, ``tperm_gated_forward``); the input's rows
 are multiplied out of their codes.  A program that only asks for answers calls ``answer``, which keeps nothing and takes few tokens through
-two kernels, with matrices as they are or held in 4 bits (``hold``); ``route`` chooses the experts and their weights from a
+two kernels (or a third that joins their shares), with matrices as they are or held in 4 bits (``hold``); ``route`` chooses the experts and their weights from a
 router's scores, ``route_backward`` takes the weights' gradient back to them.  Everything here is argument bookkeeping around the calls of
 ``include/tperm_experts.h`` and ``include/tperm_decode.h``; tensors are dense and contiguous, on the layer's GPU, and work is enqueued on
 that GPU's current stream, whichever GPU is the current one (a layer is used on one stream at a time).
@@ -149,8 +149,10 @@ class ExpertLayer:
 
     def answer(self, x, expert, weights, w_in, w_out=None):
         """The layer's result as forward() gives it, with nothing kept for a backward pass and what a forward pass kept left as it is.  w_in and
-        w_out are matrices, or w_in alone is what hold() gave.  Up to FEW_TOKENS tokens take two kernels that read the experts'
-        matrices once; more take the passes of forward(), with matrices in 4 bits brought back to the layer's type first."""
+        w_out are matrices, or w_in alone is what hold() gave.  Up to FEW_TOKENS tokens take kernels that read the named experts'
+        matrices once for every 32 tokens that name them; more take the passes of forward().  For these, matrices in 4 bits are brought back to the
+        layer's type in every call, all experts' and in memory of that size (128 experts of 2048 -> 2 x 1024 -> 2048 in 16 bits: 1.6 GB written and read);
+        a program without that memory answers in parts of FEW_TOKENS tokens."""
         torch, B = self._torch, self._B
         e, k, w, h, t = self.experts, self.slots, self.width, self.hidden, self._type
         held = w_in if isinstance(w_in, HeldMatrices) else None
