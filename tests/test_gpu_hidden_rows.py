@@ -198,3 +198,40 @@ def test_an_infinite_hidden_value_where_results_are_shared(t, four, tokens):
     near(got[1], torch.where(last == 0, math.nan, torch.sign(last) * math.inf).cpu(), torch.zeros(()))
     others = torch.arange(tokens, device="cuda") != 1
     assert torch.equal(got[others], clean[others]) and bool(clean.isfinite().all())
+
+
+def test_shared_results_in_a_graph_between_eager_passes():
+    """The third kernel in a captured pass: replays between eager passes of other tokens through the same workspace give the eager bits."""
+    tokens, slots, experts, width, hidden, t = 12, 4, 48, 1001, 1030, "bf16"
+    g = torch.Generator(device="cuda").manual_seed(3)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    keep, at = [], []
+    for rows, k in ((experts * 2 * hidden, width), (experts * width, hidden)):
+        w = (randn(rows, k) / k ** 0.5).to(TYPES[t])
+        codes, scales = (torch.empty(rows * B.four_bit_groups(k) * n, dtype=torch.uint8, device="cuda") for n in (16, 1))
+        B.tperm_four_bit_store(w.data_ptr(), k, codes.data_ptr(), scales.data_ptr(), rows, k, B.TYPES[t], stream())
+        keep += [codes, scales]
+        at += [codes.data_ptr(), scales.data_ptr()]
+    expert, weights = torch.argsort(randn(tokens, experts), dim=1)[:, :slots].to(torch.int32), torch.rand(tokens, slots, generator=g, device="cuda")
+    need = B.expert_few_workspace_bytes(tokens, slots, experts, width, hidden, B.TYPES[t], True)
+    assert need > tokens * slots * 1280 * 4      # there are shares behind the hidden rows
+    room = torch.empty(need, dtype=torch.uint8, device="cuda")
+    x, other, out = randn(tokens, width).to(TYPES[t]), randn(tokens, width).to(TYPES[t]), torch.empty(tokens, width, dtype=TYPES[t], device="cuda")
+
+    def few(x):
+        B.tperm_expert_few(x.data_ptr(), width, expert.data_ptr(), weights.data_ptr(), *at, out.data_ptr(), width, room.data_ptr(), need, tokens, slots, experts, width,
+                           hidden, B.TYPES[t], stream())
+
+    few(x)
+    torch.cuda.synchronize()
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        few(x)
+    for _ in range(4):
+        few(other)
+        torch.cuda.synchronize()
+        assert not torch.equal(out, want)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
