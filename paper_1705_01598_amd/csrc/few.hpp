@@ -32,9 +32,8 @@ __device__ __forceinline__ f32x4 multiply(f32x4 w, f32x4 x, f32x4 sum) {
     for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[i], sum, 0, 0, 0);
     return sum;
 }
-// Binary32 columns beside a matrix of binary16, which holds neither their range nor their bits: its elements are exact in binary32, whose products take the
-// matrix cores 16 times as long.
-__device__ __forceinline__ f32x4 multiply(f16x8 w, Vec<float, 8> x, f32x4 sum) {
+// Binary32 columns beside a matrix of 16 bits, whose elements are exact in binary32: products of that take the matrix cores 16 times as long.
+template <typename T> __device__ __forceinline__ f32x4 multiply(Vec<T, 8> w, Vec<float, 8> x, f32x4 sum) {
     for (int i = 0; i < 8; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32((float)w[i], x[i], sum, 0, 0, 0);
     return sum;
 }
@@ -212,10 +211,10 @@ template <typename T> struct Split {
         else parts_of<kParts>(widen<T, 8>(__builtin_bit_cast(Eight, r.v)), part);
     }
 };
-// Columns in binary32, laid out as hidden_place says and zeros to the end of their last step: as bfloat16 parts (FINITE: see there), or as they are beside a
-// matrix of PART.
-template <typename PART, bool FINITE> struct Held {
-    static constexpr bool kSplit = std::is_same_v<PART, bf16x8>;
+// Columns in binary32, laid out as hidden_place says and zeros to the end of their last step, beside a matrix whose products take PART of a lane: as bfloat16 parts
+// (SPLIT; only what is finite, and only beside what is), or as they are.  A binary16 matrix holds neither the range nor the bits of such parts.
+template <typename PART, bool SPLIT> struct Held {
+    static constexpr bool kSplit = SPLIT && std::is_same_v<PART, bf16x8>;
     static constexpr int kParts = kSplit ? 3 : 1, kNumbers = std::is_same_v<PART, f32x4> ? 4 : 8, kLoads = kNumbers / 4;
     typedef Vec<float, kNumbers> Numbers;
     typedef std::conditional_t<kSplit, bf16x8, Numbers> Part;
@@ -227,7 +226,7 @@ template <typename PART, bool FINITE> struct Held {
         return r;
     }
     static __device__ __forceinline__ void open(const Raw& r, Part (&part)[kParts]) {
-        if constexpr (kSplit) parts_of<kParts, FINITE>(__builtin_bit_cast(Numbers, r.v), part);
+        if constexpr (kSplit) parts_of<kParts, true>(__builtin_bit_cast(Numbers, r.v), part);
         else part[0] = __builtin_bit_cast(Part, r.v);
     }
 };

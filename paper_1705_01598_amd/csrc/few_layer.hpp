@@ -38,7 +38,7 @@ template <typename T, bool FOUR> using Matrix = std::conditional_t<FOUR, FourBit
 // Held in two bfloat16 parts, 16 bits, the second kernel takes 85 us for 64 x 8 of 128 instead of 91, and 14.0 for one of 8 x 4 of 64 in 4 bits instead of 14.6;
 // in three parts stored by the first kernel 97 and 17.6 (without shares, for 17.0).  In binary16 (64 x 8 of 128: 102) the matrix in two bfloat16
 // parts, which meet all three of a hidden value, was no faster than products of binary32.
-template <typename T, bool FOUR, bool FINITE = true> using Hidden = Held<typename Matrix<T, FOUR>::Part, FINITE>;
+template <typename T, bool FOUR, bool SPLIT = true> using Hidden = Held<typename Matrix<T, FOUR>::Part, SPLIT>;
 // The first product's columns: the tokens as they lie, or, for matrices in 4 bits where all tokens fit it, from LDS, in the parts that such a
 // matrix takes and with rows that are filled up with zeros.
 template <typename T, bool FOUR, bool STAGED> struct Tokens {
@@ -300,7 +300,8 @@ __device__ __forceinline__ void result_sums(const FewArgs& a, uint32_t e, uint32
     f32x4 sum[S::kSums][M] = {};
     rows_by_columns<S, STEPS, ALIGNED>(w, row, Hidden<T, FOUR>{}, x, from, to, 0u, 1u, sum);
     if constexpr (Hidden<T, FOUR>::kSplit) {
-        // An infinity in a column has made all its sums NaN: those are formed again, in the same order, with parts that hold infinities.
+        // An infinity has made sums NaN: that of a hidden value all sums of its column, since its second part is none, that of the matrix those where it met a part that is
+        // zero.  Such sums are formed again, in products of binary32.
         bool none = false;
         for (int r = 0; r < S::kSums; ++r)
             for (int m = 0; m < M; ++m) none = none || __builtin_isunordered(sum[r][m][0], sum[r][m][1]) || __builtin_isunordered(sum[r][m][2], sum[r][m][3]);

@@ -235,3 +235,18 @@ def test_shared_results_in_a_graph_between_eager_passes():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+def test_an_infinite_element_of_the_second_matrix(t):
+    """Diagonal matrices, the second one's elements infinite: results are infinite with the sign of the hidden value, whatever bits that has."""
+    tokens, n = 64, 32
+    g = torch.Generator().manual_seed(7)
+    randn = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)  # noqa: E731
+    layer = Layer(t, False, torch.cat([torch.diag(1 + randn(n).abs()) for _ in range(2)])[None], torch.diag(torch.full((n,), math.inf))[None].nan_to_num(nan=0.0, posinf=math.inf))
+    x = Matrix(tokens, n, TYPES[t], randn(tokens, n))
+    x.view()[x.view().abs() < 0.01] = 0.5
+    got = layer(x, torch.zeros(tokens, 1), torch.rand(tokens, 1, generator=g) + 0.5)
+    gate = x.values() * layer.values[0][0, :n].diagonal()
+    up = x.values() * layer.values[0][0, n:].diagonal()
+    near(got, torch.sign(gate * torch.special.expit(gate) * up) * math.inf, torch.zeros(()))
